@@ -10,7 +10,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libress.so")
 OBJ_DIR = os.path.join(HERE, "_build")
-SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_api.cpp"]
+SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_api.cpp",
+           "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_api.cpp"]
+HEADERS = [os.path.join(CSRC, "ress_internal.h"), os.path.join(CSRC, "layer_internal.h"), os.path.join(CSRC, "tiles.h"),
+           os.path.join(HERE, "..", "include", "ress.h"), os.path.join(HERE, "..", "include", "ress_layer.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-ffp-contract=fast",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -21,8 +24,7 @@ def _up_to_date(src: str, obj: str) -> bool:
     """The object is newer than its source and every header it may include."""
     if not os.path.exists(obj):
         return False
-    deps = [os.path.join(CSRC, src), os.path.join(CSRC, "ress_internal.h"),
-            os.path.join(HERE, "..", "include", "ress.h")]
+    deps = [os.path.join(CSRC, src), *HEADERS]
     return os.path.getmtime(obj) > max(os.path.getmtime(d) for d in deps)
 
 

@@ -1,0 +1,99 @@
+// Internal declarations shared by the kernels and the C ABI layer of ress_layer.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "ress_layer.h"
+
+namespace ress {
+
+struct NormParams {
+    int64_t rows, x_stride, y_stride;
+    int width;
+    float eps;
+    bool x_f32, y_f32;
+    const void *x;
+    const float *gamma, *beta;  // null: 1, 0
+    void *y;
+    float *mean, *rstd;  // null: not wanted
+};
+
+struct NormBwdParams {
+    int64_t rows, x_stride, y_stride;
+    int width;
+    int parts;  // workgroups, each with a row of partial sums (null `part`: none wanted)
+    bool x_f32, y_f32;
+    const void *dy, *x;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    float *part;  // [parts][2][width]: dgamma, dbeta
+    float *dgamma, *dbeta;
+};
+
+// Workgroups of the backward pass: a function of rows and width alone, so that the
+// workspace is.
+int norm_bwd_parts(int64_t rows, int width);
+
+constexpr int kMaxPairs = RESS_MAX_ROPE_D / 2;
+
+struct RopeParams {
+    int H, H_all;  // heads of q; of q and k together
+    int N, n_axes, n_pairs, D;
+    bool f32, inverse, interleaved;
+    bool chunks;        // pairs 8u..8u+7 are whole 16-byte chunks (see rope.hip)
+    const int32_t *pos;
+    const void *q_in, *k_in;
+    void *q_out, *k_out;
+    ress_strides qi, ki, qo, ko;
+    double turns[kMaxPairs];   // turns per position; < 0: a pair that is copied
+    uint8_t axis[kMaxPairs];
+    uint8_t ca[kMaxPairs], cb[kMaxPairs];  // the pair's channels
+};
+
+struct WindowParams {
+    int H, H_kv, group;  // group = H / H_kv
+    int n_q, n_k, q_offset;
+    int frame, window, n_sink;
+    bool causal;
+    int n_qb, n_kb;  // blocks of 128 queries, of 128 keys
+    float scale, scale_log2;
+    ress_strides qs, ks, vs, os;
+    const uint16_t *q, *k, *v;
+    uint16_t *o;
+    float *lse;
+};
+
+struct WindowBwdParams {
+    WindowParams w;  // o: the forward's output, read; lse: read
+    ress_strides dos, dqs, dks, dvs;
+    const uint16_t *d_o;
+    uint16_t *dq, *dk, *dv;
+    float *ndelta;  // [H][n_q]: -sum_d d_o o
+    float *lse2;    // [H][n_q]: lse in base 2, +inf where a query sees nothing
+};
+
+struct DecodeParams {
+    int B, H, H_kv, group;
+    int capacity, frame, window, n_sink;
+    int splits;
+    float scale_log2;
+    int64_t q_batch, q_head, k_batch, v_batch, o_batch, o_head;
+    ress_strides ks, vs;
+    const uint16_t *q, *k, *v;
+    const int32_t *lens;
+    uint16_t *o;
+    float *part;  // [B][H][splits][66]: reference, sum, output
+};
+
+int decode_splits(const ress_decode_shape *s);
+
+hipError_t launch_norm(const NormParams &p, hipStream_t s);
+hipError_t launch_norm_bwd(const NormBwdParams &p, hipStream_t s);
+hipError_t launch_rope(const RopeParams &p, hipStream_t s);
+hipError_t launch_window(const WindowParams &p, hipStream_t s);
+hipError_t launch_window_bwd(const WindowBwdParams &p, hipStream_t s);
+hipError_t launch_decode(const DecodeParams &p, hipStream_t s);
+
+}  // namespace ress

@@ -1,0 +1,225 @@
+// Windowed attention of one new token per sequence over its cache.
+//
+// Bound by the read of the visible keys and values (256 bytes a key and head for 4 D = 256
+// flops a query head), so the products run on the vector unit: 8 lanes hold a key's or a
+// value's 64 channels, a wave 8 keys at a time, and the up to R query heads that share a
+// K/V head are formed from one read. The visible keys, sinks and window, are numbered
+// through (j -> key), so no work goes into masked ones and nothing outside them is read.
+// They are cut over `splits` workgroups, and in those over 4 waves of 64 keys a turn; every
+// 8 lanes keep an online softmax of their own, joined in a fixed order in the wave, the
+// workgroup, and for more than one split by join_kernel.
+#include "layer_internal.h"
+
+namespace ress {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
+typedef unsigned int u32x4 __attribute__((__vector_size__(16)));
+
+constexpr int kPart = 66;  // floats of a partial result: reference, sum, 64 channels
+
+__device__ __forceinline__ float lo_f(unsigned int x) { return __builtin_bit_cast(float, x << 16); }
+__device__ __forceinline__ float hi_f(unsigned int x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+
+// c + a . b of two pairs of bf16. (By value: the bit cast of a vector's element in place
+// reads its first one.)
+__device__ __forceinline__ float dot2(unsigned int a, unsigned int b, float c)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
+}
+
+// exp2(a - m), 0 for a = -inf (also against m = -inf).
+__device__ __forceinline__ float weight(float a, float m)
+{
+    return a == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a - m);
+}
+
+// What sequence b's token sees, numbered through: j < sk is key j, else key j - sk + lo.
+struct Visible {
+    int sk, lo, n;
+};
+__device__ __forceinline__ Visible visible(const DecodeParams &p, int b)
+{
+    const int len = min(max(p.lens[b], 0), p.capacity);
+    Visible v = {0, 0, 0};
+    if (len == 0) return v;
+    const int64_t lo = (int64_t)((len - 1) / p.frame - p.window + 1) * p.frame;
+    v.lo = lo > 0 ? (int)lo : 0;
+    v.sk = min(p.n_sink, v.lo);
+    v.n = v.sk + len - v.lo;
+    return v;
+}
+
+template <int R>
+__global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
+{
+    __shared__ float lds[4][R][kPart];
+    const int split = blockIdx.x, b = blockIdx.z;
+    const int tiles = (p.group + R - 1) / R;
+    const int hk = blockIdx.y / tiles, h0 = hk * p.group + (blockIdx.y % tiles) * R;
+    const int heads = min(R, (hk + 1) * p.group - h0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ch = lane & 7, oct = lane >> 3;
+    const Visible vis = visible(p, b);
+
+    // Whole turns of 64 keys, in order over the splits.
+    const int turns = (vis.n + 63) / 64, each = (turns + p.splits - 1) / p.splits;
+    const int first = split * each, last = min(first + each, turns);
+
+    u32x4 q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int h = h0 + min(r, heads - 1);
+        q[r] = *reinterpret_cast<const u32x4 *>(p.q + b * p.q_batch + h * p.q_head + ch * 8);
+    }
+    const uint16_t *kb = p.k + b * p.k_batch + hk * p.ks.head + ch * 8;
+    const uint16_t *vb = p.v + b * p.v_batch + hk * p.vs.head + ch * 8;
+
+    float m[R], l[R], acc[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[r][e] = 0.f;
+    }
+    for (int t = first + wave; t < last; t += 4) {
+        u32x4 kx[8], vx[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = t * 64 + i * 8 + oct;
+            const int64_t key = j < vis.sk ? j : j - vis.sk + vis.lo;
+            kx[i] = vx[i] = u32x4{0, 0, 0, 0};
+            if (j < vis.n) {
+                kx[i] = *reinterpret_cast<const u32x4 *>(kb + key * p.ks.token);
+                vx[i] = *reinterpret_cast<const u32x4 *>(vb + key * p.vs.token);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float s[8], top = m[r];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float d = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d = dot2(kx[i][e], q[r][e], d);
+                d += __shfl_xor(d, 1);
+                d += __shfl_xor(d, 2);
+                d += __shfl_xor(d, 4);
+                s[i] = t * 64 + i * 8 + oct < vis.n ? d * p.scale_log2 : -INFINITY;
+                top = fmaxf(top, s[i]);
+            }
+            const float a = weight(m[r], top);
+            m[r] = top;
+            l[r] *= a;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[r][e] *= a;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = weight(s[i], top);
+                l[r] += w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[r][2 * e] = fmaf(w, lo_f(vx[i][e]), acc[r][2 * e]);
+                    acc[r][2 * e + 1] = fmaf(w, hi_f(vx[i][e]), acc[r][2 * e + 1]);
+                }
+            }
+        }
+    }
+    // The wave's 8 groups of lanes, then the workgroup's waves.
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float top = m[r];
+#pragma unroll
+        for (int o = 8; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float a = weight(m[r], top);
+        l[r] *= a;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[r][e] *= a;
+#pragma unroll
+        for (int o = 8; o < 64; o <<= 1) {
+            l[r] += __shfl_xor(l[r], o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[r][e] += __shfl_xor(acc[r][e], o);
+        }
+        if (oct == 0) {
+            float *d = lds[wave][r];
+            if (ch == 0) d[0] = top, d[1] = l[r];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[2 + ch * 8 + e] = acc[r][e];
+        }
+    }
+    __syncthreads();
+    for (int r = wave; r < heads; r += 4) {
+        float top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds[w][r][0]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float a = weight(lds[w][r][0], top);
+            sum = fmaf(lds[w][r][1], a, sum);
+            o = fmaf(lds[w][r][2 + lane], a, o);
+        }
+        const int h = h0 + r;
+        if (p.splits == 1) {
+            const float y = sum == 0.f ? 0.f : o / sum;
+            p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)y);
+        } else {
+            float *d = p.part + (((int64_t)b * p.H + h) * p.splits + split) * kPart;
+            if (lane == 0) d[0] = top, d[1] = sum;
+            d[2 + lane] = o;
+        }
+    }
+}
+
+// A wave a query head: its splits in order.
+__global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
+{
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)p.B * p.H) return;
+    const int lane = threadIdx.x & 63;
+    const float *d = p.part + row * p.splits * kPart;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, d[s * kPart]);
+    for (int s = 0; s < p.splits; ++s) {
+        const float a = weight(d[s * kPart], top);
+        sum = fmaf(d[s * kPart + 1], a, sum);
+        o = fmaf(d[s * kPart + 2 + lane], a, o);
+    }
+    const int64_t b = row / p.H, h = row - b * p.H;
+    p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)(sum == 0.f ? 0.f : o / sum));
+}
+
+template <int R>
+hipError_t go(const DecodeParams &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.splits, (unsigned)(p.H_kv * ((p.group + R - 1) / R)), (unsigned)p.B);
+    hipLaunchKernelGGL(decode_kernel<R>, grid, dim3(256), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.B * p.H + 3) / 4)), dim3(256), 0, s, p);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+// Workgroups per sequence and head: enough for 4 a CU, but none with less than one turn of
+// its 4 waves.
+int decode_splits(const ress_decode_shape *s)
+{
+    if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
+    const int64_t seen = (int64_t)s->window * s->frame + s->n_sink;
+    const int64_t keys = seen < s->capacity ? seen : s->capacity;
+    const int64_t heads = (int64_t)s->B * s->H_kv * ((s->H / s->H_kv + 3) / 4);
+    const int64_t want = (1024 + heads - 1) / heads, most = (keys + 255) / 256;
+    const int64_t n = want < most ? want : most;
+    return (int)(n < 1 ? 1 : n);
+}
+
+hipError_t launch_decode(const DecodeParams &p, hipStream_t s)
+{
+    return p.group == 1 ? go<1>(p, s) : p.group == 2 ? go<2>(p, s) : go<4>(p, s);
+}
+
+}  // namespace ress

@@ -1,0 +1,368 @@
+"""Python binding of include/ress_layer.h: layer norm, rotary positions with several
+axes, and attention over a sliding window of frames with sink tokens.
+
+As in the package's other functions, a function carries its C entry point's name,
+checks tensor metadata, allocates outputs (and workspaces) with torch when the caller
+passes none, and passes pointers and the current stream of the tensors' device."""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import RESS_OK, RessError, lib
+
+DTYPE_BF16, DTYPE_F32 = 0, 1
+MAX_NORM_WIDTH = 16384
+ROPE_LAYOUTS = {"split": 0, "interleaved": 1, "sections": 2}
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
+class ress_strides(C.Structure):
+    _fields_ = [("head", C.c_int64), ("token", C.c_int64)]
+
+
+class ress_norm_shape(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int), ("x_dtype", C.c_int), ("y_dtype", C.c_int),
+                ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("eps", C.c_double)]
+
+
+class ress_rope_shape(C.Structure):
+    _fields_ = [("H", C.c_int), ("H_kv", C.c_int), ("N", C.c_int), ("D", C.c_int), ("n_axes", C.c_int),
+                ("dims", C.c_int * 4), ("layout", C.c_int), ("inverse", C.c_int), ("dtype", C.c_int),
+                ("base", C.c_double), ("q", ress_strides), ("k", ress_strides), ("q_out", ress_strides),
+                ("k_out", ress_strides)]
+
+
+class ress_window_shape(C.Structure):
+    _fields_ = [("H", C.c_int), ("H_kv", C.c_int), ("n_q", C.c_int), ("n_k", C.c_int), ("D", C.c_int),
+                ("q_offset", C.c_int), ("frame", C.c_int), ("window", C.c_int), ("n_sink", C.c_int),
+                ("causal", C.c_int), ("q", ress_strides), ("k", ress_strides), ("v", ress_strides),
+                ("o", ress_strides)]
+
+
+class ress_window_grads(C.Structure):
+    _fields_ = [("d_o", ress_strides), ("dq", ress_strides), ("dk", ress_strides), ("dv", ress_strides)]
+
+
+class ress_decode_shape(C.Structure):
+    _fields_ = [("B", C.c_int), ("H", C.c_int), ("H_kv", C.c_int), ("capacity", C.c_int), ("D", C.c_int),
+                ("frame", C.c_int), ("window", C.c_int), ("n_sink", C.c_int), ("q_batch", C.c_int64),
+                ("q_head", C.c_int64), ("k_batch", C.c_int64), ("v_batch", C.c_int64), ("k", ress_strides),
+                ("v", ress_strides), ("o_batch", C.c_int64), ("o_head", C.c_int64)]
+
+
+def _declare():
+    vp, f, sz, P = C.c_void_p, C.c_float, C.c_size_t, C.POINTER
+    for name, args in (
+            ("ress_layer_norm", [P(ress_norm_shape)] + [vp] * 7),
+            ("ress_layer_norm_bwd_workspace_size", [P(ress_norm_shape), P(sz)]),
+            ("ress_layer_norm_bwd", [P(ress_norm_shape)] + [vp] * 9 + [sz, vp]),
+            ("ress_rope", [P(ress_rope_shape)] + [vp] * 6),
+            ("ress_window_attn", [P(ress_window_shape), vp, vp, vp, f, vp, vp, vp]),
+            ("ress_window_attn_bwd_workspace_size", [P(ress_window_shape), P(sz)]),
+            ("ress_window_attn_bwd", [P(ress_window_shape), P(ress_window_grads)] + [vp] * 6 + [f] + [vp] * 4 + [sz, vp]),
+            ("ress_window_attn_decode_workspace_size", [P(ress_decode_shape), P(sz)]),
+            ("ress_window_attn_decode", [P(ress_decode_shape)] + [vp] * 4 + [f, vp, vp, sz, vp])):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, C.c_int
+
+
+_declare()
+
+
+def _call(name, device, stream, *args):
+    """Calls an entry point on `stream` (default: the device's current one) with the tensors' device
+    current, as the C ABI asks."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if device.index == torch.cuda.current_device():
+        st = getattr(lib, name)(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            st = getattr(lib, name)(*args, raw)
+    if st != RESS_OK:
+        raise RessError(st, name)
+
+
+def _size(name, shape) -> int:
+    n = C.c_size_t(0)
+    st = getattr(lib, name)(C.byref(shape), C.byref(n))
+    if st != RESS_OK:
+        raise RessError(st, name)
+    return n.value
+
+
+def _workspace(workspace, need, device, stream):
+    """The caller's workspace, or one of torch's (marked as in use on a stream that is not its own)."""
+    if workspace is None:
+        workspace = torch.empty(max(need(), 1), dtype=torch.uint8, device=device)
+        if isinstance(stream, torch.cuda.Stream) and stream != torch.cuda.current_stream(device):
+            workspace.record_stream(stream)
+    elif not (workspace.is_cuda and workspace.device == device and workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _check(name, t, dtype, shape, device):
+    """Metadata of a strided tensor whose last dimension is contiguous."""
+    if not (t.is_cuda and t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape)
+            and (t.shape[-1] <= 1 or t.stride(-1) == 1)):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
+
+
+def _check_dense(name, t, dtype, shape, device):
+    if not (t.is_cuda and t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape)
+            and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _strides(t):
+    """[heads][tokens][channels]. (The stride of a dimension of one entry says nothing: torch may give any.)"""
+    return ress_strides(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+# ---------------------------------------------------------------- layer norm
+
+
+def _norm_rows(t):
+    """Rows and their stride: [rows][width] with any row stride, or a contiguous tensor of any rank."""
+    if t.dim() == 2:
+        rows, width = t.shape
+        if width > 1 and t.stride(1) != 1:
+            raise ValueError("a row's channels must be contiguous")
+        return rows, t.stride(0) if rows > 1 else width
+    if t.dim() == 0 or not t.is_contiguous():
+        raise ValueError("tensors of other ranks than [rows][width] must be contiguous")
+    return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1]
+
+
+def _norm_shape(x, y, eps):
+    rows, xs = _norm_rows(x)
+    _, ys = _norm_rows(y)
+    return ress_norm_shape(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, ys, float(eps))
+
+
+def _norm_check(name, t, like):
+    if not (t.is_cuda and t.dtype in _DTYPES and (like is None or (t.device == like.device and t.shape == like.shape))):
+        raise ValueError(f"{name} must be a bfloat16 or float32 CUDA tensor"
+                         + ("" if like is None else f" of shape {tuple(like.shape)} on {like.device}"))
+
+
+def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, out_dtype=torch.bfloat16, mean=None,
+                    rstd=None, want_stats: bool = False, stream=None) -> dict:
+    """Layer norm over the last dimension (see include/ress_layer.h). x: bfloat16 or float32, [rows][width]
+    with any row stride, or contiguous of any rank; gamma, beta: float32 [width] or None; out: as x, of
+    out_dtype when it is made here. Returns y and, with want_stats or given buffers, mean and rstd
+    (float32, one per row) for ress_layer_norm_bwd."""
+    _norm_check("x", x, None)
+    dev = x.device
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype, device=dev)
+    _norm_check("out", out, x)
+    shape = _norm_shape(x, out, eps)
+    if want_stats and mean is None and rstd is None:
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) for _ in range(2))
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _check_dense(name, t, torch.float32, (x.shape[-1],), dev)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _check_dense(name, t, torch.float32, x.shape[:-1], dev)
+    _call("ress_layer_norm", dev, stream, C.byref(shape), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean),
+          _ptr(rstd))
+    return dict(y=out, mean=mean, rstd=rstd)
+
+
+def ress_layer_norm_bwd_workspace_size(rows: int, width: int) -> int:
+    return _size("ress_layer_norm_bwd_workspace_size",
+                 ress_norm_shape(int(rows), int(width), DTYPE_BF16, DTYPE_BF16, int(width), int(width), 1.0))
+
+
+def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta=None, want_weights: bool = True,
+                        workspace=None, stream=None) -> dict:
+    """Gradients of ress_layer_norm (see include/ress_layer.h). dy: of y's type; x, mean, rstd: as given to
+    and made by the forward pass. Returns dx (of x's type) and, with want_weights, dgamma and dbeta
+    (float32 [width])."""
+    _norm_check("x", x, None)
+    _norm_check("dy", dy, x)
+    dev, width = x.device, x.shape[-1]
+    if dx is None:
+        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev)
+    _norm_check("dx", dx, x)
+    shape = _norm_shape(x, dy, 1.0)
+    if dx.dtype != x.dtype or _norm_rows(dx) != (shape.rows, shape.x_stride):
+        raise ValueError("dx must have x's type and row stride")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _check_dense(name, t, torch.float32, x.shape[:-1], dev)
+    if gamma is not None:
+        _check_dense("gamma", gamma, torch.float32, (width,), dev)
+    if want_weights:
+        dgamma = torch.empty(width, dtype=torch.float32, device=dev) if dgamma is None else dgamma
+        dbeta = torch.empty(width, dtype=torch.float32, device=dev) if dbeta is None else dbeta
+    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
+        if t is not None:
+            _check_dense(name, t, torch.float32, (width,), dev)
+    ws, ws_bytes = None, 0
+    if dgamma is not None or dbeta is not None:
+        ws, ws_bytes = _workspace(workspace, lambda: _size("ress_layer_norm_bwd_workspace_size", shape), dev, stream)
+    _call("ress_layer_norm_bwd", dev, stream, C.byref(shape), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+          _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws_bytes)
+    return dict(dx=dx, dgamma=dgamma, dbeta=dbeta)
+
+
+# --------------------------------------------------------- rotary positions
+
+
+def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, inverse: bool = False, q_out=None,
+              k_out=None, stream=None) -> dict:
+    """Rotary positions of q [H][N][D] and k [H_kv][N][D] (either may be None; any strides with contiguous
+    channels) by pos int32 [N][axes] (see include/ress_layer.h). dims: channels of each axis; layout: "split",
+    "interleaved" or "sections"; inverse: turn back (the pass of the gradients). Outputs may be the inputs (in
+    place). Returns q and k."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("one of q and k must be given")
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}")
+    if first.dtype not in _DTYPES or first.dim() != 3:
+        raise ValueError("q and k must be bfloat16 or float32 tensors [heads][tokens][channels]")
+    dev, (_, N, D) = first.device, first.shape
+    dims = [int(d) for d in dims]
+    if not 1 <= len(dims) <= 4:
+        raise ValueError("one to four axes")
+    _check_dense("pos", pos, torch.int32, (N, len(dims)), dev)
+    none = ress_strides(0, 0)
+    s = {}
+    for name, t in (("q", q), ("k", k)):
+        if t is not None:
+            _check(name, t, first.dtype, (t.shape[0], N, D), dev)
+            s[name] = _strides(t)
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+        if like is not None:
+            _check(name, t, like.dtype, like.shape, dev)
+            s[name] = _strides(t)
+    shape = ress_rope_shape(0 if q is None else q.shape[0], 0 if k is None else k.shape[0], N, D, len(dims),
+                            (C.c_int * 4)(*dims), ROPE_LAYOUTS[layout], int(bool(inverse)), _DTYPES[first.dtype],
+                            float(base), s.get("q", none), s.get("k", none), s.get("q_out", none), s.get("k_out", none))
+    _call("ress_rope", dev, stream, C.byref(shape), _ptr(pos), _ptr(q), _ptr(k), None if q is None else _ptr(q_out),
+          None if k is None else _ptr(k_out))
+    return dict(q=None if q is None else q_out, k=None if k is None else k_out)
+
+
+# -------------------------------------------- sliding window with sink tokens
+
+
+def _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, q=None, k=None, v=None, o=None):
+    st = [ress_strides(0, 0) if t is None else _strides(t) for t in (q, k, v, o)]
+    return ress_window_shape(int(H), int(H_kv), int(n_q), int(n_k), int(D), int(q_offset), int(frame), int(window),
+                             int(n_sink), int(bool(causal)), *st)
+
+
+def _check_window(q, k, v):
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.dim() != 3:
+            raise ValueError(f"{name} must be [heads][tokens][channels]")
+    dev = q.device
+    _check("q", q, torch.bfloat16, q.shape, dev)
+    _check("k", k, torch.bfloat16, (k.shape[0], k.shape[1], q.shape[2]), dev)
+    _check("v", v, torch.bfloat16, k.shape, dev)
+    return dev
+
+
+def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q_offset: int = 0, causal: bool = True,
+                     scale: float | None = None, out=None, lse=None, want_lse: bool = False, stream=None) -> dict:
+    """Attention over a sliding window of frames and the first n_sink tokens (see include/ress_layer.h). q: bf16
+    [H][n_q][64] at positions q_offset ..; k, v: bf16 [H_kv][n_k][64]; any strides with contiguous channels.
+    Returns o (bf16, as q) and, with want_lse or a given buffer, lse (float32 [H][n_q])."""
+    dev = _check_window(q, k, v)
+    H, n_q, D = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    _check("out", out, torch.bfloat16, q.shape, dev)
+    if lse is None and want_lse:
+        lse = torch.empty((H, n_q), dtype=torch.float32, device=dev)
+    if lse is not None:
+        _check_dense("lse", lse, torch.float32, (H, n_q), dev)
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, q, k, v, out)
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    _call("ress_window_attn", dev, stream, C.byref(shape), _ptr(q), _ptr(k), _ptr(v), float(scale), _ptr(out), _ptr(lse))
+    return dict(o=out, lse=lse)
+
+
+def ress_window_attn_bwd_workspace_size(H: int, H_kv: int, n_q: int, n_k: int, *, window: int, frame: int = 1,
+                                        n_sink: int = 0, q_offset: int = 0, causal: bool = True) -> int:
+    return _size("ress_window_attn_bwd_workspace_size",
+                 _window_shape(H, H_kv, n_q, n_k, 64, q_offset, frame, window, n_sink, causal))
+
+
+def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n_sink: int = 0, q_offset: int = 0,
+                         causal: bool = True, scale: float | None = None, dq=None, dk=None, dv=None, workspace=None,
+                         stream=None) -> dict:
+    """Gradients of ress_window_attn (see include/ress_layer.h): o and lse as it made them, the other arguments
+    as it was given. Returns dq, dk, dv (bf16, as q, k, v)."""
+    dev = _check_window(q, k, v)
+    H, n_q, D = q.shape
+    _check("o", o, torch.bfloat16, q.shape, dev)
+    _check("d_o", d_o, torch.bfloat16, q.shape, dev)
+    _check_dense("lse", lse, torch.float32, (H, n_q), dev)
+    grads = []
+    for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        t = torch.empty(like.shape, dtype=torch.bfloat16, device=dev) if t is None else t
+        _check(name, t, torch.bfloat16, like.shape, dev)
+        grads.append(t)
+    dq, dk, dv = grads
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, q, k, v, o)
+    g = ress_window_grads(_strides(d_o), _strides(dq), _strides(dk), _strides(dv))
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_bwd_workspace_size", shape), dev, stream)
+    _call("ress_window_attn_bwd", dev, stream, C.byref(shape), C.byref(g), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+          _ptr(lse), float(scale), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws_bytes)
+    return dict(dq=dq, dk=dk, dv=dv)
+
+
+def ress_window_attn_decode_workspace_size(B: int, H: int, H_kv: int, capacity: int, *, window: int, frame: int = 1,
+                                           n_sink: int = 0) -> int:
+    none = ress_strides(0, 0)
+    return _size("ress_window_attn_decode_workspace_size",
+                 ress_decode_shape(int(B), int(H), int(H_kv), int(capacity), 64, int(frame), int(window), int(n_sink),
+                                   0, 0, 0, 0, none, none, 0, 0))
+
+
+def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sink: int = 0, scale: float | None = None,
+                            out=None, workspace=None, stream=None):
+    """One new token per sequence over its cache (see include/ress_layer.h). q: bf16 [B][H][64]; k, v: bf16
+    [B][H_kv][capacity][64], any strides with contiguous channels; lens: int32 [B] on the device, the new tokens
+    counted. Returns o (bf16 [B][H][64])."""
+    if q.dim() != 3 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q must be [B][H][64], k and v [B][H_kv][capacity][64]")
+    dev, (B, H, D) = q.device, q.shape
+    _check("q", q, torch.bfloat16, q.shape, dev)
+    _check("k", k, torch.bfloat16, (B, k.shape[1], k.shape[2], D), dev)
+    _check("v", v, torch.bfloat16, k.shape, dev)
+    _check_dense("lens", lens, torch.int32, (B,), dev)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    _check("out", out, torch.bfloat16, q.shape, dev)
+
+    def st(t, d):
+        return t.stride(d) if t.shape[d] > 1 else 0
+
+    shape = ress_decode_shape(B, H, k.shape[1], k.shape[2], D, int(frame), int(window), int(n_sink), st(q, 0), st(q, 1),
+                              st(k, 0), st(v, 0), ress_strides(st(k, 1), st(k, 2)), ress_strides(st(v, 1), st(v, 2)),
+                              st(out, 0), st(out, 1))
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_decode_workspace_size", shape), dev, stream)
+    _call("ress_window_attn_decode", dev, stream, C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), float(scale),
+          _ptr(out), _ptr(ws), ws_bytes)
+    return out

@@ -1,0 +1,313 @@
+"""include/ress_layer.h: exported symbols, refusals on the host, sizes of workspaces, and the float64 forms
+the GPU tests compare with (CPU only: every call here fails validation or has no work)."""
+import ctypes as C
+import math
+import os
+import re
+
+import pytest
+import torch
+
+import layer_refs as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, -1, -2, -3
+P = [C.c_void_p((1 << 41) + (n << 33)) for n in range(12)]
+
+
+@pytest.fixture(scope="module")
+def ress():
+    import paper_2609_35593_amd as r
+
+    return r
+
+
+@pytest.fixture(scope="module")
+def layer():
+    from paper_2609_35593_amd import layer as m
+
+    return m
+
+
+def test_every_declared_symbol_is_exported_and_bound(ress):
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "ress_layer.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(ress_[a-z0-9_]+)\s*\(", src)))
+    assert names == ["ress_layer_norm", "ress_layer_norm_bwd", "ress_layer_norm_bwd_workspace_size", "ress_rope",
+                     "ress_window_attn", "ress_window_attn_bwd", "ress_window_attn_bwd_workspace_size",
+                     "ress_window_attn_decode", "ress_window_attn_decode_workspace_size"]
+    raw = C.CDLL(ress.LIB_PATH)
+    for n in names:
+        assert hasattr(raw, n) and hasattr(ress, n), n
+
+
+def _norm(layer, **over):
+    a = dict(rows=100, width=1024, x_dtype=1, y_dtype=0, x_stride=1024, y_stride=1024, eps=1e-5)
+    a.update(over)
+    return layer.ress_norm_shape(*a.values())
+
+
+def test_layer_norm_refusals(ress, layer):
+    f = ress.lib.ress_layer_norm
+    s = _norm(layer)
+    call = lambda sh, x=P[0], g=P[1], b=P[2], y=P[3], m=P[4], r=P[5]: f(C.byref(sh), x, g, b, y, m, r, None)
+    for bad in (dict(rows=-1), dict(width=0), dict(x_dtype=2), dict(y_dtype=-1), dict(x_stride=1023), dict(y_stride=5),
+                dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=1e-60)):
+        assert call(_norm(layer, **bad)) == INVALID, bad
+    wide = dict(width=16385, x_stride=20000, y_stride=20000)
+    assert call(_norm(layer, **wide)) == UNSUPPORTED
+    assert call(_norm(layer, rows=1 << 31)) == UNSUPPORTED
+    assert f(None, P[0], P[1], P[2], P[3], P[4], P[5], None) == INVALID
+    assert call(s, x=None) == INVALID and call(s, y=None) == INVALID
+    assert call(s, m=None) == INVALID and call(s, r=None) == INVALID  # both or neither
+    assert call(s, x=C.c_void_p(P[0].value + 2)) == INVALID  # float32 at 2 bytes
+    assert call(s, y=C.c_void_p(P[3].value + 1)) == INVALID
+    assert call(s, y=P[0]) == INVALID  # in place across types
+    assert call(_norm(layer, y_dtype=1, y_stride=2048), y=P[0]) == INVALID  # in place across strides
+    assert call(s, m=P[3]) == INVALID and call(s, r=P[4]) == INVALID and call(s, y=P[1]) == INVALID
+    assert call(_norm(layer, rows=0), x=None, y=None) == OK
+
+
+def test_layer_norm_bwd_refusals(ress, layer):
+    f = ress.lib.ress_layer_norm_bwd
+    s = _norm(layer)
+    n = C.c_size_t(0)
+    assert ress.lib.ress_layer_norm_bwd_workspace_size(C.byref(s), C.byref(n)) == OK and n.value == 100 * 2 * 1024 * 4
+    assert ress.lib.ress_layer_norm_bwd_workspace_size(C.byref(s), None) == INVALID
+    for width in (1, 64, 512, 513, 1024, 16384):
+        assert 0 < ress.ress_layer_norm_bwd_workspace_size((1 << 31) - 1, width) <= 64 << 20
+
+    def call(sh=s, dy=P[0], x=P[1], g=P[2], m=P[3], r=P[4], dx=P[5], dg=P[6], db=P[7], ws=P[8], nb=n.value):
+        return f(C.byref(sh), dy, x, g, m, r, dx, dg, db, ws, nb, None)
+
+    assert call(ws=None) == WORKSPACE and call(nb=n.value - 1) == WORKSPACE
+    assert call(ws=C.c_void_p(P[8].value + 128)) == WORKSPACE
+    for k in ("dy", "x", "m", "r", "dx"):
+        assert call(**{k: None}) == INVALID, k
+    assert call(dx=P[0]) == INVALID  # in place of dy across types
+    assert call(dg=P[7]) == INVALID and call(dg=P[1]) == INVALID and call(db=P[2]) == INVALID and call(dx=P[3]) == INVALID
+    assert call(dx=C.c_void_p(P[5].value + 2)) == INVALID
+    assert call(_norm(layer, rows=0), dy=None, x=None, m=None, r=None, dx=None, dg=None, db=None, ws=None, nb=0) == OK
+
+
+def _rope(layer, **over):
+    st = layer.ress_strides
+    a = dict(H=4, H_kv=2, N=100, D=64, n_axes=2, dims=(32, 32, 0, 0), layout=0, inverse=0, dtype=0, base=100.0,
+             q=(6400, 64), k=(6400, 64), q_out=(6400, 64), k_out=(6400, 64))
+    a.update(over)
+    a["dims"] = (C.c_int * 4)(*a["dims"])
+    for n in ("q", "k", "q_out", "k_out"):
+        a[n] = st(*a[n])
+    return layer.ress_rope_shape(*a.values())
+
+
+def test_rope_refusals(ress, layer):
+    f = ress.lib.ress_rope
+    call = lambda sh, pos=P[0], q=P[1], k=P[2], qo=P[3], ko=P[4]: f(C.byref(sh), pos, q, k, qo, ko, None)
+    for bad in (dict(H=-1), dict(H_kv=-1), dict(N=-1), dict(D=0), dict(D=63), dict(n_axes=0), dict(dtype=2),
+                dict(layout=3), dict(layout=-1), dict(base=0.5), dict(base=float("inf")), dict(base=float("nan")),
+                dict(dims=(33, 31, 0, 0)), dict(dims=(-2, 32, 0, 0)), dict(dims=(64, 2, 0, 0)), dict(q=(-1, 64)),
+                dict(q=(6400, -64)), dict(q_out=(6400, 32)), dict(q_out=(32, 64)), dict(q_out=(0, 64)),
+                dict(k_out=(64, 64)), dict(q=(6400, (1 << 22) + 1))):
+        assert call(_rope(layer, **bad)) == INVALID, bad
+    for bad in (dict(H=257), dict(H_kv=257), dict(N=(1 << 24) + 1), dict(D=258), dict(n_axes=5)):
+        assert call(_rope(layer, **bad)) == UNSUPPORTED, bad
+    s = _rope(layer)
+    for k in ("pos", "q", "k", "qo", "ko"):
+        assert call(s, **{k: None}) == INVALID, k
+    assert call(s, q=C.c_void_p(P[1].value + 1)) == INVALID
+    assert call(s, qo=P[2]) == INVALID and call(s, ko=P[3]) == INVALID and call(s, qo=P[0]) == INVALID
+    assert call(_rope(layer, q=(64, 256)), qo=P[1]) == INVALID  # in place across strides
+    assert call(_rope(layer, N=0), pos=None, q=None, k=None, qo=None, ko=None) == OK
+    assert call(_rope(layer, H=0, H_kv=0), pos=None, q=None, k=None, qo=None, ko=None) == OK
+    assert f(None, P[0], P[1], P[2], P[3], P[4], None) == INVALID
+
+
+def _win(layer, **over):
+    st = layer.ress_strides
+    a = dict(H=4, H_kv=2, n_q=100, n_k=200, D=64, q_offset=100, frame=10, window=3, n_sink=5, causal=1, q=(6400, 64),
+             k=(12800, 64), v=(12800, 64), o=(6400, 64))
+    a.update(over)
+    for n in "qkvo":
+        a[n] = st(*a[n])
+    return layer.ress_window_shape(*a.values())
+
+
+BAD_WINDOWS = (dict(H=-1), dict(H_kv=-1), dict(H_kv=3), dict(H_kv=0), dict(H=0), dict(n_q=-1), dict(n_k=-1),
+               dict(q_offset=-1), dict(frame=0), dict(window=0), dict(n_sink=-1))
+FAR_WINDOWS = (dict(H=258), dict(D=32), dict(n_q=(1 << 24) + 1), dict(n_k=(1 << 24) + 1), dict(q_offset=(1 << 24) + 1))
+
+
+def test_window_refusals(ress, layer):
+    f = ress.lib.ress_window_attn
+
+    def call(sh, q=P[0], k=P[1], v=P[2], scale=0.125, o=P[3], lse=P[4]):
+        return f(C.byref(sh), q, k, v, scale, o, lse, None)
+
+    s = _win(layer)
+    for bad in BAD_WINDOWS + (dict(q=(6400, 4)), dict(k=(12, 64)), dict(v=(-64, 64)), dict(o=(6400, 32)),
+                              dict(o=(64, 64)), dict(o=(0, 0)), dict(k=(64, (1 << 22) + 8))):
+        assert call(_win(layer, **bad)) == INVALID, bad
+    for bad in FAR_WINDOWS:
+        assert call(_win(layer, **bad)) == UNSUPPORTED, bad
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(s, scale=scale) == INVALID
+    for k in "qkvo":
+        assert call(s, **{k: None}) == INVALID, k
+        assert call(s, **{k: C.c_void_p((1 << 41) + 8)}) == INVALID, k
+    for x in P[:3]:
+        assert call(s, o=x) == INVALID
+    assert call(s, lse=P[3]) == INVALID and call(s, lse=P[0]) == INVALID
+    assert f(None, P[0], P[1], P[2], 0.125, P[3], None, None) == INVALID
+    assert call(_win(layer, n_q=0), q=None, o=None, lse=None) == OK
+    assert call(_win(layer, H=0, H_kv=0), q=None, k=None, v=None, o=None) == OK
+
+
+def test_window_bwd_refusals(ress, layer):
+    f = ress.lib.ress_window_attn_bwd
+    st = layer.ress_strides
+    s = _win(layer)
+    n = C.c_size_t(0)
+    assert ress.lib.ress_window_attn_bwd_workspace_size(C.byref(s), C.byref(n)) == OK and n.value > 0
+    assert ress.lib.ress_window_attn_bwd_workspace_size(C.byref(s), None) == INVALID
+
+    def grads(**over):
+        a = dict(d_o=(6400, 64), dq=(6400, 64), dk=(12800, 64), dv=(12800, 64))
+        a.update(over)
+        return layer.ress_window_grads(*[st(*x) for x in a.values()])
+
+    names = ("d_o", "q", "k", "v", "o", "lse", "dq", "dk", "dv")
+
+    def call(sh=s, g=None, scale=0.125, ws=P[9], nb=n.value, **over):
+        a = dict(zip(names, P))
+        a.update(over)
+        g = grads() if g is None else g
+        return f(C.byref(sh), C.byref(g), *[a[x] for x in names[:6]], scale, *[a[x] for x in names[6:]], ws, nb, None)
+
+    for bad in BAD_WINDOWS:
+        assert call(_win(layer, **bad)) == INVALID, bad
+    for bad in FAR_WINDOWS:
+        assert call(_win(layer, **bad)) == UNSUPPORTED, bad
+    for k in names:
+        assert call(**{k: None}) == INVALID, k
+        assert call(**{k: C.c_void_p(P[names.index(k)].value + 2)}) == INVALID, k
+    for a in ("dq", "dk", "dv"):
+        for b in names[:6]:
+            assert call(**{a: P[names.index(b)]}) == INVALID, (a, b)
+    assert call(dk=P[6]) == INVALID and call(dv=P[7]) == INVALID
+    for bad in (dict(dq=(6400, 32)), dict(dk=(64, 64)), dict(dv=(0, 64)), dict(d_o=(4, 64)), dict(dk=(0, 0))):
+        assert call(g=grads(**bad)) == INVALID, bad
+    assert call(scale=0.0) == INVALID
+    assert call(ws=None) == WORKSPACE and call(nb=n.value - 1) == WORKSPACE
+    assert call(ws=C.c_void_p(P[9].value + 64)) == WORKSPACE
+    assert call(_win(layer, H=0, H_kv=0), ws=None, nb=0) == OK
+    assert call(_win(layer, n_q=0, n_k=0), ws=None, nb=0, **{k: None for k in names}) == OK
+
+
+def _dec(layer, **over):
+    st = layer.ress_strides
+    a = dict(B=3, H=8, H_kv=2, capacity=100, D=64, frame=1, window=10, n_sink=4, q_batch=512, q_head=64, k_batch=12800,
+             v_batch=12800, k=(6400, 64), v=(6400, 64), o_batch=512, o_head=64)
+    a.update(over)
+    a["k"], a["v"] = st(*a["k"]), st(*a["v"])
+    return layer.ress_decode_shape(*a.values())
+
+
+def test_decode_refusals(ress, layer):
+    f = ress.lib.ress_window_attn_decode
+
+    def call(sh, q=P[0], k=P[1], v=P[2], lens=P[3], scale=0.125, o=P[4], ws=None, nb=0):
+        return f(C.byref(sh), q, k, v, lens, scale, o, ws, nb, None)
+
+    for bad in (dict(B=-1), dict(H=-1), dict(H_kv=3), dict(H_kv=0), dict(capacity=-1), dict(frame=0), dict(window=0),
+                dict(n_sink=-1), dict(q_batch=-512), dict(q_head=4), dict(k_batch=12), dict(v_batch=-8),
+                dict(k=(4, 64)), dict(v=(64, (1 << 22) + 8)), dict(o_head=32), dict(o_batch=64), dict(o_batch=0)):
+        assert call(_dec(layer, **bad)) == INVALID, bad
+    for bad in (dict(B=65536), dict(D=128), dict(capacity=(1 << 24) + 1), dict(H=264)):
+        assert call(_dec(layer, **bad)) == UNSUPPORTED, bad
+    s = _dec(layer)
+    for k in ("q", "k", "v", "lens", "o"):
+        assert call(s, **{k: None}) == INVALID, k
+        assert call(s, **{k: C.c_void_p((1 << 41) + 2)}) == INVALID, k
+    for x in P[:4]:
+        assert call(s, o=x) == INVALID
+    assert call(s, scale=float("nan")) == INVALID
+    long = _dec(layer, capacity=20000, window=15000, k=(64 * 20000, 64), v=(64 * 20000, 64))
+    n = C.c_size_t(0)
+    assert ress.lib.ress_window_attn_decode_workspace_size(C.byref(long), C.byref(n)) == OK and n.value > 0
+    assert ress.lib.ress_window_attn_decode_workspace_size(C.byref(long), None) == INVALID
+    assert call(long) == WORKSPACE and call(long, ws=P[5], nb=n.value - 1) == WORKSPACE
+    assert call(long, ws=C.c_void_p(P[5].value + 16), nb=n.value) == WORKSPACE
+    assert call(_dec(layer, B=0), q=None, k=None, v=None, lens=None, o=None) == OK
+
+
+def test_binding_refuses_host_tensors_and_shapes(ress):
+    x = torch.zeros(4, 64)
+    b = torch.zeros(2, 8, 64, dtype=torch.bfloat16)
+    for call in (lambda: ress.ress_layer_norm(x), lambda: ress.ress_layer_norm_bwd(x, x, None, x[:, 0], x[:, 0]),
+                 lambda: ress.ress_rope(b, b, torch.zeros(8, 2, dtype=torch.int32), dims=(32, 32)),
+                 lambda: ress.ress_rope(None, None, None, dims=(32, 32)),
+                 lambda: ress.ress_rope(b, b, None, dims=(32, 32), layout="halves"),
+                 lambda: ress.ress_window_attn(b, b, b, window=4), lambda: ress.ress_window_attn(b[0], b, b, window=4),
+                 lambda: ress.ress_window_attn_bwd(b, b, b, b, b, x, window=4),
+                 lambda: ress.ress_window_attn_decode(b, b, b, torch.zeros(2, dtype=torch.int32), window=4)):
+        with pytest.raises(ValueError):
+            call()
+
+
+# ------------------------------------------------- the float64 forms themselves
+
+
+def test_reference_window_by_hand():
+    """The visible sets, written out for a small case."""
+    vis = R.visible(6, 6, 0, 2, 1, 1, True)
+    assert [r.nonzero()[:, 0].tolist() for r in vis] == [[0, 1], [0, 1], [0, 2, 3], [0, 2, 3], [0, 4, 5], [0, 4, 5]]
+    vis = R.visible(2, 7, 3, 2, 2, 0, False)
+    assert [r.nonzero()[:, 0].tolist() for r in vis] == [[0, 1, 2, 3, 4, 5], [2, 3, 4, 5, 6]]
+    assert not R.visible(2, 4, 9, 1, 2, 0, True).any()
+    assert R.visible(1, 4, 9, 1, 2, 3, True)[0].tolist() == [True, True, True, False]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_reference_gradients_against_differences(causal):
+    """window_bwd against central differences of window, norm_bwd of norm: differences of float64 functions with a step
+    of 1e-5 are good to about 1e-9."""
+    g = torch.Generator().manual_seed(5)
+    q, k, v, do = (torch.randn(h, n, 64, generator=g).double() for h, n in ((4, 7), (2, 9), (2, 9), (4, 7)))
+    vis = R.visible(7, 9, 2, 2, 2, 1, causal)
+    dq, dk, dv = R.window_bwd(do, q, k, v, vis)[:3]
+    loss = lambda: float((R.window(q, k, v, vis)[0] * do).sum())
+    for t, grad in ((q, dq), (k, dk), (v, dv)):
+        for _ in range(12):
+            i = tuple(int(torch.randint(n, (1,), generator=g)) for n in t.shape)
+            x = t[i].item()
+            t[i] = x + 1e-5
+            up = loss()
+            t[i] = x - 1e-5
+            down = loss()
+            t[i] = x
+            assert abs((up - down) / 2e-5 - grad[i].item()) < 1e-7
+    x, gamma, beta, dy = (torch.randn(*s, generator=g).double() for s in ((3, 10), (10,), (10,), (3, 10)))
+    _, mean, rstd = R.norm(x, gamma, beta, 1e-5)
+    dx, dg, db = R.norm_bwd(dy, x, gamma, mean, rstd)
+    for t, grad in ((x, dx), (gamma, dg), (beta, db)):
+        for i in range(t.numel()):
+            f = t.view(-1)
+            o = f[i].item()
+            f[i] = o + 1e-5
+            up = float((R.norm(x, gamma, beta, 1e-5)[0] * dy).sum())
+            f[i] = o - 1e-5
+            down = float((R.norm(x, gamma, beta, 1e-5)[0] * dy).sum())
+            f[i] = o
+            assert abs((up - down) / 2e-5 - grad.view(-1)[i].item()) < 1e-7
+
+
+@pytest.mark.parametrize("layout", ["split", "interleaved", "sections"])
+def test_reference_rope_keeps_relative_positions(layout):
+    """Scores of turned vectors depend on differences of positions only; the inverse turns back."""
+    g = torch.Generator().manual_seed(6)
+    q, k = (torch.randn(1, 1, 64, generator=g).double() for _ in range(2))
+    a, b = (torch.randint(0, 1000, (1, 3), generator=g) for _ in range(2))
+    kw = dict(dims=(16, 24, 20), layout=layout, base=1e4)
+    dot = lambda pa, pb: float((R.rope(q, pa, **kw) * R.rope(k, pb, **kw)).sum())
+    assert math.isclose(dot(a, b), dot(a + 77, b + 77), rel_tol=0, abs_tol=1e-9)
+    assert torch.allclose(R.rope(R.rope(q, a, **kw), a, inverse=True, **kw), q, rtol=0, atol=1e-12)
