@@ -20,6 +20,7 @@ namespace ress {
 namespace tiles {
 
 typedef __bf16 bf16x8 __attribute__((__vector_size__(8 * sizeof(__bf16))));
+typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 typedef short s16x4 __attribute__((__vector_size__(4 * sizeof(short))));
 typedef short s16x8 __attribute__((__vector_size__(8 * sizeof(short))));
 typedef float f32x16 __attribute__((__vector_size__(16 * sizeof(float))));
@@ -116,6 +117,17 @@ __device__ __forceinline__ void pack(const f32x16 &x, bf16x8 (&b)[2])
     for (int u = 0; u < 2; ++u)
         b[u] = bf16x8{(__bf16)x[8 * u + 0], (__bf16)x[8 * u + 1], (__bf16)x[8 * u + 2], (__bf16)x[8 * u + 3],
                       (__bf16)x[8 * u + 4], (__bf16)x[8 * u + 5], (__bf16)x[8 * u + 6], (__bf16)x[8 * u + 7]};
+}
+
+// sum + the 16 values of two packed operands, in pairs.
+__device__ __forceinline__ float add_up(const bf16x8 (&b)[2], float sum)
+{
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{b[u][j], b[u][j + 1]}, ones, sum, false);
+    return sum;
 }
 
 // One row (column l%32 of two transposed accumulators of 32 channels each) times `f`, to

@@ -22,8 +22,6 @@ namespace {
 
 using namespace tiles;
 
-typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
-
 constexpr float kSumLimit = 0x1p50f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

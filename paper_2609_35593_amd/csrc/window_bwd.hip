@@ -7,10 +7,10 @@
 //   dq_kernel     128 queries a workgroup, walking over the key tiles they see:
 //                 S^T = K Q^T, dP^T = V dO^T - delta, dQ^T += K^T dS^T. delta off by e leaves
 //                 -e (sum P k) in dQ, which for keys with a common part outweighs dQ itself,
-//                 and o is rounded to bf16; so sum dS = e is summed as well (it is 0 for the
-//                 true delta), B^T += K^T P^T beside it, and dQ takes back e B (without it
-//                 dq was 1-1.5% off in norm where keys share a mean). The corrected delta goes
-//                 to the next kernel;
+//                 and o is rounded to bf16, as dS is for its product; so sum dS = e (0 for the
+//                 true delta and unrounded dS) is summed from the rounded values as well,
+//                 B^T += K^T P^T beside it, and dQ takes back e B (without it dq was 1-1.5% off
+//                 in norm where keys share a mean). The corrected delta goes to the next kernel;
 //   dkv_kernel    128 keys a workgroup, walking over the tiles of queries that see them,
 //                 query head after query head of those that share the keys:
 //                 S = Q K^T, dP = dO V^T - delta, dV^T += dO^T P, dK^T += Q^T dS.
@@ -137,11 +137,11 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
                 for (int v = 0; v < 16; ++v) {
                     s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
                     d[v] *= s[v];
-                    off += d[v];
                 }
                 bf16x8 pb[2], db[2];
                 pack(s, pb);
                 pack(d, db);
+                off = add_up(db, off);
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
