@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 
 import torch
 
@@ -19,77 +20,57 @@ ROPE_LAYOUTS = {"split": 0, "interleaved": 1, "sections": 2}
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
 
 
-class ress_strides(C.Structure):
-    _fields_ = [("head", C.c_int64), ("token", C.c_int64)]
-
-
-class ress_norm_shape(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("width", C.c_int), ("x_dtype", C.c_int), ("y_dtype", C.c_int),
-                ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("eps", C.c_double)]
-
-
-class ress_rope_shape(C.Structure):
-    _fields_ = [("H", C.c_int), ("H_kv", C.c_int), ("N", C.c_int), ("D", C.c_int), ("n_axes", C.c_int),
-                ("dims", C.c_int * 4), ("layout", C.c_int), ("inverse", C.c_int), ("dtype", C.c_int),
-                ("base", C.c_double), ("q", ress_strides), ("k", ress_strides), ("q_out", ress_strides),
-                ("k_out", ress_strides)]
-
-
-class ress_window_shape(C.Structure):
-    _fields_ = [("H", C.c_int), ("H_kv", C.c_int), ("n_q", C.c_int), ("n_k", C.c_int), ("D", C.c_int),
-                ("q_offset", C.c_int), ("frame", C.c_int), ("window", C.c_int), ("n_sink", C.c_int),
-                ("causal", C.c_int), ("q", ress_strides), ("k", ress_strides), ("v", ress_strides),
-                ("o", ress_strides)]
-
-
-class ress_window_grads(C.Structure):
-    _fields_ = [("d_o", ress_strides), ("dq", ress_strides), ("dk", ress_strides), ("dv", ress_strides)]
-
-
-class ress_decode_shape(C.Structure):
-    _fields_ = [("B", C.c_int), ("H", C.c_int), ("H_kv", C.c_int), ("capacity", C.c_int), ("D", C.c_int),
-                ("frame", C.c_int), ("window", C.c_int), ("n_sink", C.c_int), ("q_batch", C.c_int64),
-                ("q_head", C.c_int64), ("k_batch", C.c_int64), ("v_batch", C.c_int64), ("k", ress_strides),
-                ("v", ress_strides), ("o_batch", C.c_int64), ("o_head", C.c_int64)]
+# The shapes of ress_layer.h, packed as C lays them out (strides are pairs head, token). Packing takes a tenth of the
+# time that filling in ctypes structures does, which shows in calls of a few microseconds.
+_NORM = struct.Struct("@q3i2qd").pack      # rows; width, x_dtype, y_dtype; x_stride, y_stride; eps
+_ROPE = struct.Struct("@12id8q").pack      # H, H_kv, N, D, n_axes, dims[4], layout, inverse, dtype; base; q, k, q_out, k_out
+_WINDOW = struct.Struct("@10i8q").pack     # H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal; q, k, v, o
+_GRADS = struct.Struct("@8q").pack         # d_o, dq, dk, dv
+_DECODE = struct.Struct("@8i10q").pack     # B, H, H_kv, capacity, D, frame, window, n_sink; q_batch, q_head, k_batch,
+                                           # v_batch, k, v, o_batch, o_head
 
 
 def _declare():
-    vp, f, sz, P = C.c_void_p, C.c_float, C.c_size_t, C.POINTER
+    vp, f, sz = C.c_void_p, C.c_float, C.c_size_t
     for name, args in (
-            ("ress_layer_norm", [P(ress_norm_shape)] + [vp] * 7),
-            ("ress_layer_norm_bwd_workspace_size", [P(ress_norm_shape), P(sz)]),
-            ("ress_layer_norm_bwd", [P(ress_norm_shape)] + [vp] * 9 + [sz, vp]),
-            ("ress_rope", [P(ress_rope_shape)] + [vp] * 6),
-            ("ress_window_attn", [P(ress_window_shape), vp, vp, vp, f, vp, vp, vp]),
-            ("ress_window_attn_bwd_workspace_size", [P(ress_window_shape), P(sz)]),
-            ("ress_window_attn_bwd", [P(ress_window_shape), P(ress_window_grads)] + [vp] * 6 + [f] + [vp] * 4 + [sz, vp]),
-            ("ress_window_attn_decode_workspace_size", [P(ress_decode_shape), P(sz)]),
-            ("ress_window_attn_decode", [P(ress_decode_shape)] + [vp] * 4 + [f, vp, vp, sz, vp])):
+            ("ress_layer_norm", [vp] * 8),
+            ("ress_layer_norm_bwd_workspace_size", [vp, vp]),
+            ("ress_layer_norm_bwd", [vp] * 10 + [sz, vp]),
+            ("ress_rope", [vp] * 7),
+            ("ress_window_attn", [vp] * 4 + [f, vp, vp, vp]),
+            ("ress_window_attn_bwd_workspace_size", [vp, vp]),
+            ("ress_window_attn_bwd", [vp] * 8 + [f] + [vp] * 4 + [sz, vp]),
+            ("ress_window_attn_decode_workspace_size", [vp, vp]),
+            ("ress_window_attn_decode", [vp] * 5 + [f, vp, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, C.c_int
 
 
 _declare()
+# The current stream of a device as an address, without a Stream object around it where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _call(name, device, stream, *args):
+def _call(fn, device, stream, *args):
     """Calls an entry point on `stream` (default: the device's current one) with the tensors' device
     current, as the C ABI asks."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        stream = _raw_stream(device.index)
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        st = getattr(lib, name)(*args, raw)
+        st = fn(*args, stream)
     else:
         with torch.cuda.device(device):
-            st = getattr(lib, name)(*args, raw)
+            st = fn(*args, stream)
     if st != RESS_OK:
-        raise RessError(st, name)
+        raise RessError(st, fn.__name__)
 
 
 def _size(name, shape) -> int:
     n = C.c_size_t(0)
-    st = getattr(lib, name)(C.byref(shape), C.byref(n))
+    st = getattr(lib, name)(shape, C.byref(n))
     if st != RESS_OK:
         raise RessError(st, name)
     return n.value
@@ -108,15 +89,19 @@ def _workspace(workspace, need, device, stream):
 
 def _check(name, t, dtype, shape, device):
     """Metadata of a strided tensor whose last dimension is contiguous."""
-    if not (t.is_cuda and t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape)
-            and (t.shape[-1] <= 1 or t.stride(-1) == 1)):
+    if not (t.dtype is dtype and t.shape == shape and t.device == device and (t.stride(-1) == 1 or t.shape[-1] <= 1)):
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
 
 
 def _check_dense(name, t, dtype, shape, device):
-    if not (t.is_cuda and t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape)
-            and t.is_contiguous()):
+    if not (t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _device(name, t):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.device
 
 
 def _ptr(t):
@@ -124,8 +109,10 @@ def _ptr(t):
 
 
 def _strides(t):
-    """[heads][tokens][channels]. (The stride of a dimension of one entry says nothing: torch may give any.)"""
-    return ress_strides(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+    """Of [heads][tokens][channels]. (The stride of a dimension of one entry says nothing: torch may give any.)"""
+    n, m, _ = t.shape
+    head, token, _ = t.stride()
+    return head if n > 1 else 0, token if m > 1 else 0
 
 
 # ---------------------------------------------------------------- layer norm
@@ -146,11 +133,11 @@ def _norm_rows(t):
 def _norm_shape(x, y, eps):
     rows, xs = _norm_rows(x)
     _, ys = _norm_rows(y)
-    return ress_norm_shape(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, ys, float(eps))
+    return _NORM(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, ys, eps)
 
 
 def _norm_check(name, t, like):
-    if not (t.is_cuda and t.dtype in _DTYPES and (like is None or (t.device == like.device and t.shape == like.shape))):
+    if t.dtype not in _DTYPES or (like is not None and (t.shape != like.shape or t.device != like.device)):
         raise ValueError(f"{name} must be a bfloat16 or float32 CUDA tensor"
                          + ("" if like is None else f" of shape {tuple(like.shape)} on {like.device}"))
 
@@ -161,8 +148,8 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     with any row stride, or contiguous of any rank; gamma, beta: float32 [width] or None; out: as x, of
     out_dtype when it is made here. Returns y and, with want_stats or given buffers, mean and rstd
     (float32, one per row) for ress_layer_norm_bwd."""
+    dev = _device("x", x)
     _norm_check("x", x, None)
-    dev = x.device
     if out is None:
         out = torch.empty(x.shape, dtype=out_dtype, device=dev)
     _norm_check("out", out, x)
@@ -175,14 +162,14 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t is not None:
             _check_dense(name, t, torch.float32, x.shape[:-1], dev)
-    _call("ress_layer_norm", dev, stream, C.byref(shape), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean),
+    _call(lib.ress_layer_norm, dev, stream, shape, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean),
           _ptr(rstd))
     return dict(y=out, mean=mean, rstd=rstd)
 
 
 def ress_layer_norm_bwd_workspace_size(rows: int, width: int) -> int:
     return _size("ress_layer_norm_bwd_workspace_size",
-                 ress_norm_shape(int(rows), int(width), DTYPE_BF16, DTYPE_BF16, int(width), int(width), 1.0))
+                 _NORM(rows, width, DTYPE_BF16, DTYPE_BF16, width, width, 1.0))
 
 
 def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta=None, want_weights: bool = True,
@@ -190,14 +177,14 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     """Gradients of ress_layer_norm (see include/ress_layer.h). dy: of y's type; x, mean, rstd: as given to
     and made by the forward pass. Returns dx (of x's type) and, with want_weights, dgamma and dbeta
     (float32 [width])."""
+    dev, width = _device("x", x), x.shape[-1]
     _norm_check("x", x, None)
     _norm_check("dy", dy, x)
-    dev, width = x.device, x.shape[-1]
     if dx is None:
         dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev)
     _norm_check("dx", dx, x)
     shape = _norm_shape(x, dy, 1.0)
-    if dx.dtype != x.dtype or _norm_rows(dx) != (shape.rows, shape.x_stride):
+    if dx.dtype != x.dtype or _norm_rows(dx) != _norm_rows(x):
         raise ValueError("dx must have x's type and row stride")
     for name, t in (("mean", mean), ("rstd", rstd)):
         _check_dense(name, t, torch.float32, x.shape[:-1], dev)
@@ -212,7 +199,7 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     ws, ws_bytes = None, 0
     if dgamma is not None or dbeta is not None:
         ws, ws_bytes = _workspace(workspace, lambda: _size("ress_layer_norm_bwd_workspace_size", shape), dev, stream)
-    _call("ress_layer_norm_bwd", dev, stream, C.byref(shape), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+    _call(lib.ress_layer_norm_bwd, dev, stream, shape, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
           _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws_bytes)
     return dict(dx=dx, dgamma=dgamma, dbeta=dbeta)
 
@@ -233,47 +220,52 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
         raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}")
     if first.dtype not in _DTYPES or first.dim() != 3:
         raise ValueError("q and k must be bfloat16 or float32 tensors [heads][tokens][channels]")
-    dev, (_, N, D) = first.device, first.shape
-    dims = [int(d) for d in dims]
-    if not 1 <= len(dims) <= 4:
+    dev, (_, N, D) = _device("q and k", first), first.shape
+    axes = len(dims)
+    if not 1 <= axes <= 4:
         raise ValueError("one to four axes")
-    _check_dense("pos", pos, torch.int32, (N, len(dims)), dev)
-    none = ress_strides(0, 0)
-    s = {}
-    for name, t in (("q", q), ("k", k)):
-        if t is not None:
-            _check(name, t, first.dtype, (t.shape[0], N, D), dev)
-            s[name] = _strides(t)
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
-    for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
-        if like is not None:
-            _check(name, t, like.dtype, like.shape, dev)
-            s[name] = _strides(t)
-    shape = ress_rope_shape(0 if q is None else q.shape[0], 0 if k is None else k.shape[0], N, D, len(dims),
-                            (C.c_int * 4)(*dims), ROPE_LAYOUTS[layout], int(bool(inverse)), _DTYPES[first.dtype],
-                            float(base), s.get("q", none), s.get("k", none), s.get("q_out", none), s.get("k_out", none))
-    _call("ress_rope", dev, stream, C.byref(shape), _ptr(pos), _ptr(q), _ptr(k), None if q is None else _ptr(q_out),
-          None if k is None else _ptr(k_out))
-    return dict(q=None if q is None else q_out, k=None if k is None else k_out)
+    _check_dense("pos", pos, torch.int32, (N, axes), dev)
+    H = H_kv = 0
+    qs = ks = qo = ko = (0, 0)
+    if q is not None:
+        H = q.shape[0]
+        _check("q", q, first.dtype, (H, N, D), dev)
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
+        _check("q_out", q_out, q.dtype, q.shape, dev)
+        qs, qo = _strides(q), _strides(q_out)
+    else:
+        q_out = None
+    if k is not None:
+        H_kv = k.shape[0]
+        _check("k", k, first.dtype, (H_kv, N, D), dev)
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev) if k_out is None else k_out
+        _check("k_out", k_out, k.dtype, k.shape, dev)
+        ks, ko = _strides(k), _strides(k_out)
+    else:
+        k_out = None
+    shape = _ROPE(H, H_kv, N, D, axes, *dims, *(0,) * (4 - axes), ROPE_LAYOUTS[layout], bool(inverse), _DTYPES[first.dtype],
+                  base, *qs, *ks, *qo, *ko)
+    _call(lib.ress_rope, dev, stream, shape, _ptr(pos), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out))
+    return dict(q=q_out, k=k_out)
 
 
 # -------------------------------------------- sliding window with sink tokens
 
 
-def _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, q=None, k=None, v=None, o=None):
-    st = [ress_strides(0, 0) if t is None else _strides(t) for t in (q, k, v, o)]
-    return ress_window_shape(int(H), int(H_kv), int(n_q), int(n_k), int(D), int(q_offset), int(frame), int(window),
-                             int(n_sink), int(bool(causal)), *st)
+def _int32(n):
+    """Windows, frames and sink counts beyond every position act alike: the largest int stands for them."""
+    return n if n < 2147483647 else 2147483647
+
+
+def _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, strides=(0,) * 8):
+    return _WINDOW(H, H_kv, n_q, n_k, D, q_offset, _int32(frame), _int32(window), _int32(n_sink), bool(causal), *strides)
 
 
 def _check_window(q, k, v):
+    dev = _device("q", q)
     for name, t in (("q", q), ("k", k), ("v", v)):
         if t.dim() != 3:
             raise ValueError(f"{name} must be [heads][tokens][channels]")
-    dev = q.device
     _check("q", q, torch.bfloat16, q.shape, dev)
     _check("k", k, torch.bfloat16, (k.shape[0], k.shape[1], q.shape[2]), dev)
     _check("v", v, torch.bfloat16, k.shape, dev)
@@ -294,9 +286,10 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
         lse = torch.empty((H, n_q), dtype=torch.float32, device=dev)
     if lse is not None:
         _check_dense("lse", lse, torch.float32, (H, n_q), dev)
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, q, k, v, out)
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal,
+                          _strides(q) + _strides(k) + _strides(v) + _strides(out))
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    _call("ress_window_attn", dev, stream, C.byref(shape), _ptr(q), _ptr(k), _ptr(v), float(scale), _ptr(out), _ptr(lse))
+    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), scale, _ptr(out), _ptr(lse))
     return dict(o=out, lse=lse)
 
 
@@ -322,21 +315,20 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
         _check(name, t, torch.bfloat16, like.shape, dev)
         grads.append(t)
     dq, dk, dv = grads
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, q, k, v, o)
-    g = ress_window_grads(_strides(d_o), _strides(dq), _strides(dk), _strides(dv))
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal,
+                          _strides(q) + _strides(k) + _strides(v) + _strides(o))
+    g = _GRADS(*_strides(d_o), *_strides(dq), *_strides(dk), *_strides(dv))
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_bwd_workspace_size", shape), dev, stream)
-    _call("ress_window_attn_bwd", dev, stream, C.byref(shape), C.byref(g), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-          _ptr(lse), float(scale), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws_bytes)
+    _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), scale,
+          _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws_bytes)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
 def ress_window_attn_decode_workspace_size(B: int, H: int, H_kv: int, capacity: int, *, window: int, frame: int = 1,
                                            n_sink: int = 0) -> int:
-    none = ress_strides(0, 0)
     return _size("ress_window_attn_decode_workspace_size",
-                 ress_decode_shape(int(B), int(H), int(H_kv), int(capacity), 64, int(frame), int(window), int(n_sink),
-                                   0, 0, 0, 0, none, none, 0, 0))
+                 _DECODE(B, H, H_kv, capacity, 64, _int32(frame), _int32(window), _int32(n_sink), *(0,) * 10))
 
 
 def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sink: int = 0, scale: float | None = None,
@@ -346,23 +338,31 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     counted. Returns o (bf16 [B][H][64])."""
     if q.dim() != 3 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q must be [B][H][64], k and v [B][H_kv][capacity][64]")
-    dev, (B, H, D) = q.device, q.shape
+    dev, (B, H, D) = _device("q", q), q.shape
+    _, H_kv, capacity, _ = k.shape
     _check("q", q, torch.bfloat16, q.shape, dev)
-    _check("k", k, torch.bfloat16, (B, k.shape[1], k.shape[2], D), dev)
+    _check("k", k, torch.bfloat16, (B, H_kv, capacity, D), dev)
     _check("v", v, torch.bfloat16, k.shape, dev)
     _check_dense("lens", lens, torch.int32, (B,), dev)
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
     _check("out", out, torch.bfloat16, q.shape, dev)
-
-    def st(t, d):
-        return t.stride(d) if t.shape[d] > 1 else 0
-
-    shape = ress_decode_shape(B, H, k.shape[1], k.shape[2], D, int(frame), int(window), int(n_sink), st(q, 0), st(q, 1),
-                              st(k, 0), st(v, 0), ress_strides(st(k, 1), st(k, 2)), ress_strides(st(v, 1), st(v, 2)),
-                              st(out, 0), st(out, 1))
+    q_b, q_h, _ = q.stride()
+    k_b, k_h, k_t, _ = k.stride()
+    v_b, v_h, v_t, _ = v.stride()
+    o_b, o_h, _ = out.stride()
+    if B <= 1:  # (the stride of a dimension of one entry says nothing)
+        q_b = k_b = v_b = o_b = 0
+    if H <= 1:
+        q_h = o_h = 0
+    if H_kv <= 1:
+        k_h = v_h = 0
+    if capacity <= 1:
+        k_t = v_t = 0
+    shape = _DECODE(B, H, H_kv, capacity, D, _int32(frame), _int32(window), _int32(n_sink), q_b, q_h, k_b, v_b, k_h, k_t,
+                    v_h, v_t, o_b, o_h)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_decode_workspace_size", shape), dev, stream)
-    _call("ress_window_attn_decode", dev, stream, C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), float(scale),
-          _ptr(out), _ptr(ws), ws_bytes)
+    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), scale, _ptr(out), _ptr(ws),
+          ws_bytes)
     return out

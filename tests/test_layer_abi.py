@@ -24,9 +24,9 @@ def ress():
 
 @pytest.fixture(scope="module")
 def layer():
-    from paper_2609_35593_amd import layer as m
+    import layer_structs
 
-    return m
+    return layer_structs
 
 
 def test_every_declared_symbol_is_exported_and_bound(ress):
@@ -252,6 +252,23 @@ def test_binding_refuses_host_tensors_and_shapes(ress):
                  lambda: ress.ress_window_attn_decode(b, b, b, torch.zeros(2, dtype=torch.int32), window=4)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_packs_the_structures(ress, layer):
+    """The packed shapes have the sizes and, by their order, the offsets that C gives them."""
+    from paper_2609_35593_amd import layer as b
+
+    n = layer.ress_norm_shape.from_buffer_copy(b._NORM(1, 2, 0, 1, 5, 6, 0.5))
+    assert (n.rows, n.width, n.x_dtype, n.y_dtype, n.x_stride, n.y_stride, n.eps) == (1, 2, 0, 1, 5, 6, 0.5)
+    r = layer.ress_rope_shape.from_buffer_copy(b._ROPE(*range(1, 13), 0.25, *range(20, 28)))
+    assert (r.H, r.n_axes, list(r.dims), r.layout, r.dtype, r.base) == (1, 5, [6, 7, 8, 9], 10, 12, 0.25)
+    assert (r.q.head, r.k.token, r.q_out.head, r.k_out.token) == (20, 23, 24, 27)
+    w = layer.ress_window_shape.from_buffer_copy(b._WINDOW(*range(1, 11), *range(20, 28)))
+    assert (w.H, w.q_offset, w.causal, w.q.head, w.o.token) == (1, 6, 10, 20, 27)
+    g = layer.ress_window_grads.from_buffer_copy(b._GRADS(*range(8)))
+    assert (g.d_o.head, g.dv.token) == (0, 7)
+    d = layer.ress_decode_shape.from_buffer_copy(b._DECODE(*range(1, 9), *range(20, 30)))
+    assert (d.B, d.n_sink, d.q_batch, d.v_batch, d.k.head, d.v.token, d.o_batch, d.o_head) == (1, 8, 20, 23, 24, 27, 28, 29)
 
 
 # ------------------------------------------------- the float64 forms themselves
