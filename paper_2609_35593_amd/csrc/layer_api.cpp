@@ -243,7 +243,8 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     void *dst[2] = {q_out, k_out};
     const int heads[2] = {s.H, s.H_kv};
     const size_t size = dtype_size(s.dtype);
-    bool chunks = s.D % 16 == 0;
+    const int per = (int)(16 / size);  // channels of a chunk
+    bool chunks = s.D % per == 0;
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0 || s.N == 0) continue;
         if (!src[i] || !dst[i] || !pos || !aligned(src[i], size) || !aligned(dst[i], size) || !aligned(pos, 4))
@@ -252,16 +253,15 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
         if (!disjoint(heads[i], out[i]->head, s.N, out[i]->token, s.D)) return RESS_E_INVALID_ARG;
         if (src[i] == dst[i] && !same(*in[i], *out[i])) return RESS_E_INVALID_ARG;
         if (dst[i] == pos || (heads[1 - i] && (dst[i] == src[1 - i] || dst[i] == dst[1 - i]))) return RESS_E_INVALID_ARG;
-        chunks = chunks && aligned(src[i], 16) && aligned(dst[i], 16) && strides_ok(*in[i], 8) && strides_ok(*out[i], 8);
+        chunks = chunks && aligned(src[i], 16) && aligned(dst[i], 16) && strides_ok(*in[i], per) && strides_ok(*out[i], per);
     }
     if (s.H + s.H_kv == 0 || s.N == 0) return RESS_OK;
 
     // The pairs: axis, turns a position, channels. Copied channels pair up behind them.
-    // Chunks: 8 neighbouring pairs are two runs of 8 channels.
-    if (s.layout == RESS_ROPE_SECTIONS) chunks = chunks && turned % 16 == 0;
-    if (s.layout == RESS_ROPE_INTERLEAVED) chunks = chunks && turned % 8 == 0;
+    if (s.layout == RESS_ROPE_SECTIONS) chunks = chunks && turned % (2 * per) == 0;
+    if (s.layout == RESS_ROPE_INTERLEAVED) chunks = chunks && turned % per == 0;
     if (s.layout == RESS_ROPE_SPLIT)
-        for (int a = 0; a < s.n_axes; ++a) chunks = chunks && s.dims[a] % 16 == 0;
+        for (int a = 0; a < s.n_axes; ++a) chunks = chunks && s.dims[a] % (2 * per) == 0;
     ress::RopeParams p;
     memset(&p, 0, sizeof p);
     int n = 0, at = 0;
@@ -285,9 +285,14 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     p.interleaved = s.layout == RESS_ROPE_INTERLEAVED;
     for (int i = 0; n < s.D / 2; ++i, ++n) {
         p.turns[n] = -1.0;
-        const bool halves = chunks && !p.interleaved;  // then a whole number of 16 channels is left
-        p.ca[n] = (uint8_t)(turned + (halves ? i / 8 * 16 + i % 8 : 2 * i));
-        p.cb[n] = (uint8_t)(p.ca[n] + (halves ? 8 : 1));
+        p.ca[n] = (uint8_t)(turned + 2 * i);
+        p.cb[n] = (uint8_t)(turned + 2 * i + 1);
+    }
+    for (int c = 0; chunks && c < s.D / per; ++c) p.other[c] = (uint8_t)c;
+    for (int i = 0; chunks && i < turned / 2; ++i) {
+        const int a = p.ca[i] / per, b = p.cb[i] / per;
+        if (p.ca[i] % per == 0) p.pair_of[a] = (uint8_t)i, p.other[a] = (uint8_t)b;
+        if (p.cb[i] % per == 0) p.pair_of[b] = (uint8_t)i, p.other[b] = (uint8_t)a;
     }
     p.H = s.H;
     p.H_all = s.H + s.H_kv;
@@ -295,6 +300,7 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     p.n_axes = s.n_axes;
     p.n_pairs = s.D / 2;
     p.D = s.D;
+    p.turned = turned;
     p.f32 = s.dtype == RESS_DTYPE_F32;
     p.inverse = s.inverse != 0;
     p.chunks = chunks;

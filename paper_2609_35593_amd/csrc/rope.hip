@@ -1,10 +1,12 @@
 // Rotary positions with several axes.
 //
 // Memory bound: every element of Q and K is read and written once. A thread owns one
-// token's group of channel pairs and walks over the heads, so that the angles (float64,
-// reduced to a turn's fraction before the sine) are formed once per token and pair and
-// stay in registers. Where pairs come in whole 16-byte chunks (chunk ca against chunk cb,
-// or pairs inside a chunk), a group is two chunks of 8 channels; otherwise it is a pair.
+// 16-byte chunk of a token's channels and walks over the heads, so that the angles (float64,
+// reduced to a turn's fraction before the sine) are formed once per token and stay in
+// registers. Neighbouring threads own neighbouring chunks, so that loads and stores cover
+// whole rows; the chunk that a chunk's pairs meet is read a second time, from the L1 (with a
+// pair of chunks a thread, rows went to memory as two halves each: 32 + 32 views' heads 173
+// us). Where pairs do not come in whole chunks, a thread owns a pair.
 #include "layer_internal.h"
 
 namespace ress {
@@ -16,8 +18,9 @@ constexpr int kBatch = 4;  // heads of a thread in flight
 __device__ __forceinline__ float from_bf16(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
 
 template <typename T>
-struct alignas(16) Chunk {  // 8 channels
-    T e[8];
+struct alignas(16) Chunk {
+    static constexpr int V = 16 / sizeof(T);
+    T e[V];
 };
 
 __device__ __forceinline__ float get(float x) { return x; }
@@ -36,7 +39,7 @@ __device__ __forceinline__ void angle(const RopeParams &p, const int32_t *pos, i
 
 // The turned pair, the same roundings in every form of the kernel.
 __device__ __forceinline__ float turn_a(float a, float b, float c, float s) { return fmaf(a, c, -(b * s)); }
-__device__ __forceinline__ float turn_b(float a, float b, float c, float s) { return fmaf(a, s, b * c); }
+__device__ __forceinline__ float turn_b(float a, float b, float c, float s) { return fmaf(b, c, a * s); }
 
 // Head h of q and k together, its input and output rows of token t.
 template <typename T>
@@ -51,60 +54,56 @@ __device__ __forceinline__ void rows_of(const RopeParams &p, int h, int64_t t, c
     }
 }
 
-// A thread: token i / units, chunks ca and cb of unit i % units; heads h0 .. h0 + heads - 1.
+// A thread: token i / lanes, chunk i % lanes (a token's lanes lie in one wave: its loads are
+// ahead of its stores, also where an output is its input); heads blockIdx.y * heads ...
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads) rope_chunk_kernel(const RopeParams p, int units, int heads)
+__global__ void __launch_bounds__(kThreads) rope_chunk_kernel(const RopeParams p, int lanes_log2, int heads)
 {
+    constexpr int V = Chunk<T>::V;
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t t = i / units;
-    const int u = (int)(i - t * units);
-    if (t >= p.N) return;
-    const int32_t *pos = p.pos + t * p.n_axes;
-    const int ca = p.ca[8 * u], cb = INTERLEAVED ? p.ca[8 * u + 4] : p.cb[8 * u];
-    const bool copy_a = p.turns[8 * u] < 0.0, copy_b = p.turns[8 * u + 4] < 0.0;
-    float c[8], s[8];
+    const int64_t t = i >> lanes_log2;
+    const int c = (int)i & ((1 << lanes_log2) - 1);
+    if (t >= p.N || c * V >= p.D) return;
+    const bool copy = c * V >= p.turned;
+    const int pair = p.pair_of[c], other = p.other[c];  // first pair; the chunk that its pairs meet
+    const bool second = other < c;                      // (halves: this chunk is the pairs' b)
+    float cs[V], sn[V];
+    if (!copy) {
+        const int32_t *pos = p.pos + t * p.n_axes;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        c[e] = 1.f, s[e] = 0.f;
-        if (p.turns[8 * u + e] >= 0.0) angle(p, pos, 8 * u + e, c[e], s[e]);
+        for (int e = 0; e < (INTERLEAVED ? V / 2 : V); ++e) angle(p, pos, pair + e, cs[e], sn[e]);
     }
     const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, p.H_all);
-    // (kBatch heads at a time, all loads ahead of the stores: an output may be its input.)
     for (int hb = h0; hb < h1; hb += kBatch) {
-        Chunk<T> a[kBatch], b[kBatch];
+        Chunk<T> x[kBatch], y[kBatch];
         T *out[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const T *in;
             rows_of(p, min(hb + j, h1 - 1), t, in, out[j]);
-            a[j] = *reinterpret_cast<const Chunk<T> *>(in + ca);
-            b[j] = *reinterpret_cast<const Chunk<T> *>(in + cb);
+            x[j] = *reinterpret_cast<const Chunk<T> *>(in + c * V);
+            if constexpr (!INTERLEAVED) y[j] = *reinterpret_cast<const Chunk<T> *>(in + other * V);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (hb + j >= h1) break;
-            Chunk<T> ya, yb;
-            if constexpr (INTERLEAVED) {
+            if (!copy) {  // (copied channels keep their bits, infinities and NaN too)
+                if constexpr (INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a0 = get(a[j].e[2 * e]), a1 = get(a[j].e[2 * e + 1]);
-                    const float b0 = get(b[j].e[2 * e]), b1 = get(b[j].e[2 * e + 1]);
-                    put(ya.e[2 * e], turn_a(a0, a1, c[e], s[e]));
-                    put(ya.e[2 * e + 1], turn_b(a0, a1, c[e], s[e]));
-                    put(yb.e[2 * e], turn_a(b0, b1, c[e + 4], s[e + 4]));
-                    put(yb.e[2 * e + 1], turn_b(b0, b1, c[e + 4], s[e + 4]));
-                }
-            } else {
+                    for (int e = 0; e < V / 2; ++e) {
+                        const float a = get(x[j].e[2 * e]), b = get(x[j].e[2 * e + 1]);
+                        put(x[j].e[2 * e], turn_a(a, b, cs[e], sn[e]));
+                        put(x[j].e[2 * e + 1], turn_b(a, b, cs[e], sn[e]));
+                    }
+                } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = get(a[j].e[e]), y = get(b[j].e[e]);
-                    put(ya.e[e], turn_a(x, y, c[e], s[e]));
-                    put(yb.e[e], turn_b(x, y, c[e], s[e]));
+                    for (int e = 0; e < V; ++e) {
+                        const float a = get(x[j].e[e]), b = get(y[j].e[e]);
+                        put(x[j].e[e], second ? turn_b(b, a, cs[e], sn[e]) : turn_a(a, b, cs[e], sn[e]));
+                    }
                 }
             }
-            // (Copied channels keep their bits, infinities and NaN too.)
-            *reinterpret_cast<Chunk<T> *>(out[j] + ca) = copy_a ? a[j] : ya;
-            *reinterpret_cast<Chunk<T> *>(out[j] + cb) = copy_b ? b[j] : yb;
+            *reinterpret_cast<Chunk<T> *>(out[j] + c * V) = x[j];
         }
     }
 }
@@ -146,19 +145,21 @@ __global__ void __launch_bounds__(kThreads) rope_pair_kernel(const RopeParams p,
 template <typename T>
 hipError_t go(const RopeParams &p, hipStream_t s)
 {
-    const int units = p.chunks ? p.n_pairs / 8 : p.n_pairs;
-    const int64_t threads = (int64_t)p.N * units;
+    int lanes_log2 = 0;
+    while (Chunk<T>::V << lanes_log2 < p.D) ++lanes_log2;
+    const int64_t threads = p.chunks ? (int64_t)p.N << lanes_log2 : (int64_t)p.N * p.n_pairs;
     const int64_t blocks = (threads + kThreads - 1) / kThreads;
-    // Heads per thread: all that leave 4,096 workgroups, at least 4 to share the angles.
+    // Heads per thread: all that leave 2,048 workgroups, at least one batch.
     int heads = p.H_all;
-    while (heads > 4 && blocks * ((p.H_all + heads - 1) / heads) < 4096) heads = (heads + 1) / 2;
+    while (heads > kBatch && blocks * ((p.H_all + heads - 1) / heads) < 2048) heads = (heads + 1) / 2;
+    heads = (heads + kBatch - 1) / kBatch * kBatch;
     const dim3 grid((unsigned)blocks, (unsigned)((p.H_all + heads - 1) / heads));
     if (!p.chunks)
         hipLaunchKernelGGL(rope_pair_kernel<T>, grid, dim3(kThreads), 0, s, p, heads);
     else if (p.interleaved)
-        hipLaunchKernelGGL((rope_chunk_kernel<T, true>), grid, dim3(kThreads), 0, s, p, units, heads);
+        hipLaunchKernelGGL((rope_chunk_kernel<T, true>), grid, dim3(kThreads), 0, s, p, lanes_log2, heads);
     else
-        hipLaunchKernelGGL((rope_chunk_kernel<T, false>), grid, dim3(kThreads), 0, s, p, units, heads);
+        hipLaunchKernelGGL((rope_chunk_kernel<T, false>), grid, dim3(kThreads), 0, s, p, lanes_log2, heads);
     return hipGetLastError();
 }
 
