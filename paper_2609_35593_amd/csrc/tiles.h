@@ -46,33 +46,53 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// This lane's share of a tile's load by WAVES waves: rows r0 + 8 WAVES u, physical chunk
-// lane & 7 (the swizzle depends on row bits 1-3 only, so one source chunk serves all u).
+// Loads of one tensor's tiles by WAVES waves: this lane's share is rows r0 + 8 WAVES u, physical
+// chunk lane & 7 (the swizzle depends on row bits 1-3 only, so one source chunk serves all u).
+// 64-bit scalar arithmetic up to a tile's first row, 32 bits inside it (63 rows of at most
+// 2^22 elements); a whole tile takes no vector arithmetic at all.
 template <int WAVES>
 struct Loader {
-    int wave, r0;
-    unsigned int coff;
-    __device__ __forceinline__ Loader(int wave_, int lane) : wave(wave_), r0(wave_ * 8 + (lane >> 3))
+    const uint16_t *base;
+    int64_t stride;  // elements between rows
+    int wave, lane;
+    unsigned int whole;  // byte offset in a whole tile
+    __device__ __forceinline__ Loader(const uint16_t *base_, int64_t stride_, int wave_, int lane_)
+        : base(base_), stride(stride_), wave(wave_), lane(lane_)
     {
-        coff = (unsigned int)(((lane & 7) ^ swz(r0)) << 4);
+        const int r0 = wave * 8 + (lane >> 3);
+        whole = (unsigned int)r0 * (unsigned int)(2 * stride) + source(r0, lane);
     }
-    // Rows row0 .. row0 + 63 of a tensor of `stride` elements a row into `dst`; rows
-    // outside [lo, hi) (hi > lo) repeat the nearest one inside and are not read. 64-bit
-    // arithmetic up to the tile's first row, 32 bits inside the tile (63 rows of at
-    // most 2^22 elements).
-    __device__ __forceinline__ void operator()(const uint16_t *base, int64_t stride, int row0, int lo, int hi,
-                                               unsigned char *dst) const
+    static __device__ __forceinline__ unsigned int source(int r0, int l) { return (unsigned int)(((l & 7) ^ swz(r0)) << 4); }
+    // Rows row0 .. row0 + 63 into `dst`; rows outside [lo, hi) (hi > lo) repeat the nearest
+    // one inside and are not read.
+    __device__ __forceinline__ void operator()(int row0, int lo, int hi, unsigned char *dst) const
     {
-        const int first = min(max(row0, lo), hi - 1);
-        const int last = max(min(row0 + kTile, hi) - 1, first);
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t *>(base + (int64_t)first * stride), 0,
-            (int)((unsigned int)(last - first) * (unsigned int)(2 * stride) + 128u), 0x00020000);
+        const unsigned int step = (unsigned int)(2 * stride);  // bytes
+        if (row0 >= lo && row0 + kTile <= hi) {
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<uint16_t *>(base + (int64_t)row0 * stride), 0, (int)((kTile - 1) * step + 128u), 0x00020000);
 #pragma unroll
-        for (int u = 0; u < 8 / WAVES; ++u) {
-            const int row = min(max(row0 + r0 + 8 * WAVES * u, first), last) - first;
-            const unsigned int off = (unsigned int)row * (unsigned int)(2 * stride) + coff;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16, off, 0, 0, 0);
+            for (int u = 0; u < 8 / WAVES; ++u)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16, whole,
+                                                         (int)(8 * WAVES * u * step), 0, 0);
+        } else {
+            // (Formed from the lane each time: kept over the caller's loop, these values would be
+            // spilled, and their reload would wait for the loads in flight.)
+            int l = lane;
+            asm volatile("" : "+v"(l));
+            const int r0 = wave * 8 + (l >> 3);
+            const unsigned int coff = source(r0, l);
+            const int first = min(max(row0, lo), hi - 1);
+            const int last = max(min(row0 + kTile, hi) - 1, first);
+            const __amdgpu_buffer_rsrc_t rs =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + (int64_t)first * stride), 0,
+                                                  (int)((unsigned int)(last - first) * step + 128u), 0x00020000);
+#pragma unroll
+            for (int u = 0; u < 8 / WAVES; ++u) {
+                const int row = min(max(row0 + r0 + 8 * WAVES * u, first), last) - first;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16,
+                                                         (unsigned int)row * step + coff, 0, 0, 0);
+            }
         }
     }
 };

@@ -27,10 +27,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <bool LSE>
-__global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
+__global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowParams p)
 {
-    __shared__ __attribute__((aligned(1024))) unsigned char k_s[2][kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_s[2][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_0[kTileBytes], k_1[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_0[kTileBytes], v_1[kTileBytes];
 
     // Contiguous runs of (head, query block) per XCD, whose L2 then holds few heads'
     // windows; last blocks first (a causal row sees the more the later it is).
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
     // The workgroup's tiles: [0, ns) and [w0, w1).
     const int t_first = i * 128, t_last = min(t_first + 128, p.n_q) - 1;
     const Seen s_first = seen_by(p, p.q_offset + t_first), s_last = seen_by(p, p.q_offset + t_last);
-    int ns = (s_last.sk + kTile - 1) / kTile;
+    const int ns = (s_last.sk + kTile - 1) / kTile;
     int w0 = s_first.lo / kTile, w1 = (s_last.hi + kTile - 1) / kTile;
     if (s_first.lo >= s_last.hi) w0 = w1 = ns;
     if (w0 < ns) w0 = ns;
@@ -52,11 +52,15 @@ __global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
     const int tiles_n = ns + w1 - w0;
     auto tile_key = [&](int c) __attribute__((always_inline)) { return (c < ns ? c : c - ns + w0) * kTile; };
 
-    // What the wave's rows and this lane's row see (rows past the last repeat it).
+    // What the wave's rows and this lane's row see (rows past the last repeat it), the lane's
+    // against its first key of a tile.
     const int ta = min(t_first + wave * 32, t_last), tb = min(t_first + wave * 32 + 31, t_last);
     const Seen sa = seen_by(p, p.q_offset + ta), sb = seen_by(p, p.q_offset + tb);
     const int t = t_first + wave * 32 + ql, tq = min(t, t_last);
-    const Seen sl = seen_by(p, p.q_offset + tq);
+    Seen sl = seen_by(p, p.q_offset + tq);
+    sl.lo -= 4 * hh;
+    sl.hi -= 4 * hh;
+    sl.sk -= 4 * hh;
 
     bf16x8 qf[4];
     {
@@ -64,16 +68,16 @@ __global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + kk * 16);
     }
-    const uint16_t *kh = p.k + (h / p.group) * p.ks.head, *vh = p.v + (h / p.group) * p.vs.head;
-    const Loader<4> load(wave, lane);
+    const Loader<4> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
+    const Loader<4> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
     // Keys outside every row's sight are not read: [0, sk) and [lo, hi) of the workgroup.
-    auto fetch = [&](int c, int slot) __attribute__((always_inline)) {
+    auto fetch = [&](int c, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
         const int key0 = tile_key(c);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
-        load(kh, p.ks.token, key0, lo, hi, k_s[slot]);
-        load(vh, p.vs.token, key0, lo, hi, v_s[slot]);
+        load_k(key0, lo, hi, kd);
+        load_v(key0, lo, hi, vd);
     };
 
     const float c = p.scale_log2;
@@ -84,9 +88,9 @@ __global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
     for (int dh = 0; dh < 2; ++dh)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[dh][v] = 0.f;
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
-    auto scores = [&](const unsigned char *kt, int u, int key0, bool part, f32x16 &s) __attribute__((always_inline)) {
+    // Scores of rows 32 u .. of a tile; `part`: of the keys that the lane's row sees, else -inf.
+    auto scores = [&](bool part, const unsigned char *kt, int u, int key0, f32x16 &s) __attribute__((always_inline)) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
@@ -95,91 +99,94 @@ __global__ void __launch_bounds__(256, 4) window_kernel(const WindowParams p)
             asm volatile("" ::: "memory");  // (a real branch: whole tiles skip the comparisons)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int key = key0 + u * 32 + (v >> 2) * 8 + (v & 3) + 4 * hh;
+                const int key = __builtin_amdgcn_readfirstlane(key0 + u * 32 + (v >> 2) * 8 + (v & 3));
                 const bool in = (key >= sl.lo && key < sl.hi) || key < sl.sk;
                 s[v] = in ? s[v] : -INFINITY;
             }
         }
     };
-    // The lane's half of the row's largest logit in the tile, with the other half's.
-    auto top = [&](const unsigned char *kt, int key0, bool part) __attribute__((always_inline)) {
+    // The row's largest logit in the tile.
+    auto top = [&](bool part, const unsigned char *kt, int key0) __attribute__((always_inline)) {
         float m = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x16 s;
-            scores(kt, u, key0, part, s);
+            scores(part, kt, u, key0, s);
 #pragma unroll
             for (int v = 0; v < 16; ++v) m = fmaxf(m, s[v]);
         }
         return fmaxf(m, __shfl_xor(m, 32)) * c;
     };
-    auto probs = [&](const unsigned char *kt, int key0, bool part, bf16x8 (&pb)[2][2]) __attribute__((always_inline)) {
+    // Probabilities against the row's reference, and the lane's part of their sum.
+    auto probs = [&](bool part, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2]) __attribute__((always_inline)) {
         float l0 = 0.f, l1 = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x16 s;
-            scores(kt, u, key0, part, s);
+            scores(part, kt, u, key0, s);
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -ref));
             pack(s, pb[u]);
             if constexpr (LSE) {
 #pragma unroll
                 for (int v = 0; v < 16; v += 2) l0 += s[v], l1 += s[v + 1];
+                __builtin_amdgcn_sched_barrier(0);  // (else both halves' float32 values are held: spills)
             } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int j = 0; j < 8; j += 4) {
-                        l0 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[u][e][j], pb[u][e][j + 1]}, ones, l0, false);
-                        l1 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[u][e][j + 2], pb[u][e][j + 3]}, ones, l1, false);
-                    }
+                l0 = add_up(pb[u], l0);
             }
         }
         return l0 + l1;
     };
-
-    if (tiles_n > 0) {
-        fetch(0, 0);
-        wait_vm_all();
-        __syncthreads();
-    }
-    for (int ch = 0; ch < tiles_n; ++ch) {
-        const int slot = ch & 1, key0 = tile_key(ch);
-        if (ch + 1 < tiles_n) fetch(ch + 1, slot ^ 1);
-        const bool none = key0 >= sb.sk && (key0 + kTile <= sa.lo || key0 >= sb.hi);
-        if (!none) {
-            const bool part = !(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi));
-            const unsigned char *kt = k_s[slot], *vt = v_s[slot];
-            if (!__all(has)) {
-                const float m = top(kt, key0, part);
-                if (!has && m > -INFINITY) {
-                    ref = m;
-                    has = true;
-                }
-            }
-            bf16x8 pb[2][2];
-            float l = probs(kt, key0, part, pb);
-            if (__any(!(l <= kSumLimit))) {
-                const float m = top(kt, key0, part), to = fmaxf(ref, m);
-                const float a = __builtin_amdgcn_exp2f(ref - to);
+    auto tile = [&](bool part, const unsigned char *kt, const unsigned char *vt, int key0) __attribute__((always_inline)) {
+        bf16x8 pb[2][2];
+        float l;
+#pragma nounroll
+        for (bool again = false;; again = true) {
+            l = probs(part, kt, key0, pb);
+            // (Lanes l and l^32 share the row and decide together.)
+            const bool far = !(l <= kSumLimit);
+            if (again || !__any(far || !has)) break;
+            const bool row_far = ((int)far | __shfl_xor((int)far, 32)) != 0;
+            const float m = top(part, kt, key0);
+            if (has ? row_far : m > -INFINITY) {
+                const float to = has ? fmaxf(ref, m) : m;
+                const float a = has ? __builtin_amdgcn_exp2f(ref - to) : 0.f;
                 sum *= a;
 #pragma unroll
                 for (int dh = 0; dh < 2; ++dh)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) acc[dh][v] *= a;
                 ref = to;
-                l = probs(kt, key0, part, pb);
+                has = true;
             }
-            sum += l;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int dh = 0; dh < 2; ++dh) acc[dh] = mfma(rd.cols(vt, u, e, dh), pb[u][e], acc[dh]);
         }
+        sum += l;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dh = 0; dh < 2; ++dh) acc[dh] = mfma(rd.cols(vt, u, e, dh), pb[u][e], acc[dh]);
+    };
+    int ch = 0;
+    // Tile ch from (kt, vt), tile ch + 1 on its way into the other slots. (Slots by name: with
+    // addresses formed at run time every read takes an addition.)
+    auto step = [&](const unsigned char *kt, const unsigned char *vt, unsigned char *kd, unsigned char *vd)
+                    __attribute__((always_inline)) -> bool {
+        const int key0 = tile_key(ch);
+        if (ch + 1 < tiles_n) fetch(ch + 1, kd, vd);
+        if (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi))
+            tile(!(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi)), kt, vt, key0);
         wait_vm_all();
         __syncthreads();
+        return ++ch < tiles_n;
+    };
+    if (tiles_n > 0) {
+        fetch(0, k_0, v_0);
+        wait_vm_all();
+        __syncthreads();
+        while (step(k_0, v_0, k_1, v_1) && step(k_1, v_1, k_0, v_0)) {
+        }
     }
 
     sum += __shfl_xor(sum, 32);

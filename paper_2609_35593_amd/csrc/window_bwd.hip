@@ -85,15 +85,15 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
         }
     }
     const float lse2 = b.lse2[(int64_t)h * p.n_q + tq], nd = b.ndelta[(int64_t)h * p.n_q + tq];
-    const uint16_t *kh = p.k + (h / p.group) * p.ks.head, *vh = p.v + (h / p.group) * p.vs.head;
-    const Loader<4> load(wave, lane);
+    const Loader<4> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
+    const Loader<4> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
     auto fetch = [&](int c, int slot) __attribute__((always_inline)) {
         const int key0 = tile_key(c);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
-        load(kh, p.ks.token, key0, lo, hi, k_s[slot]);
-        load(vh, p.vs.token, key0, lo, hi, v_s[slot]);
+        load_k(key0, lo, hi, k_s[slot]);
+        load_v(key0, lo, hi, v_s[slot]);
     };
     const float c = p.scale_log2;
     f32x16 acc[2], mean[2];  // sum dS k, sum P k
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
             vf[kk] = *reinterpret_cast<const bf16x8 *>(v + kk * 16);
         }
     }
-    const Loader<4> load(wave, lane);
+    Loader<4> load_q(p.q, p.qs.token, wave, lane), load_d(b.d_o, b.dos.token, wave, lane);
     const Reader rd(lane);
     const int first = q_lo / kTile, per_head = q_hi > q_lo ? (q_hi + kTile - 1) / kTile - first : 0;
     const int tiles_n = per_head * p.group;
@@ -209,8 +209,10 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
     int fh = hk * p.group, ft = first;
     auto fetch = [&](int slot) __attribute__((always_inline)) {
         const int t0 = ft * kTile;
-        load(p.q + fh * p.qs.head, p.qs.token, t0, 0, p.n_q, q_s[slot]);
-        load(b.d_o + fh * b.dos.head, b.dos.token, t0, 0, p.n_q, d_s[slot]);
+        load_q.base = p.q + fh * p.qs.head;
+        load_d.base = b.d_o + fh * b.dos.head;
+        load_q(t0, 0, p.n_q, q_s[slot]);
+        load_d(t0, 0, p.n_q, d_s[slot]);
         if (wave < 2) {
             const float *src = (wave == 0 ? b.lse2 : b.ndelta) + (int64_t)fh * p.n_q + t0;
             const int last = min(kTile, p.n_q - t0) - 1;
