@@ -145,15 +145,20 @@ typedef struct {
     ress_strides q, k, v, o; /* multiples of 8; a token stride of at most 2^22 */
 } ress_window_shape;
 
+/* Bytes of device workspace ress_window_attn needs (0 but for few queries over long
+ * windows, whose keys are split over workgroups; strides do not matter). */
+int ress_window_attn_workspace_size(const ress_window_shape *shape, size_t *bytes);
+
 /* o = softmax over the visible keys of (scale q . k) v, bf16 [H][n_q][64] by the
  * shape's strides, bf16 products, float32 softmax and accumulation (probabilities
  * rounded to bf16 for the product with v, o once). A query that sees no key gets a
  * zero output.
  *   lse  device float32 [H][n_q] out, or NULL: the natural logarithm of the sum of
  *        exp(scale q . k) over the visible keys, -inf where there are none
+ *   workspace  256-byte aligned; may be NULL where none is needed
  * Pointers 16-byte aligned; scale > 0 and finite. */
 int ress_window_attn(const ress_window_shape *shape, const void *q, const void *k, const void *v, float scale, void *o,
-                     float *lse, hipStream_t stream);
+                     float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 typedef struct {
     ress_strides d_o, dq, dk, dv;

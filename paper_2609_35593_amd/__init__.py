@@ -375,4 +375,4 @@ def bf16_from_bits(bits: np.ndarray, device) -> torch.Tensor:
 # The further steps of a layer (include/ress_layer.h).
 from .layer import (ress_layer_norm, ress_layer_norm_bwd, ress_layer_norm_bwd_workspace_size, ress_rope,  # noqa: E402
                     ress_window_attn, ress_window_attn_bwd, ress_window_attn_bwd_workspace_size,
-                    ress_window_attn_decode, ress_window_attn_decode_workspace_size)
+                    ress_window_attn_decode, ress_window_attn_decode_workspace_size, ress_window_attn_workspace_size)

@@ -115,6 +115,13 @@ ress::WindowParams window_params(const ress_window_shape *s, float scale)
 
 bool scale_ok(float scale) { return scale > 0.f && isfinite(scale); }
 
+size_t window_workspace(const ress_window_shape *s)
+{
+    if (s->H == 0) return 0;
+    const int splits = ress::window_plan(s).splits;
+    return splits == 1 ? 0 : align256((size_t)splits * s->H * s->n_q * 66 * sizeof(float));
+}
+
 size_t rows_bytes(const ress_window_shape *s) { return align256((size_t)s->H * s->n_q * sizeof(float)); }
 
 int check_decode(const ress_decode_shape *s)
@@ -316,8 +323,17 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     return ress::launch_rope(p, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }
 
+int ress_window_attn_workspace_size(const ress_window_shape *shape, size_t *bytes)
+{
+    int st = check_window(shape, false);
+    if (st != RESS_OK) return st;
+    if (!bytes) return RESS_E_INVALID_ARG;
+    *bytes = window_workspace(shape);
+    return RESS_OK;
+}
+
 int ress_window_attn(const ress_window_shape *shape, const void *q, const void *k, const void *v, float scale, void *o,
-                     float *lse, hipStream_t stream)
+                     float *lse, void *workspace, size_t ws_bytes, hipStream_t stream)
 {
     int st = check_window(shape, true);
     if (st != RESS_OK) return st;
@@ -329,13 +345,22 @@ int ress_window_attn(const ress_window_shape *shape, const void *q, const void *
     if (o == q || o == k || o == v || (lse && ((void *)lse == o || lse == q || lse == k || lse == v)))
         return RESS_E_INVALID_ARG;
     if (!disjoint(shape->H, shape->o.head, shape->n_q, shape->o.token, kHead)) return RESS_E_INVALID_ARG;
+    const size_t need = window_workspace(shape);
+    if (need && (!workspace || ws_bytes < need || !aligned(workspace, 256))) return RESS_E_WORKSPACE;
+    const ress::WindowPlan plan = ress::window_plan(shape);
     ress::WindowParams p = window_params(shape, scale);
     p.q = static_cast<const uint16_t *>(q);
     p.k = static_cast<const uint16_t *>(k);
     p.v = static_cast<const uint16_t *>(v);
     p.o = static_cast<uint16_t *>(o);
     p.lse = lse;
-    return ress::launch_window(p, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
+    p.splits = plan.splits;
+    p.n_qb = (p.n_q * plan.groups + 127) / 128;
+    if (plan.splits > 1) {
+        p.part = static_cast<float *>(workspace);
+        p.part_row = reinterpret_cast<float2 *>(p.part + (size_t)plan.splits * p.H * p.n_q * 64);
+    }
+    return ress::launch_window(p, plan.groups, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }
 
 int ress_window_attn_bwd_workspace_size(const ress_window_shape *shape, size_t *bytes)

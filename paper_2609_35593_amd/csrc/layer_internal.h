@@ -60,13 +60,23 @@ struct WindowParams {
     int n_q, n_k, q_offset;
     int frame, window, n_sink;
     bool causal;
-    int n_qb, n_kb;  // blocks of 128 queries, of 128 keys
+    int n_qb, n_kb;  // blocks of 128 / groups queries, of 128 keys
+    int splits;      // workgroups that share a block's keys (forward)
     float scale, scale_log2;
     ress_strides qs, ks, vs, os;
     const uint16_t *q, *k, *v;
     uint16_t *o;
     float *lse;
+    float *part;        // splits > 1: [splits][H][n_q][64], unnormalised outputs,
+    float2 *part_row;   // and [splits][H][n_q], references and sums
 };
+
+// How the forward pass spreads over the chip: key groups in a workgroup (1, 2, 4),
+// workgroups per block of 128 / groups queries. A function of the shape alone.
+struct WindowPlan {
+    int groups, splits;
+};
+WindowPlan window_plan(const ress_window_shape *s);
 
 struct WindowBwdParams {
     WindowParams w;  // o: the forward's output, read; lse: read
@@ -95,7 +105,7 @@ int decode_splits(const ress_decode_shape *s);
 hipError_t launch_norm(const NormParams &p, hipStream_t s);
 hipError_t launch_norm_bwd(const NormBwdParams &p, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, hipStream_t s);
-hipError_t launch_window(const WindowParams &p, hipStream_t s);
+hipError_t launch_window(const WindowParams &p, int groups, hipStream_t s);
 hipError_t launch_window_bwd(const WindowBwdParams &p, hipStream_t s);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s);
 

@@ -47,7 +47,8 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c)
 }
 
 // Loads of one tensor's tiles by WAVES waves: this lane's share is rows r0 + 8 WAVES u, physical
-// chunk lane & 7 (the swizzle depends on row bits 1-3 only, so one source chunk serves all u).
+// chunk lane & 7. (The swizzle depends on row bits 1-3 only, so one source chunk serves all u,
+// but for a single wave, where bit 3 alternates with u and the source chunk by 2.)
 // 64-bit scalar arithmetic up to a tile's first row, 32 bits inside it (63 rows of at most
 // 2^22 elements); a whole tile takes no vector arithmetic at all.
 template <int WAVES>
@@ -55,12 +56,13 @@ struct Loader {
     const uint16_t *base;
     int64_t stride;  // elements between rows
     int wave, lane;
-    unsigned int whole;  // byte offset in a whole tile
+    unsigned int whole, whole1;  // byte offsets in a whole tile, for even and odd u
     __device__ __forceinline__ Loader(const uint16_t *base_, int64_t stride_, int wave_, int lane_)
         : base(base_), stride(stride_), wave(wave_), lane(lane_)
     {
         const int r0 = wave * 8 + (lane >> 3);
         whole = (unsigned int)r0 * (unsigned int)(2 * stride) + source(r0, lane);
+        whole1 = (unsigned int)r0 * (unsigned int)(2 * stride) + (source(r0, lane) ^ (WAVES == 1 ? 32u : 0u));
     }
     static __device__ __forceinline__ unsigned int source(int r0, int l) { return (unsigned int)(((l & 7) ^ swz(r0)) << 4); }
     // Rows row0 .. row0 + 63 into `dst`; rows outside [lo, hi) (hi > lo) repeat the nearest
@@ -73,7 +75,8 @@ struct Loader {
                 const_cast<uint16_t *>(base + (int64_t)row0 * stride), 0, (int)((kTile - 1) * step + 128u), 0x00020000);
 #pragma unroll
             for (int u = 0; u < 8 / WAVES; ++u)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16, whole,
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16,
+                                                         WAVES == 1 && u % 2 ? whole1 : whole,
                                                          (int)(8 * WAVES * u * step), 0, 0);
         } else {
             // (Formed from the lane each time: kept over the caller's loop, these values would be
@@ -91,7 +94,8 @@ struct Loader {
             for (int u = 0; u < 8 / WAVES; ++u) {
                 const int row = min(max(row0 + r0 + 8 * WAVES * u, first), last) - first;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16,
-                                                         (unsigned int)row * step + coff, 0, 0, 0);
+                                                         (unsigned int)row * step + (WAVES == 1 && u % 2 ? coff ^ 32u : coff),
+                                                         0, 0, 0);
             }
         }
     }

@@ -9,6 +9,12 @@
 // in part, by two comparisons a score against its lane's range, and passes over those
 // that none sees.
 //
+// Small calls: a wave's tiles come one after the other, and a chip of 1,024 SIMDs wants more
+// waves than there are rows. With G > 1 a workgroup's waves split into G groups over the same
+// 128 / G queries, group g with LDS slots of its own taking tiles g, g + G, ...; and a block's
+// tiles are cut over `splits` workgroups, whose partial results join_kernel adds up. Both
+// joins take the parts in order.
+//
 // Softmax: base 2, against a reference per row that is the row's largest logit in the
 // first tile where it sees a key, and moves (O and the sum rescaled) only when a tile's
 // sum exceeds 2^50; so a tile costs no maximum, float32 keeps every digit of the sum, and a
@@ -26,11 +32,19 @@ constexpr float kSumLimit = 0x1p50f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <bool LSE>
-__global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowParams p)
+// exp2(a - top) for a part that holds mass, 0 for one that holds none.
+__device__ __forceinline__ float share(float ref, float sum, float top)
 {
-    __shared__ __attribute__((aligned(1024))) unsigned char k_0[kTileBytes], k_1[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_0[kTileBytes], v_1[kTileBytes];
+    return sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+}
+
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+template <bool LSE, int G>
+__global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const WindowParams p)
+{
+    constexpr int QW = 4 / G, ROWS = 32 * QW;  // waves and queries of a group
+    __shared__ __attribute__((aligned(1024))) unsigned char slots[4][G * kTileBytes];
 
     // Contiguous runs of (head, query block) per XCD, whose L2 then holds few heads'
     // windows; last blocks first (a causal row sees the more the later it is).
@@ -38,19 +52,32 @@ __global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowPa
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || at >= rows) return;
     const int h = at / p.n_qb, i = p.n_qb - 1 - (at - h * p.n_qb);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
+    unsigned char *const k_0 = slots[0] + grp * kTileBytes, *const k_1 = slots[1] + grp * kTileBytes;
+    unsigned char *const v_0 = slots[2] + grp * kTileBytes, *const v_1 = slots[3] + grp * kTileBytes;
 
-    // The workgroup's tiles: [0, ns) and [w0, w1).
-    const int t_first = i * 128, t_last = min(t_first + 128, p.n_q) - 1;
+    // The block's tiles: [0, ns) and [w0, w1); this workgroup's: from `begin`, tiles_n of them.
+    const int t_first = i * ROWS, t_last = min(t_first + ROWS, p.n_q) - 1;
     const Seen s_first = seen_by(p, p.q_offset + t_first), s_last = seen_by(p, p.q_offset + t_last);
     const int ns = (s_last.sk + kTile - 1) / kTile;
     int w0 = s_first.lo / kTile, w1 = (s_last.hi + kTile - 1) / kTile;
     if (s_first.lo >= s_last.hi) w0 = w1 = ns;
     if (w0 < ns) w0 = ns;
     if (w1 < w0) w1 = w0;
-    const int tiles_n = ns + w1 - w0;
-    auto tile_key = [&](int c) __attribute__((always_inline)) { return (c < ns ? c : c - ns + w0) * kTile; };
+    int begin = 0, tiles_n = ns + w1 - w0;
+    if (p.splits > 1) {
+        const int all = tiles_n, split = blockIdx.y;
+        begin = (int)((int64_t)all * split / p.splits);
+        tiles_n = (int)((int64_t)all * (split + 1) / p.splits) - begin;
+    }
+    // Key of the group's turn n.
+    auto tile_key = [&](int n) __attribute__((always_inline)) {
+        const int c = begin + n * G + grp;
+        return (c < ns ? c : c - ns + w0) * kTile;
+    };
+    const int turns = (tiles_n + G - 1) / G;
 
     // What the wave's rows and this lane's row see (rows past the last repeat it), the lane's
     // against its first key of a tile.
@@ -68,12 +95,13 @@ __global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowPa
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + kk * 16);
     }
-    const Loader<4> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
-    const Loader<4> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
+    const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
+    const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
     // Keys outside every row's sight are not read: [0, sk) and [lo, hi) of the workgroup.
-    auto fetch = [&](int c, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
-        const int key0 = tile_key(c);
+    auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
+        if (n * G + grp >= tiles_n) return;
+        const int key0 = tile_key(n);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
         load_k(key0, lo, hi, kd);
@@ -140,25 +168,30 @@ __global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowPa
     auto tile = [&](bool part, const unsigned char *kt, const unsigned char *vt, int key0) __attribute__((always_inline)) {
         bf16x8 pb[2][2];
         float l;
+        // (Rare: a row's first tile, or logits far above those so far. Lanes l and l^32 share the
+        // row and decide together.)
+        bool look = __any(!has), far = false;
 #pragma nounroll
         for (bool again = false;; again = true) {
-            l = probs(part, kt, key0, pb);
-            // (Lanes l and l^32 share the row and decide together.)
-            const bool far = !(l <= kSumLimit);
-            if (again || !__any(far || !has)) break;
-            const bool row_far = ((int)far | __shfl_xor((int)far, 32)) != 0;
-            const float m = top(part, kt, key0);
-            if (has ? row_far : m > -INFINITY) {
-                const float to = has ? fmaxf(ref, m) : m;
-                const float a = has ? __builtin_amdgcn_exp2f(ref - to) : 0.f;
-                sum *= a;
+            if (look) {
+                const float m = top(part, kt, key0);
+                if (has ? far : m > -INFINITY) {
+                    const float to = has ? fmaxf(ref, m) : m;
+                    const float a = has ? __builtin_amdgcn_exp2f(ref - to) : 0.f;
+                    sum *= a;
 #pragma unroll
-                for (int dh = 0; dh < 2; ++dh)
+                    for (int dh = 0; dh < 2; ++dh)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[dh][v] *= a;
-                ref = to;
-                has = true;
+                        for (int v = 0; v < 16; ++v) acc[dh][v] *= a;
+                    ref = to;
+                    has = true;
+                }
             }
+            l = probs(part, kt, key0, pb);
+            far = !(l <= kSumLimit);
+            look = __any(far);
+            if (!look || again) break;
+            far = ((int)far | __shfl_xor((int)far, 32)) != 0;
         }
         sum += l;
 #pragma unroll
@@ -168,20 +201,20 @@ __global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowPa
 #pragma unroll
                 for (int dh = 0; dh < 2; ++dh) acc[dh] = mfma(rd.cols(vt, u, e, dh), pb[u][e], acc[dh]);
     };
-    int ch = 0;
-    // Tile ch from (kt, vt), tile ch + 1 on its way into the other slots. (Slots by name: with
+    int n = 0;
+    // Turn n from (kt, vt), turn n + 1 on its way into the other slots. (Slots by name: with
     // addresses formed at run time every read takes an addition.)
     auto step = [&](const unsigned char *kt, const unsigned char *vt, unsigned char *kd, unsigned char *vd)
                     __attribute__((always_inline)) -> bool {
-        const int key0 = tile_key(ch);
-        if (ch + 1 < tiles_n) fetch(ch + 1, kd, vd);
-        if (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi))
+        const int key0 = tile_key(n);
+        fetch(n + 1, kd, vd);
+        if ((G == 1 || n * G + grp < tiles_n) && (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi)))
             tile(!(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi)), kt, vt, key0);
         wait_vm_all();
         __syncthreads();
-        return ++ch < tiles_n;
+        return ++n < turns;
     };
-    if (tiles_n > 0) {
+    if (turns > 0) {
         fetch(0, k_0, v_0);
         wait_vm_all();
         __syncthreads();
@@ -190,21 +223,128 @@ __global__ void __launch_bounds__(256, LSE ? 3 : 4) window_kernel(const WindowPa
     }
 
     sum += __shfl_xor(sum, 32);
+    if constexpr (G > 1) {
+        // The groups behind the first leave reference, sum and O in the slots (34 floats a lane).
+        constexpr int PER = 34 * 64;
+        static_assert((G - 1) * QW * PER * sizeof(float) <= sizeof slots, "the joined parts fit the slots");
+        float *const area = reinterpret_cast<float *>(slots[0]);
+        if (grp > 0) {
+            float *m = area + ((grp - 1) * QW + wave) * PER + lane;
+            m[0] = ref;
+            m[64] = sum;
+#pragma unroll
+            for (int v = 0; v < 32; ++v) m[(2 + v) * 64] = acc[v >> 4][v & 15];
+        }
+        __syncthreads();
+        if (grp > 0) return;
+        float to = sum == 0.f ? -INFINITY : ref;
+#pragma unroll
+        for (int g = 1; g < G; ++g) {
+            const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+            if (m[64] != 0.f) to = fmaxf(to, m[0]);
+        }
+        const float a0 = share(ref, sum, to);
+        sum *= a0;
+#pragma unroll
+        for (int v = 0; v < 32; ++v) acc[v >> 4][v & 15] *= a0;
+#pragma unroll
+        for (int g = 1; g < G; ++g) {
+            const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+            const float a = share(m[0], m[64], to);
+            sum = fmaf(m[64], a, sum);
+#pragma unroll
+            for (int v = 0; v < 32; ++v) acc[v >> 4][v & 15] = fmaf(m[(2 + v) * 64], a, acc[v >> 4][v & 15]);
+        }
+        ref = to;
+    }
     if (t > t_last) return;
-    store_row(p.o + h * p.os.head + (int64_t)t * p.os.token, acc, sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum), hh);
+    if (p.splits > 1) {
+        const int64_t row = ((int64_t)blockIdx.y * p.H + h) * p.n_q + t;
+#pragma unroll
+        for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4 *>(p.part + row * 64 + dh * 32 + g * 8 + hh * 4) =
+                    f32x4{acc[dh][g * 4], acc[dh][g * 4 + 1], acc[dh][g * 4 + 2], acc[dh][g * 4 + 3]};
+        if (hh == 0) p.part_row[row] = make_float2(ref, sum);
+        return;
+    }
+    store_row(p.o + h * p.os.head + (int64_t)t * p.os.token, acc, inverse(sum), hh);
     if (LSE && hh == 0) p.lse[(int64_t)h * p.n_q + t] = sum == 0.f ? -INFINITY : ref * kLn2 + logf(sum);
+}
+
+// A wave a row (a channel a lane): its at most 32 parts, their weights one a lane.
+__global__ void __launch_bounds__(256) join_kernel(const WindowParams p)
+{
+    const int64_t rows = (int64_t)p.H * p.n_q, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int lane = threadIdx.x & 63;
+    const float2 r = lane < p.splits ? p.part_row[lane * rows + row] : make_float2(0.f, 0.f);
+    float top = r.y == 0.f ? -INFINITY : r.x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float w = share(r.x, r.y, top);
+    float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
+#pragma unroll
+    for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
+#pragma unroll 8
+    for (int s = 0; s < p.splits; ++s) {
+        const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s));
+        o = fmaf(ws, p.part[(s * rows + row) * 64 + lane], o);
+    }
+    const int64_t h = row / p.n_q, t = row - h * p.n_q;
+    p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(o * inverse(sum));
+    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+}
+
+template <int G>
+hipError_t go(const WindowParams &p, hipStream_t s)
+{
+    const dim3 grid(8u * (unsigned)((p.H * p.n_qb + 7) / 8), (unsigned)p.splits), block(256);
+    if (p.lse)
+        hipLaunchKernelGGL((window_kernel<true, G>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((window_kernel<false, G>), grid, block, 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.H * p.n_q + 3) / 4)), block, 0, s, p);
+        return hipGetLastError();
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
-hipError_t launch_window(const WindowParams &p, hipStream_t s)
+WindowPlan window_plan(const ress_window_shape *s)
 {
-    const dim3 grid(8u * (unsigned)((p.H * p.n_qb + 7) / 8)), block(256);
-    if (p.lse)
-        hipLaunchKernelGGL(window_kernel<true>, grid, block, 0, s, p);
-    else
-        hipLaunchKernelGGL(window_kernel<false>, grid, block, 0, s, p);
-    return hipGetLastError();
+    // Tiles a block sees at most.
+    const int64_t window = (int64_t)s->window * s->frame * (s->causal ? 1 : 2) + 128;
+    const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k;
+    const int64_t keys = window + sinks < s->n_k ? window + sinks : s->n_k;
+    const int64_t tiles = (keys + 63) / 64;
+    auto blocks = [&](int g) { return (int64_t)s->H * (((int64_t)s->n_q * g + 127) / 128); };
+    WindowPlan plan = {1, 1};
+    // 512 workgroups of 128 queries are two a CU: from there on key groups only cost (us with 1 /
+    // 2 / 4: 1,264 blocks of 18 tiles 80 / 97 / 246; 352 of 87 197 / 155 / 243; 64 of 9 13.4 / 9.4
+    // / 9.2; 18 of 3 13 / 7.3 / 8.5).
+    if (tiles < 2 || blocks(1) >= 512) return plan;
+    // Four groups (one workgroup a CU, by its LDS) once that still is one filling, and with tiles
+    // enough for each: 125 blocks of 64 tiles 61 / 36 / 26. Below, workgroups to fill the CUs, each
+    // with two tiles a group at least: 125 blocks 26 -> 20 with 2; 16 blocks of 80 tiles 33 -> 15
+    // with 10; one of 625 203 -> 22 with 32.
+    const int64_t n = blocks(4);
+    plan.groups = n <= 256 && tiles >= 8 ? 4 : 2;
+    if (plan.groups == 4 && n > 0) {
+        int64_t want = 256 / n;
+        if (want > tiles / 8) want = tiles / 8;
+        plan.splits = (int)(want < 1 ? 1 : want > 32 ? 32 : want);
+    }
+    return plan;
+}
+
+hipError_t launch_window(const WindowParams &p, int groups, hipStream_t s)
+{
+    return groups == 1 ? go<1>(p, s) : groups == 2 ? go<2>(p, s) : go<4>(p, s);
 }
 
 }  // namespace ress

@@ -37,7 +37,8 @@ def _declare():
             ("ress_layer_norm_bwd_workspace_size", [vp, vp]),
             ("ress_layer_norm_bwd", [vp] * 10 + [sz, vp]),
             ("ress_rope", [vp] * 7),
-            ("ress_window_attn", [vp] * 4 + [f, vp, vp, vp]),
+            ("ress_window_attn_workspace_size", [vp, vp]),
+            ("ress_window_attn", [vp] * 4 + [f, vp, vp, vp, sz, vp]),
             ("ress_window_attn_bwd_workspace_size", [vp, vp]),
             ("ress_window_attn_bwd", [vp] * 8 + [f] + [vp] * 4 + [sz, vp]),
             ("ress_window_attn_decode_workspace_size", [vp, vp]),
@@ -76,15 +77,31 @@ def _size(name, shape) -> int:
     return n.value
 
 
-def _workspace(workspace, need, device, stream):
-    """The caller's workspace, or one of torch's (marked as in use on a stream that is not its own)."""
+def _workspace(workspace, size, shape, device, stream):
+    """Address and bytes of the caller's workspace, or of one of torch's (marked as in use on a stream that is not its
+    own), or none where the call needs none."""
     if workspace is None:
-        workspace = torch.empty(max(need(), 1), dtype=torch.uint8, device=device)
-        if isinstance(stream, torch.cuda.Stream) and stream != torch.cuda.current_stream(device):
-            workspace.record_stream(stream)
+        n = _size(size, shape)
+        if n == 0:
+            return None, 0
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(_as_stream(stream, device))
     elif not (workspace.is_cuda and workspace.device == device and workspace.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _as_stream(stream, device):
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _empty(shape, dtype, device, stream):
+    """An output, marked as in use on a stream that is not torch's current one."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(_as_stream(stream, device))
+    return t
 
 
 def _check(name, t, dtype, shape, device):
@@ -151,11 +168,11 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     dev = _device("x", x)
     _norm_check("x", x, None)
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype, device=dev)
+        out = _empty(x.shape, out_dtype, dev, stream)
     _norm_check("out", out, x)
     shape = _norm_shape(x, out, eps)
     if want_stats and mean is None and rstd is None:
-        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) for _ in range(2))
+        mean, rstd = (_empty(x.shape[:-1], torch.float32, dev, stream) for _ in range(2))
     for name, t in (("gamma", gamma), ("beta", beta)):
         if t is not None:
             _check_dense(name, t, torch.float32, (x.shape[-1],), dev)
@@ -182,6 +199,8 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     _norm_check("dy", dy, x)
     if dx is None:
         dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev)
+        if stream is not None:
+            dx.record_stream(_as_stream(stream, dev))
     _norm_check("dx", dx, x)
     shape = _norm_shape(x, dy, 1.0)
     if dx.dtype != x.dtype or _norm_rows(dx) != _norm_rows(x):
@@ -191,16 +210,16 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     if gamma is not None:
         _check_dense("gamma", gamma, torch.float32, (width,), dev)
     if want_weights:
-        dgamma = torch.empty(width, dtype=torch.float32, device=dev) if dgamma is None else dgamma
-        dbeta = torch.empty(width, dtype=torch.float32, device=dev) if dbeta is None else dbeta
+        dgamma = _empty(width, torch.float32, dev, stream) if dgamma is None else dgamma
+        dbeta = _empty(width, torch.float32, dev, stream) if dbeta is None else dbeta
     for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
         if t is not None:
             _check_dense(name, t, torch.float32, (width,), dev)
     ws, ws_bytes = None, 0
     if dgamma is not None or dbeta is not None:
-        ws, ws_bytes = _workspace(workspace, lambda: _size("ress_layer_norm_bwd_workspace_size", shape), dev, stream)
+        ws, ws_bytes = _workspace(workspace, "ress_layer_norm_bwd_workspace_size", shape, dev, stream)
     _call(lib.ress_layer_norm_bwd, dev, stream, shape, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
-          _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws_bytes)
+          _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws, ws_bytes)
     return dict(dx=dx, dgamma=dgamma, dbeta=dbeta)
 
 
@@ -230,7 +249,7 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     if q is not None:
         H = q.shape[0]
         _check("q", q, first.dtype, (H, N, D), dev)
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
+        q_out = _empty(q.shape, q.dtype, dev, stream) if q_out is None else q_out
         _check("q_out", q_out, q.dtype, q.shape, dev)
         qs, qo = _strides(q), _strides(q_out)
     else:
@@ -238,7 +257,7 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     if k is not None:
         H_kv = k.shape[0]
         _check("k", k, first.dtype, (H_kv, N, D), dev)
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev) if k_out is None else k_out
+        k_out = _empty(k.shape, k.dtype, dev, stream) if k_out is None else k_out
         _check("k_out", k_out, k.dtype, k.shape, dev)
         ks, ko = _strides(k), _strides(k_out)
     else:
@@ -273,24 +292,31 @@ def _check_window(q, k, v):
 
 
 def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q_offset: int = 0, causal: bool = True,
-                     scale: float | None = None, out=None, lse=None, want_lse: bool = False, stream=None) -> dict:
+                     scale: float | None = None, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None) -> dict:
     """Attention over a sliding window of frames and the first n_sink tokens (see include/ress_layer.h). q: bf16
     [H][n_q][64] at positions q_offset ..; k, v: bf16 [H_kv][n_k][64]; any strides with contiguous channels.
     Returns o (bf16, as q) and, with want_lse or a given buffer, lse (float32 [H][n_q])."""
     dev = _check_window(q, k, v)
     H, n_q, D = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        out = _empty(q.shape, torch.bfloat16, dev, stream)
     _check("out", out, torch.bfloat16, q.shape, dev)
     if lse is None and want_lse:
-        lse = torch.empty((H, n_q), dtype=torch.float32, device=dev)
+        lse = _empty((H, n_q), torch.float32, dev, stream)
     if lse is not None:
         _check_dense("lse", lse, torch.float32, (H, n_q), dev)
     shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal,
                           _strides(q) + _strides(k) + _strides(v) + _strides(out))
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), scale, _ptr(out), _ptr(lse))
+    ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
+    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), scale, _ptr(out), _ptr(lse), ws, ws_bytes)
     return dict(o=out, lse=lse)
+
+
+def ress_window_attn_workspace_size(H: int, H_kv: int, n_q: int, n_k: int, *, window: int, frame: int = 1, n_sink: int = 0,
+                                    q_offset: int = 0, causal: bool = True) -> int:
+    return _size("ress_window_attn_workspace_size",
+                 _window_shape(H, H_kv, n_q, n_k, 64, q_offset, frame, window, n_sink, causal))
 
 
 def ress_window_attn_bwd_workspace_size(H: int, H_kv: int, n_q: int, n_k: int, *, window: int, frame: int = 1,
@@ -311,7 +337,7 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
     _check_dense("lse", lse, torch.float32, (H, n_q), dev)
     grads = []
     for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-        t = torch.empty(like.shape, dtype=torch.bfloat16, device=dev) if t is None else t
+        t = _empty(like.shape, torch.bfloat16, dev, stream) if t is None else t
         _check(name, t, torch.bfloat16, like.shape, dev)
         grads.append(t)
     dq, dk, dv = grads
@@ -319,9 +345,9 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
                           _strides(q) + _strides(k) + _strides(v) + _strides(o))
     g = _GRADS(*_strides(d_o), *_strides(dq), *_strides(dk), *_strides(dv))
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_bwd_workspace_size", shape), dev, stream)
+    ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), scale,
-          _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws_bytes)
+          _ptr(dq), _ptr(dk), _ptr(dv), ws, ws_bytes)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
@@ -345,7 +371,7 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     _check("v", v, torch.bfloat16, k.shape, dev)
     _check_dense("lens", lens, torch.int32, (B,), dev)
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        out = _empty(q.shape, torch.bfloat16, dev, stream)
     _check("out", out, torch.bfloat16, q.shape, dev)
     q_b, q_h, _ = q.stride()
     k_b, k_h, k_t, _ = k.stride()
@@ -362,7 +388,6 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     shape = _DECODE(B, H, H_kv, capacity, D, _int32(frame), _int32(window), _int32(n_sink), q_b, q_h, k_b, v_b, k_h, k_t,
                     v_h, v_t, o_b, o_h)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    ws, ws_bytes = _workspace(workspace, lambda: _size("ress_window_attn_decode_workspace_size", shape), dev, stream)
-    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), scale, _ptr(out), _ptr(ws),
-          ws_bytes)
+    ws, ws_bytes = _workspace(workspace, "ress_window_attn_decode_workspace_size", shape, dev, stream)
+    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), scale, _ptr(out), ws, ws_bytes)
     return out

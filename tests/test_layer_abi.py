@@ -34,7 +34,8 @@ def test_every_declared_symbol_is_exported_and_bound(ress):
     names = sorted(set(re.findall(r"\b(ress_[a-z0-9_]+)\s*\(", src)))
     assert names == ["ress_layer_norm", "ress_layer_norm_bwd", "ress_layer_norm_bwd_workspace_size", "ress_rope",
                      "ress_window_attn", "ress_window_attn_bwd", "ress_window_attn_bwd_workspace_size",
-                     "ress_window_attn_decode", "ress_window_attn_decode_workspace_size"]
+                     "ress_window_attn_decode", "ress_window_attn_decode_workspace_size",
+                     "ress_window_attn_workspace_size"]
     raw = C.CDLL(ress.LIB_PATH)
     for n in names:
         assert hasattr(raw, n) and hasattr(ress, n), n
@@ -140,10 +141,16 @@ FAR_WINDOWS = (dict(H=258), dict(D=32), dict(n_q=(1 << 24) + 1), dict(n_k=(1 << 
 def test_window_refusals(ress, layer):
     f = ress.lib.ress_window_attn
 
-    def call(sh, q=P[0], k=P[1], v=P[2], scale=0.125, o=P[3], lse=P[4]):
-        return f(C.byref(sh), q, k, v, scale, o, lse, None)
+    def call(sh, q=P[0], k=P[1], v=P[2], scale=0.125, o=P[3], lse=P[4], ws=None, nb=0):
+        return f(C.byref(sh), q, k, v, scale, o, lse, ws, nb, None)
 
     s = _win(layer)
+    long = _win(layer, H=1, H_kv=1, n_q=3, n_k=60000, window=50000, frame=1, k=(0, 64), v=(0, 64))
+    n = C.c_size_t(0)
+    size = ress.lib.ress_window_attn_workspace_size
+    assert size(C.byref(long), C.byref(n)) == OK and n.value > 0 and size(C.byref(long), None) == INVALID
+    assert call(long) == WORKSPACE and call(long, ws=P[5], nb=n.value - 1) == WORKSPACE
+    assert call(long, ws=C.c_void_p(P[5].value + 128), nb=n.value) == WORKSPACE
     for bad in BAD_WINDOWS + (dict(q=(6400, 4)), dict(k=(12, 64)), dict(v=(-64, 64)), dict(o=(6400, 32)),
                               dict(o=(64, 64)), dict(o=(0, 0)), dict(k=(64, (1 << 22) + 8))):
         assert call(_win(layer, **bad)) == INVALID, bad
@@ -157,7 +164,7 @@ def test_window_refusals(ress, layer):
     for x in P[:3]:
         assert call(s, o=x) == INVALID
     assert call(s, lse=P[3]) == INVALID and call(s, lse=P[0]) == INVALID
-    assert f(None, P[0], P[1], P[2], 0.125, P[3], None, None) == INVALID
+    assert f(None, P[0], P[1], P[2], 0.125, P[3], None, None, 0, None) == INVALID
     assert call(_win(layer, n_q=0), q=None, o=None, lse=None) == OK
     assert call(_win(layer, H=0, H_kv=0), q=None, k=None, v=None, o=None) == OK
 
