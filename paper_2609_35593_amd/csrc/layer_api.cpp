@@ -122,7 +122,15 @@ size_t window_workspace(const ress_window_shape *s)
     return splits == 1 ? 0 : align256((size_t)splits * s->H * s->n_q * 66 * sizeof(float));
 }
 
+// Per-query values (two of them), then the slices' sums.
 size_t rows_bytes(const ress_window_shape *s) { return align256((size_t)s->H * s->n_q * sizeof(float)); }
+
+size_t window_bwd_workspace(const ress_window_shape *s)
+{
+    const ress::WindowBwdPlan plan = ress::window_bwd_plan(s);
+    const size_t cut = plan.slices > 1 || plan.sink_slices > 1 ? (size_t)s->H_kv * plan.items : 0;
+    return 2 * rows_bytes(s) + cut * 2 * 128 * 64 * sizeof(float);
+}
 
 int check_decode(const ress_decode_shape *s)
 {
@@ -368,7 +376,7 @@ int ress_window_attn_bwd_workspace_size(const ress_window_shape *shape, size_t *
     int st = check_window(shape, false);
     if (st != RESS_OK) return st;
     if (!bytes) return RESS_E_INVALID_ARG;
-    *bytes = 2 * rows_bytes(shape);
+    *bytes = window_bwd_workspace(shape);
     return RESS_OK;
 }
 
@@ -399,8 +407,8 @@ int ress_window_attn_bwd(const ress_window_shape *shape, const ress_window_grads
         !disjoint(shape->H_kv, grads->dk.head, shape->n_k, grads->dk.token, kHead) ||
         !disjoint(shape->H_kv, grads->dv.head, shape->n_k, grads->dv.token, kHead))
         return RESS_E_INVALID_ARG;
-    const size_t rows = rows_bytes(shape);
-    if (shape->n_q > 0 && (!workspace || ws_bytes < 2 * rows || !aligned(workspace, 256))) return RESS_E_WORKSPACE;
+    const size_t rows = rows_bytes(shape), need = window_bwd_workspace(shape);
+    if (need && (!workspace || ws_bytes < need || !aligned(workspace, 256))) return RESS_E_WORKSPACE;
     ress::WindowBwdParams b;
     b.w = window_params(shape, scale);
     b.w.q = static_cast<const uint16_t *>(q);
@@ -418,7 +426,14 @@ int ress_window_attn_bwd(const ress_window_shape *shape, const ress_window_grads
     b.dv = static_cast<uint16_t *>(dv);
     b.ndelta = static_cast<float *>(workspace);
     b.lse2 = reinterpret_cast<float *>(static_cast<char *>(workspace) + rows);
-    return ress::launch_window_bwd(b, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
+    const ress::WindowBwdPlan plan = ress::window_bwd_plan(shape);
+    b.sink_blocks = plan.sink_blocks;
+    b.sink_slices = plan.sink_slices;
+    b.slices = plan.slices;
+    b.items = plan.items;
+    b.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * rows);
+    b.w.n_qb = (shape->n_q * plan.groups + 127) / 128;
+    return ress::launch_window_bwd(b, plan.groups, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }
 
 int ress_window_attn_decode_workspace_size(const ress_decode_shape *shape, size_t *bytes)

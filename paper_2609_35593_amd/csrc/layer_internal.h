@@ -85,7 +85,17 @@ struct WindowBwdParams {
     uint16_t *dq, *dk, *dv;
     float *ndelta;  // [H][n_q]: -sum_d d_o o
     float *lse2;    // [H][n_q]: lse in base 2, +inf where a query sees nothing
+    // The keys' pass: blocks of 128 keys, those with sinks first, in slices; items per head.
+    int sink_blocks, sink_slices, slices, items;
+    float *part;    // [H_kv items][2][128][64]: dk, dv of the slices of a block that has several
 };
+
+// How the backward pass spreads over the chip. A function of the shape alone.
+struct WindowBwdPlan {
+    int groups;  // key groups of the queries' pass
+    int sink_blocks, sink_slices, slices, items;
+};
+WindowBwdPlan window_bwd_plan(const ress_window_shape *s);
 
 struct DecodeParams {
     int B, H, H_kv, group;
@@ -106,7 +116,7 @@ hipError_t launch_norm(const NormParams &p, hipStream_t s);
 hipError_t launch_norm_bwd(const NormBwdParams &p, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, hipStream_t s);
 hipError_t launch_window(const WindowParams &p, int groups, hipStream_t s);
-hipError_t launch_window_bwd(const WindowBwdParams &p, hipStream_t s);
+hipError_t launch_window_bwd(const WindowBwdParams &p, int groups, hipStream_t s);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s);
 
 }  // namespace ress

@@ -13,7 +13,10 @@
 //                 in norm where keys share a mean). The corrected delta goes to the next kernel;
 //   dkv_kernel    128 keys a workgroup, walking over the tiles of queries that see them,
 //                 query head after query head of those that share the keys:
-//                 S = Q K^T, dP = dO V^T - delta, dV^T += dO^T P, dK^T += Q^T dS.
+//                 S = Q K^T, dP = dO V^T - delta, dV^T += dO^T P, dK^T += Q^T dS. Keys of
+//                 sinks are seen by all later queries, and small calls have few blocks of keys,
+//                 so a block's list may be cut over several workgroups (`slices`), whose float32
+//                 sums join_kernel adds in order.
 // In both a lane holds one column of the score tile (a query, a key), so P and dS, rounded
 // to bf16, are the next products' operands as they lie (tiles.h); -delta enters as the
 // initial value of the accumulator.
@@ -47,32 +50,42 @@ __global__ void __launch_bounds__(256) delta_kernel(const WindowBwdParams b)
     }
 }
 
+template <int G>
 __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
 {
-    __shared__ __attribute__((aligned(1024))) unsigned char k_s[2][kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_s[2][kTileBytes];
+    constexpr int QW = 4 / G, ROWS = 32 * QW;  // waves and queries of a key group (window.hip)
+    __shared__ __attribute__((aligned(1024))) unsigned char slots[4][G * kTileBytes];
     const WindowParams &p = b.w;
     const int rows = p.H * p.n_qb, per = (rows + 7) / 8;
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || at >= rows) return;
     const int h = at / p.n_qb, i = p.n_qb - 1 - (at - h * p.n_qb);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
+    unsigned char *const k_0 = slots[0] + grp * kTileBytes, *const k_1 = slots[1] + grp * kTileBytes;
+    unsigned char *const v_0 = slots[2] + grp * kTileBytes, *const v_1 = slots[3] + grp * kTileBytes;
 
     // Tiles and ranges as in the forward pass (window.hip).
-    const int t_first = i * 128, t_last = min(t_first + 128, p.n_q) - 1;
+    const int t_first = i * ROWS, t_last = min(t_first + ROWS, p.n_q) - 1;
     const Seen s_first = seen_by(p, p.q_offset + t_first), s_last = seen_by(p, p.q_offset + t_last);
     const int ns = (s_last.sk + kTile - 1) / kTile;
     int w0 = s_first.lo / kTile, w1 = (s_last.hi + kTile - 1) / kTile;
     if (s_first.lo >= s_last.hi) w0 = w1 = ns;
     if (w0 < ns) w0 = ns;
     if (w1 < w0) w1 = w0;
-    const int tiles_n = ns + w1 - w0;
-    auto tile_key = [&](int c) __attribute__((always_inline)) { return (c < ns ? c : c - ns + w0) * kTile; };
+    const int tiles_n = ns + w1 - w0, turns = (tiles_n + G - 1) / G;
+    auto tile_key = [&](int n) __attribute__((always_inline)) {
+        const int c = n * G + grp;
+        return (c < ns ? c : c - ns + w0) * kTile;
+    };
     const int ta = min(t_first + wave * 32, t_last), tb = min(t_first + wave * 32 + 31, t_last);
     const Seen sa = seen_by(p, p.q_offset + ta), sb = seen_by(p, p.q_offset + tb);
     const int t = t_first + wave * 32 + ql, tq = min(t, t_last);
-    const Seen sl = seen_by(p, p.q_offset + tq);
+    Seen sl = seen_by(p, p.q_offset + tq);
+    sl.lo -= 4 * hh;
+    sl.hi -= 4 * hh;
+    sl.sk -= 4 * hh;
 
     bf16x8 qf[4], df[4];
     {
@@ -85,75 +98,107 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
         }
     }
     const float lse2 = b.lse2[(int64_t)h * p.n_q + tq], nd = b.ndelta[(int64_t)h * p.n_q + tq];
-    const Loader<4> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
-    const Loader<4> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
+    const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
+    const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
-    auto fetch = [&](int c, int slot) __attribute__((always_inline)) {
-        const int key0 = tile_key(c);
+    auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
+        if (n * G + grp >= tiles_n) return;
+        const int key0 = tile_key(n);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
-        load_k(key0, lo, hi, k_s[slot]);
-        load_v(key0, lo, hi, v_s[slot]);
+        load_k(key0, lo, hi, kd);
+        load_v(key0, lo, hi, vd);
     };
     const float c = p.scale_log2;
     f32x16 acc[2], mean[2];  // sum dS k, sum P k
+    f32x16 nd16;
     float off = 0.f;         // the lane's half of sum dS
 #pragma unroll
-    for (int dh = 0; dh < 2; ++dh)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[dh][v] = mean[dh][v] = 0.f;
+    for (int v = 0; v < 16; ++v) acc[0][v] = acc[1][v] = mean[0][v] = mean[1][v] = 0.f, nd16[v] = nd;
 
-    if (tiles_n > 0) {
-        fetch(0, 0);
-        wait_vm_all();
-        __syncthreads();
-    }
-    for (int ch = 0; ch < tiles_n; ++ch) {
-        const int slot = ch & 1, key0 = tile_key(ch);
-        if (ch + 1 < tiles_n) fetch(ch + 1, slot ^ 1);
-        const bool none = key0 >= sb.sk && (key0 + kTile <= sa.lo || key0 >= sb.hi);
-        if (!none) {
-            const bool part = !(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi));
-            const unsigned char *kt = k_s[slot], *vt = v_s[slot];
+    auto tile = [&](bool part, const unsigned char *kt, const unsigned char *vt, int key0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                f32x16 s, d;
+        for (int u = 0; u < 2; ++u) {
+            f32x16 s, d = nd16;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s[v] = 0.f, d[v] = nd;
+            for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
+            for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(vt, u, kk), df[kk], d);
-                if (part) {
-                    asm volatile("" ::: "memory");
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int key = key0 + u * 32 + (v >> 2) * 8 + (v & 3) + 4 * hh;
-                        const bool in = (key >= sl.lo && key < sl.hi) || key < sl.sk;
-                        s[v] = in ? s[v] : -INFINITY;
-                    }
-                }
+            for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(vt, u, kk), df[kk], d);
+            if (part) {
+                asm volatile("" ::: "memory");
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
-                    d[v] *= s[v];
+                    const int key = __builtin_amdgcn_readfirstlane(key0 + u * 32 + (v >> 2) * 8 + (v & 3));
+                    const bool in = (key >= sl.lo && key < sl.hi) || key < sl.sk;
+                    s[v] = in ? s[v] : -INFINITY;
                 }
-                bf16x8 pb[2], db[2];
-                pack(s, pb);
-                pack(d, db);
-                off = add_up(db, off);
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int dh = 0; dh < 2; ++dh) {
-                        const bf16x8 kc = rd.cols(kt, u, e, dh);
-                        acc[dh] = mfma(kc, db[e], acc[dh]);
-                        mean[dh] = mfma(kc, pb[e], mean[dh]);
-                    }
             }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
+                d[v] *= s[v];
+            }
+            bf16x8 pb[2], db[2];
+            pack(s, pb);
+            pack(d, db);
+            off = add_up(db, off);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dh = 0; dh < 2; ++dh) {
+                    const bf16x8 kc = rd.cols(kt, u, e, dh);
+                    acc[dh] = mfma(kc, db[e], acc[dh]);
+                    mean[dh] = mfma(kc, pb[e], mean[dh]);
+                }
         }
+    };
+    int n = 0;
+    auto step = [&](const unsigned char *kt, const unsigned char *vt, unsigned char *kd, unsigned char *vd)
+                    __attribute__((always_inline)) -> bool {
+        const int key0 = tile_key(n);
+        fetch(n + 1, kd, vd);
+        if ((G == 1 || n * G + grp < tiles_n) && (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi)))
+            tile(!(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi)), kt, vt, key0);
         wait_vm_all();
         __syncthreads();
+        return ++n < turns;
+    };
+    if (turns > 0) {
+        fetch(0, k_0, v_0);
+        wait_vm_all();
+        __syncthreads();
+        while (step(k_0, v_0, k_1, v_1) && step(k_1, v_1, k_0, v_0)) {
+        }
+    }
+    if constexpr (G > 1) {
+        // The groups behind the first leave their sums in the slots (65 floats a lane), in two
+        // rounds: the slots hold one 32-channel half of all of them.
+        constexpr int PER = 33 * 64;
+        static_assert((G - 1) * QW * PER * sizeof(float) <= sizeof slots, "a round's parts fit the slots");
+        float *const area = reinterpret_cast<float *>(slots[0]);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            if (r) __syncthreads();
+            if (grp > 0) {
+                float *m = area + ((grp - 1) * QW + wave) * PER + lane;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) m[v * 64] = acc[r][v], m[(16 + v) * 64] = mean[r][v];
+                m[32 * 64] = off;
+            }
+            __syncthreads();
+            if (grp == 0) {
+#pragma unroll
+                for (int g = 1; g < G; ++g) {
+                    const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[r][v] += m[v * 64], mean[r][v] += m[(16 + v) * 64];
+                    if (r == 0) off += m[32 * 64];
+                }
+            }
+        }
+        if (grp > 0) return;
     }
     off += __shfl_xor(off, 32);
 #pragma unroll
@@ -165,20 +210,39 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
     store_row(b.dq + h * b.dqs.head + (int64_t)t * b.dqs.token, acc, p.scale, hh);
 }
 
+// Item `at` of the keys' pass: a slice of a block of keys. Sink blocks' items come first.
+struct Item {
+    int hk, block, slice, slices;
+};
+__device__ __forceinline__ Item item_of(const WindowBwdParams &b, int at)
+{
+    Item r;
+    r.hk = at / b.items;
+    int x = at - r.hk * b.items;
+    const int sinks = b.sink_blocks * b.sink_slices;
+    r.slices = x < sinks ? b.sink_slices : b.slices;
+    if (x >= sinks) x -= sinks;
+    r.block = x / r.slices;
+    r.slice = x - r.block * r.slices;
+    if (at - r.hk * b.items >= sinks) r.block += b.sink_blocks;
+    return r;
+}
+
 __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
 {
-    __shared__ __attribute__((aligned(1024))) unsigned char q_s[2][kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char d_s[2][kTileBytes];
-    __shared__ __attribute__((aligned(256))) float row_s[2][2][kTile];  // lse2, ndelta of the tile's queries
+    __shared__ __attribute__((aligned(1024))) unsigned char q_0[kTileBytes], q_1[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char d_0[kTileBytes], d_1[kTileBytes];
+    __shared__ __attribute__((aligned(256))) float row_0[2][kTile], row_1[2][kTile];  // lse2, ndelta of the tile's queries
     const WindowParams &p = b.w;
-    const int blocks = p.H_kv * p.n_kb, per = (blocks + 7) / 8;
+    const int items = p.H_kv * b.items, per = (items + 7) / 8;
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || at >= blocks) return;
-    const int hk = at / p.n_kb, j = at - hk * p.n_kb;
+    if ((int)(blockIdx.x >> 3) >= per || at >= items) return;
+    const Item item = item_of(b, at);
+    const int hk = item.hk;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hh = lane >> 5, kl = lane & 31;
 
-    const int s_first = j * 128, s_last = min(s_first + 128, p.n_k) - 1;
+    const int s_first = item.block * 128, s_last = min(s_first + 128, p.n_k) - 1;
     // Queries that see any of the workgroup's keys; of the wave's (none outside [wlo, whi), all
     // inside [alo, ahi)); of the lane's. (The first key's range starts first; sinks are seen
     // to the end, and from keys behind them the last one's range ends last.)
@@ -188,7 +252,9 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
     const int wlo = queries_of(p, ka).lo, whi = ka < p.n_sink ? p.n_q : qb.hi;
     const int alo = qb.lo, ahi = kb < p.n_sink ? p.n_q : queries_of(p, max(ka, p.n_sink)).hi;
     const int key = s_first + wave * 32 + kl, kq = min(key, s_last);
-    const SeenBy ql = queries_of(p, kq);
+    SeenBy ql = queries_of(p, kq);
+    ql.lo -= 4 * hh;
+    ql.hi -= 4 * hh;
 
     bf16x8 kf[4], vf[4];
     {
@@ -202,26 +268,34 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
     }
     Loader<4> load_q(p.q, p.qs.token, wave, lane), load_d(b.d_o, b.dos.token, wave, lane);
     const Reader rd(lane);
+    // The block's list, query head after query head, and this slice's part of it: [n, end).
     const int first = q_lo / kTile, per_head = q_hi > q_lo ? (q_hi + kTile - 1) / kTile - first : 0;
-    const int tiles_n = per_head * p.group;
-    // Tile n: query head hk group + n / per_head, queries 64 (first + n % per_head) ..; kept
-    // as running counters of the next tile to fetch and the one to compute.
-    int fh = hk * p.group, ft = first;
-    auto fetch = [&](int slot) __attribute__((always_inline)) {
-        const int t0 = ft * kTile;
+    const int64_t all = (int64_t)per_head * p.group;
+    int n = (int)(all * item.slice / item.slices);
+    const int end = (int)(all * (item.slice + 1) / item.slices);
+    // Query head and first query of the next tile to fetch, and the latter of the one to compute.
+    int fh = 0, ft = 0, t0 = 0;
+    if (n < end) {
+        fh = hk * p.group + n / per_head;
+        ft = (first + n % per_head) * kTile;
+        t0 = ft;
+    }
+    const int t_end = (first + per_head) * kTile;
+    auto fetch = [&](unsigned char *qd, unsigned char *dd, float (&rows)[2][kTile]) __attribute__((always_inline)) {
         load_q.base = p.q + fh * p.qs.head;
         load_d.base = b.d_o + fh * b.dos.head;
-        load_q(t0, 0, p.n_q, q_s[slot]);
-        load_d(t0, 0, p.n_q, d_s[slot]);
+        load_q(ft, 0, p.n_q, qd);
+        load_d(ft, 0, p.n_q, dd);
         if (wave < 2) {
-            const float *src = (wave == 0 ? b.lse2 : b.ndelta) + (int64_t)fh * p.n_q + t0;
-            const int last = min(kTile, p.n_q - t0) - 1;
+            const float *src = (wave == 0 ? b.lse2 : b.ndelta) + (int64_t)fh * p.n_q + ft;
+            const int last = min(kTile, p.n_q - ft) - 1;
             const __amdgpu_buffer_rsrc_t rs =
                 __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(src), 0, 4 * (last + 1), 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)row_s[slot][wave], 4, 4 * min(lane, last), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)rows[wave], 4, 4 * min(lane, last), 0, 0, 0);
         }
-        if (++ft == first + per_head) {
-            ft = first;
+        ft += kTile;
+        if (ft == t_end) {
+            ft = first * kTile;
             ++fh;
         }
     };
@@ -232,83 +306,159 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) dk[dh][v] = 0.f, dv[dh][v] = 0.f;
 
-    if (tiles_n > 0) {
-        fetch(0);
-        wait_vm_all();
-        __syncthreads();
-    }
-    int t0 = first * kTile;
-    for (int n = 0; n < tiles_n; ++n) {
-        const int slot = n & 1;
-        if (n + 1 < tiles_n) fetch(slot ^ 1);
-        if (t0 < whi && t0 + kTile > wlo) {
-            const bool part = !(t0 >= alo && t0 + kTile <= ahi);
-            const unsigned char *qt = q_s[slot], *dt = d_s[slot];
+    auto tile = [&](bool part, const unsigned char *qt, const unsigned char *dt, const float (&rows)[2][kTile])
+                    __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                f32x16 s, d, l;
+        for (int u = 0; u < 2; ++u) {
+            f32x16 s, d, l;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 a = *reinterpret_cast<const f32x4 *>(&row_s[slot][0][u * 32 + g * 8 + hh * 4]);
-                    const f32x4 e = *reinterpret_cast<const f32x4 *>(&row_s[slot][1][u * 32 + g * 8 + hh * 4]);
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 a = *reinterpret_cast<const f32x4 *>(&rows[0][u * 32 + g * 8 + hh * 4]);
+                const f32x4 e = *reinterpret_cast<const f32x4 *>(&rows[1][u * 32 + g * 8 + hh * 4]);
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) s[g * 4 + v] = 0.f, l[g * 4 + v] = a[v], d[g * 4 + v] = e[v];
-                }
+                for (int v = 0; v < 4; ++v) s[g * 4 + v] = 0.f, l[g * 4 + v] = a[v], d[g * 4 + v] = e[v];
+            }
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(qt, u, kk), kf[kk], s);
+            for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(qt, u, kk), kf[kk], s);
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(dt, u, kk), vf[kk], d);
-                if (part) {
-                    asm volatile("" ::: "memory");
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int t = t0 + u * 32 + (v >> 2) * 8 + (v & 3) + 4 * hh;
-                        s[v] = t >= ql.lo && t < ql.hi ? s[v] : -INFINITY;
-                    }
-                }
+            for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(dt, u, kk), vf[kk], d);
+            if (part) {
+                asm volatile("" ::: "memory");
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -l[v]));
-                    d[v] *= s[v];
+                    const int t = __builtin_amdgcn_readfirstlane(t0 + u * 32 + (v >> 2) * 8 + (v & 3));
+                    s[v] = t >= ql.lo && t < ql.hi ? s[v] : -INFINITY;
                 }
-                bf16x8 pb[2], db[2];
-                pack(s, pb);
-                pack(d, db);
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int dh = 0; dh < 2; ++dh) {
-                        dv[dh] = mfma(rd.cols(dt, u, e, dh), pb[e], dv[dh]);
-                        dk[dh] = mfma(rd.cols(qt, u, e, dh), db[e], dk[dh]);
-                    }
             }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -l[v]));
+                d[v] *= s[v];
+            }
+            bf16x8 pb[2], db[2];
+            pack(s, pb);
+            pack(d, db);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dh = 0; dh < 2; ++dh) {
+                    dv[dh] = mfma(rd.cols(dt, u, e, dh), pb[e], dv[dh]);
+                    dk[dh] = mfma(rd.cols(qt, u, e, dh), db[e], dk[dh]);
+                }
         }
+    };
+    auto step = [&](const unsigned char *qt, const unsigned char *dt, const float (&rt)[2][kTile], unsigned char *qd,
+                    unsigned char *dd, float (&rd_)[2][kTile]) __attribute__((always_inline)) -> bool {
+        if (n + 1 < end) fetch(qd, dd, rd_);
+        if (t0 < whi && t0 + kTile > wlo) tile(!(t0 >= alo && t0 + kTile <= ahi), qt, dt, rt);
         t0 += kTile;
-        if (t0 == (first + per_head) * kTile) t0 = first * kTile;
+        if (t0 == t_end) t0 = first * kTile;
         wait_vm_all();
         __syncthreads();
+        return ++n < end;
+    };
+    if (n < end) {
+        fetch(q_0, d_0, row_0);
+        wait_vm_all();
+        __syncthreads();
+        while (step(q_0, d_0, row_0, q_1, d_1, row_1) && step(q_1, d_1, row_1, q_0, d_0, row_0)) {
+        }
     }
-    if (key <= s_last) {
+    if (item.slices > 1) {
+        float *part = b.part + ((int64_t)at * 2 * 128 + wave * 32 + kl) * 64;
+#pragma unroll
+        for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float *at_c = part + dh * 32 + g * 8 + hh * 4;
+                *reinterpret_cast<f32x4 *>(at_c) = f32x4{dk[dh][g * 4], dk[dh][g * 4 + 1], dk[dh][g * 4 + 2], dk[dh][g * 4 + 3]};
+                *reinterpret_cast<f32x4 *>(at_c + 128 * 64) =
+                    f32x4{dv[dh][g * 4], dv[dh][g * 4 + 1], dv[dh][g * 4 + 2], dv[dh][g * 4 + 3]};
+            }
+    } else if (key <= s_last) {
         store_row(b.dk + hk * b.dks.head + (int64_t)key * b.dks.token, dk, p.scale, hh);
         store_row(b.dv + hk * b.dvs.head + (int64_t)key * b.dvs.token, dv, 1.f, hh);
     }
 }
 
+// Blocks of keys whose list was cut: a workgroup 32 keys of dk (even) or dv, 2 x 4 channels a
+// thread, the slices in order. blockIdx.y counts the cut blocks of all heads.
+__global__ void __launch_bounds__(256) join_kernel(const WindowBwdParams b, int cut)
+{
+    const WindowParams &p = b.w;
+    const int hk = blockIdx.y / cut, block = blockIdx.y % cut;
+    const int slices = block < b.sink_blocks ? b.sink_slices : b.slices;
+    const int at = hk * b.items + (block < b.sink_blocks
+                                       ? block * b.sink_slices
+                                       : b.sink_blocks * b.sink_slices + (block - b.sink_blocks) * b.slices);
+    const int tensor = blockIdx.x & 1, row = (blockIdx.x >> 1) * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+    const int key = block * 128 + row;
+    if (key >= p.n_k) return;
+    const float *part = b.part + (((int64_t)at * 2 + tensor) * 128 + row) * 64 + c;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll 4
+    for (int s = 0; s < slices; ++s) {
+        x += *reinterpret_cast<const f32x4 *>(part + (int64_t)s * 2 * 128 * 64);
+        y += *reinterpret_cast<const f32x4 *>(part + (int64_t)s * 2 * 128 * 64 + 4);
+    }
+    const float f = tensor ? 1.f : p.scale;
+    uint16_t *out = tensor ? b.dv + hk * b.dvs.head + (int64_t)key * b.dvs.token : b.dk + hk * b.dks.head + (int64_t)key * b.dks.token;
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)(x[e] * f), o[e + 4] = (__bf16)(y[e] * f);
+    *reinterpret_cast<bf16x8 *>(out + c) = o;
+}
+
 }  // namespace
 
-hipError_t launch_window_bwd(const WindowBwdParams &b, hipStream_t s)
+WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
+{
+    WindowBwdPlan r = {window_plan(s).groups, 0, 1, 1, 0};
+    const int64_t blocks = (s->n_k + 127) / 128;
+    if (s->H_kv == 0 || blocks == 0) return r;
+    const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k, group = s->H / s->H_kv;
+    r.sink_blocks = (int)((sinks + 127) / 128);
+    // Tiles of queries in a list at most: of sinks, and of other keys.
+    const int64_t span = (int64_t)s->frame * s->window * (s->causal ? 1 : 2) + s->frame + 127;
+    const int64_t all = ((int64_t)s->n_q + 63) / 64;
+    const int64_t some = span < s->n_q ? (span + 63) / 64 + 1 : all;
+    const int64_t t_sink = group * all, t_win = group * (some < all ? some : all);
+    const int64_t total = s->H_kv * (r.sink_blocks * t_sink + (blocks - r.sink_blocks) * t_win);
+    // Lists of about a 1,024th of the work (the chip holds 512 workgroups), of 12 tiles at least:
+    // shorter ones take more to join than they save (3,001 tokens, 12 heads, 5 sinks: lists of 6 /
+    // 8 / 12 / 16 tiles 40.7 / 42.4 / 38.6 / 41.2 us with the join; uncut 232).
+    const int64_t goal = total / 1024 > 12 ? total / 1024 : 12;
+    auto slices = [&](int64_t t) { return (int)(2 * t <= 3 * goal ? 1 : (t + goal - 1) / goal > 64 ? 64 : (t + goal - 1) / goal); };
+    r.sink_slices = slices(t_sink);
+    r.slices = slices(t_win);
+    r.items = (int)(r.sink_blocks * r.sink_slices + (blocks - r.sink_blocks) * r.slices);
+    return r;
+}
+
+hipError_t launch_window_bwd(const WindowBwdParams &b, int groups, hipStream_t s)
 {
     const WindowParams &p = b.w;
     if (p.n_q > 0) {
         const int64_t rows = (int64_t)p.H * p.n_q;
         hipLaunchKernelGGL(delta_kernel, dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, s, b);
         if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL(dq_kernel, dim3(8u * (unsigned)((p.H * p.n_qb + 7) / 8)), dim3(256), 0, s, b);
+        const dim3 grid(8u * (unsigned)((p.H * p.n_qb + 7) / 8)), block(256);
+        if (groups == 1)
+            hipLaunchKernelGGL(dq_kernel<1>, grid, block, 0, s, b);
+        else if (groups == 2)
+            hipLaunchKernelGGL(dq_kernel<2>, grid, block, 0, s, b);
+        else
+            hipLaunchKernelGGL(dq_kernel<4>, grid, block, 0, s, b);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (p.n_k > 0) {
-        hipLaunchKernelGGL(dkv_kernel, dim3(8u * (unsigned)((p.H_kv * p.n_kb + 7) / 8)), dim3(256), 0, s, b);
-        return hipGetLastError();
+        hipLaunchKernelGGL(dkv_kernel, dim3(8u * (unsigned)((p.H_kv * b.items + 7) / 8)), dim3(256), 0, s, b);
+        if (hipError_t e = hipGetLastError()) return e;
+        const int cut = b.slices > 1 ? p.n_kb : b.sink_slices > 1 ? b.sink_blocks : 0;
+        if (cut) {
+            hipLaunchKernelGGL(join_kernel, dim3(8, (unsigned)(p.H_kv * cut)), dim3(256), 0, s, b, cut);
+            return hipGetLastError();
+        }
     }
     return hipSuccess;
 }
