@@ -5,9 +5,9 @@
 // value's 64 channels, a wave 8 keys at a time, and the up to R query heads that share a
 // K/V head are formed from one read. The visible keys, sinks and window, are numbered
 // through (j -> key), so no work goes into masked ones and nothing outside them is read.
-// They are cut over `splits` workgroups, and in those over 4 waves of 64 keys a turn; every
-// 8 lanes keep an online softmax of their own, joined in a fixed order in the wave, the
-// workgroup, and for more than one split by join_kernel.
+// They are cut over `splits` workgroups of 4 waves, a run of turns of 32 keys each, the next
+// turn's loads under way; every 8 lanes keep an online softmax of their own, joined in a
+// fixed order in the wave, the workgroup, and for more than one split by join_kernel.
 #include "layer_internal.h"
 
 namespace ress {
@@ -28,10 +28,21 @@ __device__ __forceinline__ float dot2(unsigned int a, unsigned int b, float c)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
 }
 
-// exp2(a - m), 0 for a = -inf (also against m = -inf).
-__device__ __forceinline__ float weight(float a, float m)
+// The reference of a part without keys: below every logit, and finite, so that its weight and
+// that of a masked key are 0 without a test.
+constexpr float kNone = -1e30f;
+
+// Sum over the 8 lanes of a key, the same in each.
+template <int CTRL>
+__device__ __forceinline__ float add_from(float x)
 {
-    return a == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a - m);
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum8(float x)
+{
+    x = add_from<0xB1>(x);   // lanes 1 0 3 2
+    x = add_from<0x4E>(x);   // lanes 2 3 0 1
+    return add_from<0x141>(x);  // mirrored in 8 lanes
 }
 
 // What sequence b's token sees, numbered through: j < sk is key j, else key j - sk + lo.
@@ -61,9 +72,9 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ch = lane & 7, oct = lane >> 3;
     const Visible vis = visible(p, b);
 
-    // Whole turns of 64 keys, in order over the splits.
-    const int turns = (vis.n + 63) / 64, each = (turns + p.splits - 1) / p.splits;
-    const int first = split * each, last = min(first + each, turns);
+    // Whole turns of 32 keys, evenly over the splits' waves.
+    const int turns = (vis.n + 31) / 32, waves = p.splits * 4, each = (turns + waves - 1) / waves;
+    const int first = (split * 4 + wave) * each, last = min(first + each, turns);
 
     u32x4 q[R];
 #pragma unroll
@@ -77,45 +88,47 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     float m[R], l[R], acc[R][8];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        m[r] = -INFINITY;
+        m[r] = kNone;
         l[r] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[r][e] = 0.f;
     }
-    for (int t = first + wave; t < last; t += 4) {
-        u32x4 kx[8], vx[8];
+    u32x4 kx[4], vx[4], kn[4], vn[4];
+    auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = t * 64 + i * 8 + oct;
+        for (int i = 0; i < 4; ++i) {
+            // (Past the end: the last key again, its weight 0 and its value left out.)
+            const int j = min(t * 32 + i * 8 + oct, vis.n - 1);
             const int64_t key = j < vis.sk ? j : j - vis.sk + vis.lo;
-            kx[i] = vx[i] = u32x4{0, 0, 0, 0};
-            if (j < vis.n) {
-                kx[i] = *reinterpret_cast<const u32x4 *>(kb + key * p.ks.token);
-                vx[i] = *reinterpret_cast<const u32x4 *>(vb + key * p.vs.token);
-            }
+            kn[i] = *reinterpret_cast<const u32x4 *>(kb + key * p.ks.token);
+            vn[i] = *reinterpret_cast<const u32x4 *>(vb + key * p.vs.token);
         }
+    };
+    if (first < last) fetch(first);
+    for (int t = first; t < last; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kx[i] = kn[i], vx[i] = vn[i];
+        if (t + 1 < last) fetch(t + 1);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float s[8], top = m[r];
+            float s[4], top = m[r];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 float d = 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d = dot2(kx[i][e], q[r][e], d);
-                d += __shfl_xor(d, 1);
-                d += __shfl_xor(d, 2);
-                d += __shfl_xor(d, 4);
-                s[i] = t * 64 + i * 8 + oct < vis.n ? d * p.scale_log2 : -INFINITY;
+                d = sum8(d) * p.scale_log2;
+                s[i] = t * 32 + i * 8 + oct < vis.n ? d : -INFINITY;
                 top = fmaxf(top, s[i]);
             }
-            const float a = weight(m[r], top);
+            const float a = __builtin_amdgcn_exp2f(m[r] - top);
             m[r] = top;
             l[r] *= a;
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[r][e] *= a;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w = weight(s[i], top);
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(s[i] - top);
                 l[r] += w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -131,7 +144,7 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
         float top = m[r];
 #pragma unroll
         for (int o = 8; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-        const float a = weight(m[r], top);
+        const float a = __builtin_amdgcn_exp2f(m[r] - top);
         l[r] *= a;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[r][e] *= a;
@@ -150,12 +163,12 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     }
     __syncthreads();
     for (int r = wave; r < heads; r += 4) {
-        float top = -INFINITY, sum = 0.f, o = 0.f;
+        float top = kNone, sum = 0.f, o = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, lds[w][r][0]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float a = weight(lds[w][r][0], top);
+            const float a = __builtin_amdgcn_exp2f(lds[w][r][0] - top);
             sum = fmaf(lds[w][r][1], a, sum);
             o = fmaf(lds[w][r][2 + lane], a, o);
         }
@@ -171,20 +184,33 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     }
 }
 
-// A wave a query head: its splits in order.
+// A wave a query head, a channel a lane: its at most 64 splits in order, their weights one a
+// lane first.
 __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
 {
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= (int64_t)p.B * p.H) return;
     const int lane = threadIdx.x & 63;
     const float *d = p.part + row * p.splits * kPart;
-    float top = -INFINITY, sum = 0.f, o = 0.f;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, d[s * kPart]);
-    for (int s = 0; s < p.splits; ++s) {
-        const float a = weight(d[s * kPart], top);
-        sum = fmaf(d[s * kPart + 1], a, sum);
-        o = fmaf(d[s * kPart + 2 + lane], a, o);
-    }
+    // (The first parts are on their way with their references: one round trip for most calls.)
+    constexpr int AHEAD = 16;
+    float m = kNone, sum = 0.f, o = 0.f, x[AHEAD];
+    if (lane < p.splits) m = d[lane * kPart], sum = d[lane * kPart + 1];
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) x[s] = d[min(s, p.splits - 1) * kPart + 2 + lane];
+    float top = m;
+#pragma unroll
+    for (int e = 1; e < 64; e <<= 1) top = fmaxf(top, __shfl_xor(top, e));
+    const float w = __builtin_amdgcn_exp2f(m - top);
+    sum *= w;
+#pragma unroll
+    for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
+    auto weight = [&](int s) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s)); };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (s < p.splits) o = fmaf(weight(s), x[s], o);
+#pragma unroll 8
+    for (int s = AHEAD; s < p.splits; ++s) o = fmaf(weight(s), d[s * kPart + 2 + lane], o);
     const int64_t b = row / p.H, h = row - b * p.H;
     p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)(sum == 0.f ? 0.f : o / sum));
 }
@@ -204,17 +230,19 @@ hipError_t go(const DecodeParams &p, hipStream_t s)
 
 }  // namespace
 
-// Workgroups per sequence and head: enough for 4 a CU, but none with less than one turn of
-// its 4 waves.
+// Workgroups per sequence and head: enough for 4 a CU, but none with less than 4 turns for
+// each of its 4 waves (us with 256 / 512 keys at least, the join counted: 16 heads of 6,870 keys
+// 13.1 / 10.3, 8 x 4 of 4,000 23 / 18, 4 x 8 of 300 7.5 / 5.3, 4 of 1,000 10.6 / 12.0; 768 heads
+// in two halves each 81, whole 74).
 int decode_splits(const ress_decode_shape *s)
 {
     if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
     const int64_t seen = (int64_t)s->window * s->frame + s->n_sink;
     const int64_t keys = seen < s->capacity ? seen : s->capacity;
     const int64_t heads = (int64_t)s->B * s->H_kv * ((s->H / s->H_kv + 3) / 4);
-    const int64_t want = (1024 + heads - 1) / heads, most = (keys + 255) / 256;
+    const int64_t want = 1024 / heads, most = (keys + 511) / 512;
     const int64_t n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n);
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
 
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s)
