@@ -51,7 +51,7 @@ int check_norm(const ress_norm_shape *s)
 
 size_t norm_workspace(const ress_norm_shape *s)
 {
-    return align256((size_t)ress::norm_bwd_parts(s->rows, s->width) * 2 * s->width * sizeof(float));
+    return align256((size_t)ress::norm_bwd_parts(s->rows) * 2 * s->width * sizeof(float));
 }
 
 // An output that is an input must lie as it does.
@@ -221,7 +221,7 @@ int ress_layer_norm_bwd(const ress_norm_shape *shape, const void *dy, const void
     p.x_stride = shape->x_stride;
     p.y_stride = shape->y_stride;
     p.width = shape->width;
-    p.parts = ress::norm_bwd_parts(shape->rows, shape->width);
+    p.parts = ress::norm_bwd_parts(shape->rows);
     p.x_f32 = shape->x_dtype == RESS_DTYPE_F32;
     p.y_f32 = shape->y_dtype == RESS_DTYPE_F32;
     p.dy = dy;

@@ -32,9 +32,8 @@ struct NormBwdParams {
     float *dgamma, *dbeta;
 };
 
-// Workgroups of the backward pass: a function of rows and width alone, so that the
-// workspace is.
-int norm_bwd_parts(int64_t rows, int width);
+// Workgroups of the backward pass at most, each with a row of partial sums.
+int norm_bwd_parts(int64_t rows);
 
 constexpr int kMaxPairs = RESS_MAX_ROPE_D / 2;
 
