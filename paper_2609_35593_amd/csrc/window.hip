@@ -41,10 +41,13 @@ __device__ __forceinline__ float share(float ref, float sum, float top)
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
 template <bool LSE, int G>
-__global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const WindowParams p)
+__global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const WindowParams p)
 {
     constexpr int QW = 4 / G, ROWS = 32 * QW;  // waves and queries of a group
-    __shared__ __attribute__((aligned(1024))) unsigned char slots[4][G * kTileBytes];
+    // (Arrays of their own: of one array's parts the compiler does not see that a read of one
+    // slot need not wait for the load into another.)
+    __shared__ __attribute__((aligned(1024))) unsigned char k_a0[G * kTileBytes], k_a1[G * kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_a0[G * kTileBytes], v_a1[G * kTileBytes];
 
     // Contiguous runs of (head, query block) per XCD, whose L2 then holds few heads'
     // windows; last blocks first (a causal row sees the more the later it is).
@@ -55,8 +58,8 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const Window
     const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
-    unsigned char *const k_0 = slots[0] + grp * kTileBytes, *const k_1 = slots[1] + grp * kTileBytes;
-    unsigned char *const v_0 = slots[2] + grp * kTileBytes, *const v_1 = slots[3] + grp * kTileBytes;
+    unsigned char *const k_0 = k_a0 + grp * kTileBytes, *const k_1 = k_a1 + grp * kTileBytes;
+    unsigned char *const v_0 = v_a0 + grp * kTileBytes, *const v_1 = v_a1 + grp * kTileBytes;
 
     // The block's tiles: [0, ns) and [w0, w1); this workgroup's: from `begin`, tiles_n of them.
     const int t_first = i * ROWS, t_last = min(t_first + ROWS, p.n_q) - 1;
@@ -226,10 +229,13 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const Window
     if constexpr (G > 1) {
         // The groups behind the first leave reference, sum and O in the slots (34 floats a lane).
         constexpr int PER = 34 * 64;
-        static_assert((G - 1) * QW * PER * sizeof(float) <= sizeof slots, "the joined parts fit the slots");
-        float *const area = reinterpret_cast<float *>(slots[0]);
+        constexpr int FIT = G * kTileBytes / (PER * 4);  // waves per slot array
+        static_assert((G - 1) * QW <= 2 * FIT, "the joined parts fit the key slots");
+        auto area = [&](int w) __attribute__((always_inline)) -> float * {
+            return reinterpret_cast<float *>(w < FIT ? k_a0 : k_a1) + w % FIT * PER + lane;
+        };
         if (grp > 0) {
-            float *m = area + ((grp - 1) * QW + wave) * PER + lane;
+            float *m = area((grp - 1) * QW + wave);
             m[0] = ref;
             m[64] = sum;
 #pragma unroll
@@ -240,7 +246,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const Window
         float to = sum == 0.f ? -INFINITY : ref;
 #pragma unroll
         for (int g = 1; g < G; ++g) {
-            const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+            const float *m = area((g - 1) * QW + wave);
             if (m[64] != 0.f) to = fmaxf(to, m[0]);
         }
         const float a0 = share(ref, sum, to);
@@ -249,7 +255,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 3) window_kernel(const Window
         for (int v = 0; v < 32; ++v) acc[v >> 4][v & 15] *= a0;
 #pragma unroll
         for (int g = 1; g < G; ++g) {
-            const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+            const float *m = area((g - 1) * QW + wave);
             const float a = share(m[0], m[64], to);
             sum = fmaf(m[64], a, sum);
 #pragma unroll

@@ -54,7 +54,10 @@ template <int G>
 __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
 {
     constexpr int QW = 4 / G, ROWS = 32 * QW;  // waves and queries of a key group (window.hip)
-    __shared__ __attribute__((aligned(1024))) unsigned char slots[4][G * kTileBytes];
+    // (Arrays of their own: of one array's parts the compiler does not see that a read of one
+    // slot need not wait for the load into another.)
+    __shared__ __attribute__((aligned(1024))) unsigned char k_a0[G * kTileBytes], k_a1[G * kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_a0[G * kTileBytes], v_a1[G * kTileBytes];
     const WindowParams &p = b.w;
     const int rows = p.H * p.n_qb, per = (rows + 7) / 8;
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -63,8 +66,8 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
     const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
-    unsigned char *const k_0 = slots[0] + grp * kTileBytes, *const k_1 = slots[1] + grp * kTileBytes;
-    unsigned char *const v_0 = slots[2] + grp * kTileBytes, *const v_1 = slots[3] + grp * kTileBytes;
+    unsigned char *const k_0 = k_a0 + grp * kTileBytes, *const k_1 = k_a1 + grp * kTileBytes;
+    unsigned char *const v_0 = v_a0 + grp * kTileBytes, *const v_1 = v_a1 + grp * kTileBytes;
 
     // Tiles and ranges as in the forward pass (window.hip).
     const int t_first = i * ROWS, t_last = min(t_first + ROWS, p.n_q) - 1;
@@ -176,13 +179,16 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
         // The groups behind the first leave their sums in the slots (65 floats a lane), in two
         // rounds: the slots hold one 32-channel half of all of them.
         constexpr int PER = 33 * 64;
-        static_assert((G - 1) * QW * PER * sizeof(float) <= sizeof slots, "a round's parts fit the slots");
-        float *const area = reinterpret_cast<float *>(slots[0]);
+        constexpr int FIT = G * kTileBytes / (PER * 4);  // waves per slot array
+        static_assert((G - 1) * QW <= 2 * FIT, "a round's parts fit the key slots");
+        auto area = [&](int w) __attribute__((always_inline)) -> float * {
+            return reinterpret_cast<float *>(w < FIT ? k_a0 : k_a1) + w % FIT * PER + lane;
+        };
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             if (r) __syncthreads();
             if (grp > 0) {
-                float *m = area + ((grp - 1) * QW + wave) * PER + lane;
+                float *m = area((grp - 1) * QW + wave);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) m[v * 64] = acc[r][v], m[(16 + v) * 64] = mean[r][v];
                 m[32 * 64] = off;
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
             if (grp == 0) {
 #pragma unroll
                 for (int g = 1; g < G; ++g) {
-                    const float *m = area + ((g - 1) * QW + wave) * PER + lane;
+                    const float *m = area((g - 1) * QW + wave);
 #pragma unroll
                     for (int v = 0; v < 16; ++v) acc[r][v] += m[v * 64], mean[r][v] += m[(16 + v) * 64];
                     if (r == 0) off += m[32 * 64];
