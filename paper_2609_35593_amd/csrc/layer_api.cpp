@@ -85,9 +85,6 @@ int check_window(const ress_window_shape *s, bool strides)
     return RESS_OK;
 }
 
-// Positions stay below 2^25, so frames and windows beyond 2^26 act as 2^26 does.
-int at_most_2_26(int x) { return x < (1 << 26) ? x : 1 << 26; }
-
 ress::WindowParams window_params(const ress_window_shape *s, float scale)
 {
     ress::WindowParams p;
@@ -98,8 +95,8 @@ ress::WindowParams window_params(const ress_window_shape *s, float scale)
     p.n_q = s->n_q;
     p.n_k = s->n_k;
     p.q_offset = s->q_offset;
-    p.frame = at_most_2_26(s->frame);
-    p.window = at_most_2_26(s->window);
+    p.frame = ress::at_most_2_26(s->frame);
+    p.window = ress::at_most_2_26(s->window);
     p.n_sink = s->n_sink;
     p.causal = s->causal != 0;
     p.n_qb = (s->n_q + 127) / 128;
@@ -470,8 +467,8 @@ int ress_window_attn_decode(const ress_decode_shape *shape, const void *q, const
     p.H_kv = s.H_kv;
     p.group = s.H / s.H_kv;
     p.capacity = s.capacity;
-    p.frame = at_most_2_26(s.frame);
-    p.window = at_most_2_26(s.window);
+    p.frame = ress::at_most_2_26(s.frame);
+    p.window = ress::at_most_2_26(s.window);
     p.n_sink = s.n_sink;
     p.splits = ress::decode_splits(shape);
     p.scale_log2 = scale * 1.4426950408889634f;

@@ -70,6 +70,11 @@ struct WindowParams {
     float2 *part_row;   // and [splits][H][n_q], references and sums
 };
 
+// Positions stay below 2^25, so frames and windows beyond 2^26 act as 2^26 does, whose product
+// leaves room in 64 bits.
+inline int at_most_2_26(int x) { return x < (1 << 26) ? x : 1 << 26; }
+inline int64_t window_tokens(int frame, int window) { return (int64_t)at_most_2_26(frame) * at_most_2_26(window); }
+
 // How the forward pass spreads over the chip: key groups in a workgroup (1, 2, 4),
 // workgroups per block of 128 / groups queries. A function of the shape alone.
 struct WindowPlan {

@@ -324,7 +324,7 @@ hipError_t go(const WindowParams &p, hipStream_t s)
 WindowPlan window_plan(const ress_window_shape *s)
 {
     // Tiles a block sees at most.
-    const int64_t window = (int64_t)s->window * s->frame * (s->causal ? 1 : 2) + 128;
+    const int64_t window = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2) + 128;
     const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k;
     const int64_t keys = window + sinks < s->n_k ? window + sinks : s->n_k;
     const int64_t tiles = (keys + 63) / 64;

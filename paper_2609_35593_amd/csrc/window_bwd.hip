@@ -425,7 +425,7 @@ WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
     const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k, group = s->H / s->H_kv;
     r.sink_blocks = (int)((sinks + 127) / 128);
     // Tiles of queries in a list at most: of sinks, and of other keys.
-    const int64_t span = (int64_t)s->frame * s->window * (s->causal ? 1 : 2) + s->frame + 127;
+    const int64_t span = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2) + at_most_2_26(s->frame) + 127;
     const int64_t all = ((int64_t)s->n_q + 63) / 64;
     const int64_t some = span < s->n_q ? (span + 63) / 64 + 1 : all;
     const int64_t t_sink = group * all, t_win = group * (some < all ? some : all);

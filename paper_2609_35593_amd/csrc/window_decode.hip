@@ -237,7 +237,7 @@ hipError_t go(const DecodeParams &p, hipStream_t s)
 int decode_splits(const ress_decode_shape *s)
 {
     if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
-    const int64_t seen = (int64_t)s->window * s->frame + s->n_sink;
+    const int64_t seen = window_tokens(s->frame, s->window) + s->n_sink;
     const int64_t keys = seen < s->capacity ? seen : s->capacity;
     const int64_t heads = (int64_t)s->B * s->H_kv * ((s->H / s->H_kv + 3) / 4);
     const int64_t want = 1024 / heads, most = (keys + 511) / 512;

@@ -20,14 +20,26 @@ ROPE_LAYOUTS = {"split": 0, "interleaved": 1, "sections": 2}
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
 
 
+def _packer(fields):
+    pack = struct.Struct(fields).pack
+
+    def packed(*values):
+        try:
+            return pack(*values)
+        except struct.error as e:
+            raise ValueError(f"an argument is no number of its C type: {e}") from None
+
+    return packed
+
+
 # The shapes of ress_layer.h, packed as C lays them out (strides are pairs head, token). Packing takes a tenth of the
 # time that filling in ctypes structures does, which shows in calls of a few microseconds.
-_NORM = struct.Struct("@q3i2qd").pack      # rows; width, x_dtype, y_dtype; x_stride, y_stride; eps
-_ROPE = struct.Struct("@12id8q").pack      # H, H_kv, N, D, n_axes, dims[4], layout, inverse, dtype; base; q, k, q_out, k_out
-_WINDOW = struct.Struct("@10i8q").pack     # H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal; q, k, v, o
-_GRADS = struct.Struct("@8q").pack         # d_o, dq, dk, dv
-_DECODE = struct.Struct("@8i10q").pack     # B, H, H_kv, capacity, D, frame, window, n_sink; q_batch, q_head, k_batch,
-                                           # v_batch, k, v, o_batch, o_head
+_NORM = _packer("@q3i2qd")     # rows; width, x_dtype, y_dtype; x_stride, y_stride; eps
+_ROPE = _packer("@12id8q")     # H, H_kv, N, D, n_axes, dims[4], layout, inverse, dtype; base; q, k, q_out, k_out
+_WINDOW = _packer("@10i8q")    # H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal; q, k, v, o
+_GRADS = _packer("@8q")        # d_o, dq, dk, dv
+_DECODE = _packer("@8i10q")    # B, H, H_kv, capacity, D, frame, window, n_sink; q_batch, q_head, k_batch, v_batch, k, v,
+                               # o_batch, o_head
 
 
 def _declare():
@@ -125,11 +137,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _strides(t):
-    """Of [heads][tokens][channels]. (The stride of a dimension of one entry says nothing: torch may give any.)"""
-    n, m, _ = t.shape
-    head, token, _ = t.stride()
-    return head if n > 1 else 0, token if m > 1 else 0
+def _strides(name, t, dtype, shape, device):
+    """The strides (heads, tokens) of a [heads][tokens][channels] tensor whose metadata must be these. (The stride of a
+    dimension of one entry says nothing: torch may give any.)"""
+    if t.dtype is dtype and t.shape == shape and t.device == device:
+        head, token, channel = t.stride()
+        if channel == 1 or shape[2] <= 1:
+            return head if shape[0] > 1 else 0, token if shape[1] > 1 else 0
+    raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
 
 
 # ---------------------------------------------------------------- layer norm
@@ -139,9 +154,10 @@ def _norm_rows(t):
     """Rows and their stride: [rows][width] with any row stride, or a contiguous tensor of any rank."""
     if t.dim() == 2:
         rows, width = t.shape
-        if width > 1 and t.stride(1) != 1:
+        stride, channel = t.stride()
+        if channel != 1 and width > 1:
             raise ValueError("a row's channels must be contiguous")
-        return rows, t.stride(0) if rows > 1 else width
+        return rows, stride if rows > 1 else width
     if t.dim() == 0 or not t.is_contiguous():
         raise ValueError("tensors of other ranks than [rows][width] must be contiguous")
     return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1]
@@ -149,8 +165,7 @@ def _norm_rows(t):
 
 def _norm_shape(x, y, eps):
     rows, xs = _norm_rows(x)
-    _, ys = _norm_rows(y)
-    return _NORM(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, ys, eps)
+    return _NORM(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, _norm_rows(y)[1], eps)
 
 
 def _norm_check(name, t, like):
@@ -173,12 +188,14 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     shape = _norm_shape(x, out, eps)
     if want_stats and mean is None and rstd is None:
         mean, rstd = (_empty(x.shape[:-1], torch.float32, dev, stream) for _ in range(2))
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        if t is not None:
-            _check_dense(name, t, torch.float32, (x.shape[-1],), dev)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is not None:
-            _check_dense(name, t, torch.float32, x.shape[:-1], dev)
+    if gamma is not None:
+        _check_dense("gamma", gamma, torch.float32, x.shape[-1:], dev)
+    if beta is not None:
+        _check_dense("beta", beta, torch.float32, x.shape[-1:], dev)
+    if mean is not None:
+        _check_dense("mean", mean, torch.float32, x.shape[:-1], dev)
+    if rstd is not None:
+        _check_dense("rstd", rstd, torch.float32, x.shape[:-1], dev)
     _call(lib.ress_layer_norm, dev, stream, shape, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean),
           _ptr(rstd))
     return dict(y=out, mean=mean, rstd=rstd)
@@ -248,18 +265,16 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     qs = ks = qo = ko = (0, 0)
     if q is not None:
         H = q.shape[0]
-        _check("q", q, first.dtype, (H, N, D), dev)
+        qs = _strides("q", q, first.dtype, (H, N, D), dev)
         q_out = _empty(q.shape, q.dtype, dev, stream) if q_out is None else q_out
-        _check("q_out", q_out, q.dtype, q.shape, dev)
-        qs, qo = _strides(q), _strides(q_out)
+        qo = _strides("q_out", q_out, q.dtype, q.shape, dev)
     else:
         q_out = None
     if k is not None:
         H_kv = k.shape[0]
-        _check("k", k, first.dtype, (H_kv, N, D), dev)
+        ks = _strides("k", k, first.dtype, (H_kv, N, D), dev)
         k_out = _empty(k.shape, k.dtype, dev, stream) if k_out is None else k_out
-        _check("k_out", k_out, k.dtype, k.shape, dev)
-        ks, ko = _strides(k), _strides(k_out)
+        ko = _strides("k_out", k_out, k.dtype, k.shape, dev)
     else:
         k_out = None
     shape = _ROPE(H, H_kv, N, D, axes, *dims, *(0,) * (4 - axes), ROPE_LAYOUTS[layout], bool(inverse), _DTYPES[first.dtype],
@@ -280,15 +295,13 @@ def _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal,
     return _WINDOW(H, H_kv, n_q, n_k, D, q_offset, _int32(frame), _int32(window), _int32(n_sink), bool(causal), *strides)
 
 
-def _check_window(q, k, v):
+def _qkv_strides(q, k, v):
     dev = _device("q", q)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t.dim() != 3:
-            raise ValueError(f"{name} must be [heads][tokens][channels]")
-    _check("q", q, torch.bfloat16, q.shape, dev)
-    _check("k", k, torch.bfloat16, (k.shape[0], k.shape[1], q.shape[2]), dev)
-    _check("v", v, torch.bfloat16, k.shape, dev)
-    return dev
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [heads][tokens][channels]")
+    return dev, (_strides("q", q, torch.bfloat16, q.shape, dev)
+                 + _strides("k", k, torch.bfloat16, (k.shape[0], k.shape[1], q.shape[2]), dev)
+                 + _strides("v", v, torch.bfloat16, k.shape, dev))
 
 
 def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q_offset: int = 0, causal: bool = True,
@@ -296,17 +309,16 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
     """Attention over a sliding window of frames and the first n_sink tokens (see include/ress_layer.h). q: bf16
     [H][n_q][64] at positions q_offset ..; k, v: bf16 [H_kv][n_k][64]; any strides with contiguous channels.
     Returns o (bf16, as q) and, with want_lse or a given buffer, lse (float32 [H][n_q])."""
-    dev = _check_window(q, k, v)
+    dev, st = _qkv_strides(q, k, v)
     H, n_q, D = q.shape
     if out is None:
         out = _empty(q.shape, torch.bfloat16, dev, stream)
-    _check("out", out, torch.bfloat16, q.shape, dev)
+    st += _strides("out", out, torch.bfloat16, q.shape, dev)
     if lse is None and want_lse:
         lse = _empty((H, n_q), torch.float32, dev, stream)
     if lse is not None:
         _check_dense("lse", lse, torch.float32, (H, n_q), dev)
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal,
-                          _strides(q) + _strides(k) + _strides(v) + _strides(out))
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, st)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), scale, _ptr(out), _ptr(lse), ws, ws_bytes)
@@ -330,20 +342,19 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
                          stream=None) -> dict:
     """Gradients of ress_window_attn (see include/ress_layer.h): o and lse as it made them, the other arguments
     as it was given. Returns dq, dk, dv (bf16, as q, k, v)."""
-    dev = _check_window(q, k, v)
+    dev, st = _qkv_strides(q, k, v)
     H, n_q, D = q.shape
-    _check("o", o, torch.bfloat16, q.shape, dev)
-    _check("d_o", d_o, torch.bfloat16, q.shape, dev)
+    st += _strides("o", o, torch.bfloat16, q.shape, dev)
+    gst = _strides("d_o", d_o, torch.bfloat16, q.shape, dev)
     _check_dense("lse", lse, torch.float32, (H, n_q), dev)
     grads = []
     for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         t = _empty(like.shape, torch.bfloat16, dev, stream) if t is None else t
-        _check(name, t, torch.bfloat16, like.shape, dev)
+        gst += _strides(name, t, torch.bfloat16, like.shape, dev)
         grads.append(t)
     dq, dk, dv = grads
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal,
-                          _strides(q) + _strides(k) + _strides(v) + _strides(o))
-    g = _GRADS(*_strides(d_o), *_strides(dq), *_strides(dk), *_strides(dv))
+    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, st)
+    g = _GRADS(*gst)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), scale,

@@ -32,6 +32,10 @@ SHAPES = [
     (2, 2, 190, 190, 0, 1374, 4, 1374, True),  # one frame
     (2, 2, 400, 400, 0, 1, 2 ** 31 - 1, 2 ** 31 - 1, True),
     (2, 2, 300, 300, 0, 2 ** 31 - 1, 1, 0, False),
+    (2, 1, 130, 130, 0, 2 ** 31 - 1, 2 ** 31 - 1, 0, False),
+    (2, 1, 0, 150, 0, 1, 10, 3, True),         # no queries
+    (6, 2, 1100, 1100, 0, 1, 30, 5, False),    # the sinks' queries cut into slices, the others' not
+    (1, 1, 2500, 2500, 0, 1, 2500, 0, True),   # every block's queries cut, keys split over workgroups
     (8, 1, 150, 150, 0, 1, 50, 1, True),
     (2, 2, 1400, 1400, 0, 300, 2, 300, True),
     (2, 2, 700, 700, 0, 1, 90, 650, True),     # sinks beyond most windows
