@@ -61,7 +61,7 @@ struct WindowParams {
     bool causal;
     int n_qb, n_kb;  // blocks of 128 / groups queries, of 128 keys
     int splits;      // workgroups that share a block's keys (forward)
-    float scale, scale_log2;
+    float scale, scale_log2;  // of dq and dk; of the logits, in base 2
     ress_strides qs, ks, vs, os;
     const uint16_t *q, *k, *v;
     uint16_t *o;

@@ -3,14 +3,15 @@
 // in one workgroup's registers, in one order, with no atomics: 7 products of 64 channels
 // per visible pair instead of 5.
 //
-//   delta_kernel  per query -sum_d d_o o, and lse in base 2;
-//   dq_kernel     128 queries a workgroup, walking over the key tiles they see:
+//   dq_kernel     128 queries a workgroup, walking over the key tiles they see, with
+//                 delta = sum_d d_o o of its rows:
 //                 S^T = K Q^T, dP^T = V dO^T - delta, dQ^T += K^T dS^T. delta off by e leaves
 //                 -e (sum P k) in dQ, which for keys with a common part outweighs dQ itself,
 //                 and o is rounded to bf16, as dS is for its product; so sum dS = e (0 for the
 //                 true delta and unrounded dS) is summed from the rounded values as well,
 //                 B^T += K^T P^T beside it, and dQ takes back e B (without it dq was 1-1.5% off
-//                 in norm where keys share a mean). The corrected delta goes to the next kernel;
+//                 in norm where keys share a mean). The corrected delta and lse in base 2 go to the
+//                 next kernel;
 //   dkv_kernel    128 keys a workgroup, walking over the tiles of queries that see them,
 //                 query head after query head of those that share the keys:
 //                 S = Q K^T, dP = dO V^T - delta, dV^T += dO^T P, dK^T += Q^T dS. Keys of
@@ -28,27 +29,6 @@ namespace {
 using namespace tiles;
 
 constexpr float kLog2e = 1.4426950408889634f;
-
-// 8 lanes a query.
-__global__ void __launch_bounds__(256) delta_kernel(const WindowBwdParams b)
-{
-    const WindowParams &p = b.w;
-    const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
-    if (row >= (int64_t)p.H * p.n_q) return;
-    const int h = (int)(row / p.n_q), t = (int)(row - (int64_t)h * p.n_q), l = threadIdx.x & 7;
-    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(b.d_o + h * b.dos.head + (int64_t)t * b.dos.token + l * 8);
-    const bf16x8 y = *reinterpret_cast<const bf16x8 *>(p.o + h * p.os.head + (int64_t)t * p.os.token + l * 8);
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)y[e], s);
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
-    if (l == 0) {
-        const float lse = p.lse[row];
-        b.ndelta[row] = -s;
-        b.lse2[row] = lse == -INFINITY ? INFINITY : lse * kLog2e;  // (a query that sees nothing: P = 0)
-    }
-}
 
 template <int G>
 __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
@@ -100,7 +80,19 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
             df[kk] = *reinterpret_cast<const bf16x8 *>(d + kk * 16);
         }
     }
-    const float lse2 = b.lse2[(int64_t)h * p.n_q + tq], nd = b.ndelta[(int64_t)h * p.n_q + tq];
+    float nd = 0.f;
+    {
+        const uint16_t *o = p.o + h * p.os.head + (int64_t)tq * p.os.token + hh * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8 *>(o + kk * 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) nd = fmaf(-(float)df[kk][e], (float)x[e], nd);
+        }
+        nd += __shfl_xor(nd, 32);
+    }
+    // (A query that sees nothing: P = 0.)
+    const float lse = p.lse[(int64_t)h * p.n_q + tq], lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
     const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
     const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
@@ -212,7 +204,10 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[dh][v] = fmaf(-off, mean[dh][v], acc[dh][v]);
     if (t > t_last) return;
-    if (hh == 0) b.ndelta[(int64_t)h * p.n_q + t] = nd - off;
+    if (hh == 0) {
+        b.ndelta[(int64_t)h * p.n_q + t] = nd - off;
+        b.lse2[(int64_t)h * p.n_q + t] = lse2;
+    }
     store_row(b.dq + h * b.dqs.head + (int64_t)t * b.dqs.token, acc, p.scale, hh);
 }
 
@@ -445,9 +440,6 @@ hipError_t launch_window_bwd(const WindowBwdParams &b, int groups, hipStream_t s
 {
     const WindowParams &p = b.w;
     if (p.n_q > 0) {
-        const int64_t rows = (int64_t)p.H * p.n_q;
-        hipLaunchKernelGGL(delta_kernel, dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, s, b);
-        if (hipError_t e = hipGetLastError()) return e;
         const dim3 grid(8u * (unsigned)((p.H * p.n_qb + 7) / 8)), block(256);
         if (groups == 1)
             hipLaunchKernelGGL(dq_kernel<1>, grid, block, 0, s, b);

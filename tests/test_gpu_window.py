@@ -211,6 +211,21 @@ def test_backward(ress, shape):
     assert all(torch.equal(again[n], g[n]) for n in g)
 
 
+@pytest.mark.parametrize("shape", [(4, 2, 1, 1, 0, 1, 7, 1, False), (3, 1, 200, 200, 0, 1, 1, 0, True),
+                                   (2, 2, 150, 150, 0, 1, 1, 0, False), (4, 4, 90, 1, 0, 50, 1, 0, True)])
+def test_one_key_has_no_gradient_of_its_logit(ress, shape):
+    """A softmax over one key is 1: dq and dk are zero exactly, dv is d_o of the queries that see the key."""
+    H, H_kv, n_q, n_k = shape[:4]
+    q, k, v, do = _inputs(77, H, H_kv, n_q, n_k)
+    kw = _kw(*shape[4:])
+    f = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    g = ress.ress_window_attn_bwd(do, q, k, v, f["o"], f["lse"], **kw)
+    vis = R.visible(n_q, n_k, *shape[4:], device="cuda")
+    assert not g["dq"].any() and not g["dk"].any()
+    _, _, dv, _, _, bv = R.window_bwd(do, q, k, v, vis)
+    R.within(g["dv"], dv, bv, "dv")
+
+
 def test_backward_keeps_small_gradients_beside_a_common_key(ress):
     """Keys with a mean far above their spread: dq is what is left of sums that nearly cancel, and stays within its bound
     (delta taken from the rounded o alone would leave that mean times the rounding in it)."""
