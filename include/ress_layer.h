@@ -51,7 +51,7 @@ typedef struct {
     int y_dtype;      /* of y and dy */
     int64_t x_stride; /* between rows of x and dx, >= width */
     int64_t y_stride; /* between rows of y and dy, >= width */
-    double eps;       /* added to the variance, > 0 */
+    double eps;       /* added to the variance, > 0; not used by the backward pass */
 } ress_norm_shape;
 
 /* y = (x - mean) rstd gamma + beta over the channels of every row, with
@@ -144,6 +144,11 @@ typedef struct {
     int causal;
     ress_strides q, k, v, o; /* multiples of 8; a token stride of at most 2^22 */
 } ress_window_shape;
+
+/* Blocks: a block of 128 queries (keys, in the backward pass) is computed together. Keys
+ * that none of its queries sees (queries that see none of its keys) are not read
+ * and may hold anything; a NaN or infinity in one that some of them see may also
+ * reach the others of the block. */
 
 /* Bytes of device workspace ress_window_attn needs (0 but for few queries over long
  * windows, whose keys are split over workgroups; strides do not matter). */

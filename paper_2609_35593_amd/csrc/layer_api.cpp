@@ -38,14 +38,14 @@ bool same(const ress_strides &a, const ress_strides &b) { return a.head == b.hea
 
 // ---------------------------------------------------------------- layer norm
 
-int check_norm(const ress_norm_shape *s)
+int check_norm(const ress_norm_shape *s, bool forward)
 {
     if (!s) return RESS_E_INVALID_ARG;
     if (s->rows < 0 || s->width < 1 || !dtype_ok(s->x_dtype) || !dtype_ok(s->y_dtype)) return RESS_E_INVALID_ARG;
     if (s->rows > kMaxRows || s->width > RESS_MAX_NORM_WIDTH) return RESS_E_UNSUPPORTED;
     if (s->x_stride < s->width || s->y_stride < s->width || s->x_stride > kMaxRows || s->y_stride > kMaxRows)
         return RESS_E_INVALID_ARG;
-    if (!((float)s->eps > 0.f) || !isfinite((float)s->eps)) return RESS_E_INVALID_ARG;
+    if (forward && (!((float)s->eps > 0.f) || !isfinite((float)s->eps))) return RESS_E_INVALID_ARG;
     return RESS_OK;
 }
 
@@ -154,7 +154,7 @@ extern "C" {
 int ress_layer_norm(const ress_norm_shape *shape, const void *x, const float *gamma, const float *beta, void *y,
                     float *mean, float *rstd, hipStream_t stream)
 {
-    int st = check_norm(shape);
+    int st = check_norm(shape, true);
     if (st != RESS_OK) return st;
     if ((mean == nullptr) != (rstd == nullptr)) return RESS_E_INVALID_ARG;
     if (shape->rows == 0) return RESS_OK;
@@ -183,7 +183,7 @@ int ress_layer_norm(const ress_norm_shape *shape, const void *x, const float *ga
 
 int ress_layer_norm_bwd_workspace_size(const ress_norm_shape *shape, size_t *bytes)
 {
-    int st = check_norm(shape);
+    int st = check_norm(shape, false);
     if (st != RESS_OK) return st;
     if (!bytes) return RESS_E_INVALID_ARG;
     *bytes = norm_workspace(shape);
@@ -194,7 +194,7 @@ int ress_layer_norm_bwd(const ress_norm_shape *shape, const void *dy, const void
                         const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *workspace,
                         size_t ws_bytes, hipStream_t stream)
 {
-    int st = check_norm(shape);
+    int st = check_norm(shape, false);
     if (st != RESS_OK) return st;
     const bool sums = dgamma || dbeta;
     if (shape->rows == 0 && !sums) return RESS_OK;

@@ -66,11 +66,12 @@ struct Loader {
     }
     static __device__ __forceinline__ unsigned int source(int r0, int l) { return (unsigned int)(((l & 7) ^ swz(r0)) << 4); }
     // Rows row0 .. row0 + 63 into `dst`; rows outside [lo, hi) (hi > lo) repeat the nearest
-    // one inside and are not read.
-    __device__ __forceinline__ void operator()(int row0, int lo, int hi, unsigned char *dst) const
+    // one inside, rows in [gap, end) (end < hi, inside the tile, or gap >= end) row `end`; none
+    // of them is read.
+    __device__ __forceinline__ void operator()(int row0, int lo, int hi, int gap, int end, unsigned char *dst) const
     {
         const unsigned int step = (unsigned int)(2 * stride);  // bytes
-        if (row0 >= lo && row0 + kTile <= hi) {
+        if (row0 >= lo && row0 + kTile <= hi && gap >= end) {
             const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
                 const_cast<uint16_t *>(base + (int64_t)row0 * stride), 0, (int)((kTile - 1) * step + 128u), 0x00020000);
 #pragma unroll
@@ -92,7 +93,8 @@ struct Loader {
                                                   (int)((unsigned int)(last - first) * step + 128u), 0x00020000);
 #pragma unroll
             for (int u = 0; u < 8 / WAVES; ++u) {
-                const int row = min(max(row0 + r0 + 8 * WAVES * u, first), last) - first;
+                int row = min(max(row0 + r0 + 8 * WAVES * u, first), last);
+                row = (row >= gap && row < end ? end : row) - first;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(dst + (u * WAVES + wave) * 1024), 16,
                                                          (unsigned int)row * step + (WAVES == 1 && u % 2 ? coff ^ 32u : coff),
                                                          0, 0, 0);

@@ -101,14 +101,15 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
     const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
     const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
-    // Keys outside every row's sight are not read: [0, sk) and [lo, hi) of the workgroup.
+    // Keys outside every row's sight are not read: only [0, sk) and [lo, hi) of the workgroup are.
     auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
         if (n * G + grp >= tiles_n) return;
         const int key0 = tile_key(n);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
-        load_k(key0, lo, hi, kd);
-        load_v(key0, lo, hi, vd);
+        const int end = sinks && window ? s_first.lo : 0;  // a tile of both: what lies between them
+        load_k(key0, lo, hi, s_last.sk, end, kd);
+        load_v(key0, lo, hi, s_last.sk, end, vd);
     };
 
     const float c = p.scale_log2;

@@ -101,8 +101,9 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
         const int key0 = tile_key(n);
         const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
-        load_k(key0, lo, hi, kd);
-        load_v(key0, lo, hi, vd);
+        const int end = sinks && window ? s_first.lo : 0;  // a tile of both: what lies between them
+        load_k(key0, lo, hi, s_last.sk, end, kd);
+        load_v(key0, lo, hi, s_last.sk, end, vd);
     };
     const float c = p.scale_log2;
     f32x16 acc[2], mean[2];  // sum dS k, sum P k
@@ -285,14 +286,16 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
     auto fetch = [&](unsigned char *qd, unsigned char *dd, float (&rows)[2][kTile]) __attribute__((always_inline)) {
         load_q.base = p.q + fh * p.qs.head;
         load_d.base = b.d_o + fh * b.dos.head;
-        load_q(ft, 0, p.n_q, qd);
-        load_d(ft, 0, p.n_q, dd);
+        // (Queries that see none of the keys are not read.)
+        load_q(ft, q_lo, q_hi, 0, 0, qd);
+        load_d(ft, q_lo, q_hi, 0, 0, dd);
         if (wave < 2) {
-            const float *src = (wave == 0 ? b.lse2 : b.ndelta) + (int64_t)fh * p.n_q + ft;
-            const int last = min(kTile, p.n_q - ft) - 1;
+            const int t_a = max(ft, q_lo), last = min(ft + kTile, q_hi) - 1 - t_a;
+            const float *src = (wave == 0 ? b.lse2 : b.ndelta) + (int64_t)fh * p.n_q + t_a;
             const __amdgpu_buffer_rsrc_t rs =
                 __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(src), 0, 4 * (last + 1), 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)rows[wave], 4, 4 * min(lane, last), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)rows[wave], 4, 4 * min(max(lane + ft - t_a, 0), last), 0,
+                                                     0, 0);
         }
         ft += kTile;
         if (ft == t_end) {

@@ -321,7 +321,8 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
     shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, st)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), scale, _ptr(out), _ptr(lse), ws, ws_bytes)
+    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), float(scale), _ptr(out), _ptr(lse), ws,
+          ws_bytes)
     return dict(o=out, lse=lse)
 
 
@@ -357,8 +358,8 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
     g = _GRADS(*gst)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), scale,
-          _ptr(dq), _ptr(dk), _ptr(dv), ws, ws_bytes)
+    _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+          float(scale), _ptr(dq), _ptr(dk), _ptr(dv), ws, ws_bytes)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
@@ -400,5 +401,6 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
                     v_h, v_t, o_b, o_h)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_decode_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), scale, _ptr(out), ws, ws_bytes)
+    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), float(scale), _ptr(out), ws,
+          ws_bytes)
     return out

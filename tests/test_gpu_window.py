@@ -119,6 +119,17 @@ def test_unseen_keys_may_hold_anything(ress):
         t[:, 900:950] = float("inf")
         t[:, 950:] = float("nan")
     assert torch.equal(ress.ress_window_attn(q, k, v, **kw)["o"], ref)
+    # ... also where sinks and window share a tile of 64 keys: the block sees [0, 5) and [40, 199).
+    q, k, v, do = _inputs(6, 2, 2, 60, 300)
+    kw = _kw(139, 1, 100, 5, True)
+    ref = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    gref = ress.ress_window_attn_bwd(do, q, k, v, ref["o"], ref["lse"], **kw)
+    for t in (k, v):
+        t[:, 5:40] = float("nan")
+        t[:, 199:] = float("inf")
+    got = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    grad = ress.ress_window_attn_bwd(do, q, k, v, got["o"], got["lse"], **kw)
+    assert torch.equal(got["o"], ref["o"]) and torch.equal(got["lse"], ref["lse"]) and torch.equal(grad["dq"], gref["dq"])
     # A NaN key inside only spoils the queries that see it.
     q, k, v, _ = _inputs(6, 1, 1, 300, 300)
     kw = _kw(0, 100, 1, 0, True)
@@ -126,6 +137,21 @@ def test_unseen_keys_may_hold_anything(ress):
     k[:, 150] = float("nan")
     o = ress.ress_window_attn(q, k, v, **kw)["o"]
     assert torch.equal(o[:, :100], ref[:, :100]) and torch.equal(o[:, 200:], ref[:, 200:]) and bool(o[:, 100:200].isnan().all())
+
+
+def test_unseen_queries_may_hold_anything(ress):
+    """Queries that see none of a block of 128 keys have no part in the block's gradients, whatever they and their
+    gradients hold: keys 0 .. 127 are seen by queries 0 .. 146 alone."""
+    q, k, v, do = _inputs(13, 2, 1, 500, 500)
+    kw = _kw(0, 1, 20, 0, True)
+    f = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    ref = ress.ress_window_attn_bwd(do, q, k, v, f["o"], f["lse"], **kw)
+    q[:, 147:] = float("nan")
+    do[:, 147:] = float("inf")
+    f = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    got = ress.ress_window_attn_bwd(do, q, k, v, f["o"], f["lse"], **kw)
+    assert torch.equal(got["dk"][:, :128], ref["dk"][:, :128]) and torch.equal(got["dv"][:, :128], ref["dv"][:, :128])
+    assert torch.equal(got["dq"][:, :128], ref["dq"][:, :128])
 
 
 def test_dense_window_matches_dense_attention(ress):
