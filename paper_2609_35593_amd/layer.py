@@ -150,28 +150,22 @@ def _strides(name, t, dtype, shape, device):
 # ---------------------------------------------------------------- layer norm
 
 
-def _norm_rows(t):
-    """Rows and their stride: [rows][width] with any row stride, or a contiguous tensor of any rank."""
+def _norm_view(name, t, like):
+    """Rows, their stride and the type of [rows][width] with any row stride, or of a contiguous tensor of any rank; of
+    `like`'s shape and device where that is given."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None or (like is not None and (t.shape != like.shape or t.device != like.device)):
+        raise ValueError(f"{name} must be a bfloat16 or float32 CUDA tensor"
+                         + ("" if like is None else f" of shape {tuple(like.shape)} on {like.device}"))
     if t.dim() == 2:
         rows, width = t.shape
         stride, channel = t.stride()
         if channel != 1 and width > 1:
-            raise ValueError("a row's channels must be contiguous")
-        return rows, stride if rows > 1 else width
+            raise ValueError(f"{name}: a row's channels must be contiguous")
+        return rows, stride if rows > 1 else width, dtype
     if t.dim() == 0 or not t.is_contiguous():
-        raise ValueError("tensors of other ranks than [rows][width] must be contiguous")
-    return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1]
-
-
-def _norm_shape(x, y, eps):
-    rows, xs = _norm_rows(x)
-    return _NORM(rows, x.shape[-1], _DTYPES[x.dtype], _DTYPES[y.dtype], xs, _norm_rows(y)[1], eps)
-
-
-def _norm_check(name, t, like):
-    if t.dtype not in _DTYPES or (like is not None and (t.shape != like.shape or t.device != like.device)):
-        raise ValueError(f"{name} must be a bfloat16 or float32 CUDA tensor"
-                         + ("" if like is None else f" of shape {tuple(like.shape)} on {like.device}"))
+        raise ValueError(f"{name}: tensors of other ranks than [rows][width] must be contiguous")
+    return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1], dtype
 
 
 def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, out_dtype=torch.bfloat16, mean=None,
@@ -181,11 +175,11 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     out_dtype when it is made here. Returns y and, with want_stats or given buffers, mean and rstd
     (float32, one per row) for ress_layer_norm_bwd."""
     dev = _device("x", x)
-    _norm_check("x", x, None)
+    rows, xs, xt = _norm_view("x", x, None)
     if out is None:
         out = _empty(x.shape, out_dtype, dev, stream)
-    _norm_check("out", out, x)
-    shape = _norm_shape(x, out, eps)
+    _, ys, yt = _norm_view("out", out, x)
+    shape = _NORM(rows, x.shape[-1], xt, yt, xs, ys, eps)
     if want_stats and mean is None and rstd is None:
         mean, rstd = (_empty(x.shape[:-1], torch.float32, dev, stream) for _ in range(2))
     if gamma is not None:
@@ -211,17 +205,17 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     """Gradients of ress_layer_norm (see include/ress_layer.h). dy: of y's type; x, mean, rstd: as given to
     and made by the forward pass. Returns dx (of x's type) and, with want_weights, dgamma and dbeta
     (float32 [width])."""
-    dev, width = _device("x", x), x.shape[-1]
-    _norm_check("x", x, None)
-    _norm_check("dy", dy, x)
+    dev = _device("x", x)
+    rows, xs, xt = _norm_view("x", x, None)
+    _, ys, yt = _norm_view("dy", dy, x)
+    width = x.shape[-1]
     if dx is None:
         dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev)
         if stream is not None:
             dx.record_stream(_as_stream(stream, dev))
-    _norm_check("dx", dx, x)
-    shape = _norm_shape(x, dy, 1.0)
-    if dx.dtype != x.dtype or _norm_rows(dx) != _norm_rows(x):
+    if _norm_view("dx", dx, x)[1:] != (xs, xt):
         raise ValueError("dx must have x's type and row stride")
+    shape = _NORM(rows, width, xt, yt, xs, ys, 1.0)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _check_dense(name, t, torch.float32, x.shape[:-1], dev)
     if gamma is not None:
