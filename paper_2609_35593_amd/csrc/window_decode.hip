@@ -5,7 +5,7 @@
 // value's 64 channels, a wave 8 keys at a time, and the up to R query heads that share a
 // K/V head are formed from one read. The visible keys, sinks and window, are numbered
 // through (j -> key), so no work goes into masked ones and nothing outside them is read.
-// They are cut over `splits` workgroups of 4 waves, a run of turns of 32 keys each, the next
+// They are cut over `splits` workgroups of 4 or 8 waves, a run of turns of 32 keys each, the next
 // turn's loads under way; every 8 lanes keep an online softmax of their own, joined in a
 // fixed order in the wave, the workgroup, and for more than one split by join_kernel.
 #include "layer_internal.h"
@@ -16,6 +16,7 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 typedef unsigned int u32x4 __attribute__((__vector_size__(16)));
 
+constexpr int kMaxSplits = 32;
 constexpr int kPart = 66;  // floats of a partial result: reference, sum, 64 channels
 
 __device__ __forceinline__ float lo_f(unsigned int x) { return __builtin_bit_cast(float, x << 16); }
@@ -61,10 +62,15 @@ __device__ __forceinline__ Visible visible(const DecodeParams &p, int b)
     return v;
 }
 
+// Waves of a workgroup: one head's lanes leave registers for twice the waves of four heads' (us
+// with 4 / 8: 16 heads of 6,870 keys, one a K/V head, 10.5 / 9.3; 24 streams, four a K/V head, 27 / 34).
+constexpr int waves_of(int heads) { return heads == 1 ? 8 : 4; }
+
 template <int R>
-__global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
+__global__ void __launch_bounds__(64 * waves_of(R)) decode_kernel(const DecodeParams p)
 {
-    __shared__ float lds[4][R][kPart];
+    constexpr int kWaves = waves_of(R);
+    __shared__ float lds[kWaves][R][kPart];
     const int split = blockIdx.x, b = blockIdx.z;
     const int tiles = (p.group + R - 1) / R;
     const int hk = blockIdx.y / tiles, h0 = hk * p.group + (blockIdx.y % tiles) * R;
@@ -73,8 +79,8 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     const Visible vis = visible(p, b);
 
     // Whole turns of 32 keys, evenly over the splits' waves.
-    const int turns = (vis.n + 31) / 32, waves = p.splits * 4, each = (turns + waves - 1) / waves;
-    const int first = (split * 4 + wave) * each, last = min(first + each, turns);
+    const int turns = (vis.n + 31) / 32, waves = p.splits * kWaves, each = (turns + waves - 1) / waves;
+    const int first = (split * kWaves + wave) * each, last = min(first + each, turns);
 
     u32x4 q[R];
 #pragma unroll
@@ -162,12 +168,12 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
         }
     }
     __syncthreads();
-    for (int r = wave; r < heads; r += 4) {
+    for (int r = wave; r < heads; r += kWaves) {
         float top = kNone, sum = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds[w][r][0]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds[w][r][0]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
             const float a = __builtin_amdgcn_exp2f(lds[w][r][0] - top);
             sum = fmaf(lds[w][r][1], a, sum);
             o = fmaf(lds[w][r][2 + lane], a, o);
@@ -184,7 +190,7 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecodeParams p)
     }
 }
 
-// A wave a query head, a channel a lane: its at most 64 splits in order, their weights one a
+// A wave a query head, a channel a lane: its at most 32 splits in order, their weights one a
 // lane first.
 __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
 {
@@ -192,12 +198,11 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
     if (row >= (int64_t)p.B * p.H) return;
     const int lane = threadIdx.x & 63;
     const float *d = p.part + row * p.splits * kPart;
-    // (The first parts are on their way with their references: one round trip for most calls.)
-    constexpr int AHEAD = 16;
-    float m = kNone, sum = 0.f, o = 0.f, x[AHEAD];
+    // (All parts are on their way with their references: one round trip.)
+    float m = kNone, sum = 0.f, o = 0.f, x[kMaxSplits];
     if (lane < p.splits) m = d[lane * kPart], sum = d[lane * kPart + 1];
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s) x[s] = d[min(s, p.splits - 1) * kPart + 2 + lane];
+    for (int s = 0; s < kMaxSplits; ++s) x[s] = d[min(s, p.splits - 1) * kPart + 2 + lane];
     float top = m;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) top = fmaxf(top, __shfl_xor(top, e));
@@ -207,10 +212,8 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
     auto weight = [&](int s) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s)); };
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
+    for (int s = 0; s < kMaxSplits; ++s)
         if (s < p.splits) o = fmaf(weight(s), x[s], o);
-#pragma unroll 8
-    for (int s = AHEAD; s < p.splits; ++s) o = fmaf(weight(s), d[s * kPart + 2 + lane], o);
     const int64_t b = row / p.H, h = row - b * p.H;
     p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)(sum == 0.f ? 0.f : o / sum));
 }
@@ -219,7 +222,7 @@ template <int R>
 hipError_t go(const DecodeParams &p, hipStream_t s)
 {
     const dim3 grid((unsigned)p.splits, (unsigned)(p.H_kv * ((p.group + R - 1) / R)), (unsigned)p.B);
-    hipLaunchKernelGGL(decode_kernel<R>, grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(decode_kernel<R>, grid, dim3(64 * waves_of(R)), 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.splits > 1) {
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.B * p.H + 3) / 4)), dim3(256), 0, s, p);
@@ -230,19 +233,20 @@ hipError_t go(const DecodeParams &p, hipStream_t s)
 
 }  // namespace
 
-// Workgroups per sequence and head: enough for 4 a CU, but none with less than 4 turns for
-// each of its 4 waves (us with 256 / 512 keys at least, the join counted: 16 heads of 6,870 keys
-// 13.1 / 10.3, 8 x 4 of 4,000 23 / 18, 4 x 8 of 300 7.5 / 5.3, 4 of 1,000 10.6 / 12.0; 768 heads
-// in two halves each 81, whole 74).
+// Workgroups per sequence and head: enough for 4 a CU, but none with less than 256 keys, and one
+// up to 512 (us with at least 256 / 512 / 1,024 keys, the join counted: 4 heads of 900 keys for 16
+// 10.1 / 12.2 / 13.5, of 8,000 10.6 / 12.6 / 17.2; 16 heads of 6,870 9.6 / 9.3 / 10.8; 8 streams
+// of 4 heads of 4,000 19.6 / 18.1 / 20.9; 32 heads of 300 7.4 / 5.1 / 5.2; 768 heads of 2,000 in
+// halves 81, whole 74).
 int decode_splits(const ress_decode_shape *s)
 {
     if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
     const int64_t seen = window_tokens(s->frame, s->window) + s->n_sink;
     const int64_t keys = seen < s->capacity ? seen : s->capacity;
     const int64_t heads = (int64_t)s->B * s->H_kv * ((s->H / s->H_kv + 3) / 4);
-    const int64_t want = 1024 / heads, most = (keys + 511) / 512;
+    const int64_t want = 1024 / heads, most = keys <= 512 ? 1 : (keys + 255) / 256;
     const int64_t n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    return (int)(n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n);
 }
 
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s)
