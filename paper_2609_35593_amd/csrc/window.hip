@@ -30,6 +30,7 @@ using namespace tiles;
 
 constexpr float kSumLimit = 0x1p50f;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxSplits = 32;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // exp2(a - top) for a part that holds mass, 0 for one that holds none.
@@ -280,13 +281,20 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
     if (LSE && hh == 0) p.lse[(int64_t)h * p.n_q + t] = sum == 0.f ? -INFINITY : ref * kLn2 + logf(sum);
 }
 
-// A wave a row (a channel a lane): its at most 32 parts, their weights one a lane.
+// A wave a row, a channel a lane: its parts in order, their weights one a lane first. (All of them
+// are on their way with their references: one round trip.)
 __global__ void __launch_bounds__(256) join_kernel(const WindowParams p)
 {
     const int64_t rows = (int64_t)p.H * p.n_q, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= rows) return;
     const int lane = threadIdx.x & 63;
+    float x[kMaxSplits];
     const float2 r = lane < p.splits ? p.part_row[lane * rows + row] : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int s0 = 0; s0 < kMaxSplits; s0 += 4)
+        if (s0 < p.splits)
+#pragma unroll
+            for (int s = s0; s < s0 + 4; ++s) x[s] = p.part[(min(s, p.splits - 1) * rows + row) * 64 + lane];
     float top = r.y == 0.f ? -INFINITY : r.x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -294,11 +302,10 @@ __global__ void __launch_bounds__(256) join_kernel(const WindowParams p)
     float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
-#pragma unroll 8
-    for (int s = 0; s < p.splits; ++s) {
-        const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s));
-        o = fmaf(ws, p.part[(s * rows + row) * 64 + lane], o);
-    }
+#pragma unroll
+    for (int s = 0; s < kMaxSplits; ++s)
+        if (s < p.splits)
+            o = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s)), x[s], o);
     const int64_t h = row / p.n_q, t = row - h * p.n_q;
     p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(o * inverse(sum));
     if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
@@ -344,7 +351,7 @@ WindowPlan window_plan(const ress_window_shape *s)
     if (plan.groups == 4 && n > 0) {
         int64_t want = 256 / n;
         if (want > tiles / 8) want = tiles / 8;
-        plan.splits = (int)(want < 1 ? 1 : want > 32 ? 32 : want);
+        plan.splits = (int)(want < 1 ? 1 : want > kMaxSplits ? kMaxSplits : want);
     }
     return plan;
 }

@@ -202,7 +202,10 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
     float m = kNone, sum = 0.f, o = 0.f, x[kMaxSplits];
     if (lane < p.splits) m = d[lane * kPart], sum = d[lane * kPart + 1];
 #pragma unroll
-    for (int s = 0; s < kMaxSplits; ++s) x[s] = d[min(s, p.splits - 1) * kPart + 2 + lane];
+    for (int s0 = 0; s0 < kMaxSplits; s0 += 4)
+        if (s0 < p.splits)
+#pragma unroll
+            for (int s = s0; s < s0 + 4; ++s) x[s] = d[min(s, p.splits - 1) * kPart + 2 + lane];
     float top = m;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) top = fmaxf(top, __shfl_xor(top, e));
