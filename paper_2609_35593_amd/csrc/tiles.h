@@ -156,20 +156,6 @@ __device__ __forceinline__ float add_up(const bf16x8 (&b)[2], float sum)
     return sum;
 }
 
-// One row (column l%32 of two transposed accumulators of 32 channels each) times `f`, to
-// bf16 global memory.
-__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[2], float f, int hh)
-{
-#pragma unroll
-    for (int dh = 0; dh < 2; ++dh)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const unsigned int lo = bf16_bits(acc[dh][g * 4 + 0] * f) | (bf16_bits(acc[dh][g * 4 + 1] * f) << 16);
-            const unsigned int hi = bf16_bits(acc[dh][g * 4 + 2] * f) | (bf16_bits(acc[dh][g * 4 + 3] * f) << 16);
-            *reinterpret_cast<uint2 *>(row + dh * 32 + g * 8 + hh * 4) = make_uint2(lo, hi);
-        }
-}
-
 // The keys that query position p sees: [lo, hi) and [0, sk).
 struct Seen {
     int lo, hi, sk;
@@ -185,6 +171,44 @@ __device__ __forceinline__ Seen seen_by(const WindowParams &p, int pos)
     s.lo = (int)min(max(lo, (int64_t)0), (int64_t)s.hi);
     s.sk = min(p.n_sink, p.causal ? s.hi : p.n_k);
     return s;
+}
+
+// Scores (keys or queries base .. base + 31, the lane's from 4 (l/32) on, which `lo` and `sk`
+// allow for) outside [lo, lo + span), and with `sinks` (wave-uniform) not below sk, become -inf.
+// One vector comparison and selection a score and condition: conditions joined as masks go
+// through the scalar unit and wait for it each time.
+__device__ __forceinline__ void hide(f32x16 &s, int base, int lo, unsigned int span, bool sinks, int sk)
+{
+    asm volatile("" ::: "memory");  // (a real branch around this: whole tiles skip it)
+    if (sinks) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = __builtin_amdgcn_readfirstlane(base + (v >> 2) * 8 + (v & 3));
+            float x = (unsigned int)(key - lo) < span ? s[v] : -INFINITY;
+            asm volatile("" : "+v"(x));
+            s[v] = key < sk ? s[v] : x;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = __builtin_amdgcn_readfirstlane(base + (v >> 2) * 8 + (v & 3));
+            s[v] = (unsigned int)(key - lo) < span ? s[v] : -INFINITY;
+        }
+    }
+}
+
+// One row (column l%32 of two transposed accumulators of 32 channels each) times `f`, to
+// bf16 global memory.
+__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[2], float f, int hh)
+{
+#pragma unroll
+    for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const unsigned int lo = bf16_bits(acc[dh][g * 4 + 0] * f) | (bf16_bits(acc[dh][g * 4 + 1] * f) << 16);
+            const unsigned int hi = bf16_bits(acc[dh][g * 4 + 2] * f) | (bf16_bits(acc[dh][g * 4 + 3] * f) << 16);
+            *reinterpret_cast<uint2 *>(row + dh * 32 + g * 8 + hh * 4) = make_uint2(lo, hi);
+        }
 }
 
 // The queries [lo, hi) that see key s (by their index, not their position).

@@ -128,15 +128,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
         for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
-        if (part) {
-            asm volatile("" ::: "memory");  // (a real branch: whole tiles skip the comparisons)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int key = __builtin_amdgcn_readfirstlane(key0 + u * 32 + (v >> 2) * 8 + (v & 3));
-                const bool in = (key >= sl.lo && key < sl.hi) || key < sl.sk;
-                s[v] = in ? s[v] : -INFINITY;
-            }
-        }
+        if (part) hide(s, key0 + u * 32, sl.lo, (unsigned int)(sl.hi - sl.lo), key0 < sb.sk, sl.sk);
     };
     // The row's largest logit in the tile.
     auto top = [&](bool part, const unsigned char *kt, int key0) __attribute__((always_inline)) {

@@ -21,6 +21,7 @@
 // In both a lane holds one column of the score tile (a query, a key), so P and dS, rounded
 // to bf16, are the next products' operands as they lie (tiles.h); -delta enters as the
 // initial value of the accumulator.
+#include <stdlib.h>
 #include "tiles.h"
 
 namespace ress {
@@ -122,15 +123,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
             for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(vt, u, kk), df[kk], d);
-            if (part) {
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int key = __builtin_amdgcn_readfirstlane(key0 + u * 32 + (v >> 2) * 8 + (v & 3));
-                    const bool in = (key >= sl.lo && key < sl.hi) || key < sl.sk;
-                    s[v] = in ? s[v] : -INFINITY;
-                }
-            }
+            if (part) hide(s, key0 + u * 32, sl.lo, (unsigned int)(sl.hi - sl.lo), key0 < sb.sk, sl.sk);
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
@@ -326,14 +319,7 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
             for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(qt, u, kk), kf[kk], s);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) d = mfma(rd.rows(dt, u, kk), vf[kk], d);
-            if (part) {
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int t = __builtin_amdgcn_readfirstlane(t0 + u * 32 + (v >> 2) * 8 + (v & 3));
-                    s[v] = t >= ql.lo && t < ql.hi ? s[v] : -INFINITY;
-                }
-            }
+            if (part) hide(s, t0 + u * 32, ql.lo, (unsigned int)(ql.hi - ql.lo), false, 0);
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -l[v]));
@@ -419,6 +405,7 @@ WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
 {
     WindowBwdPlan r = {window_plan(s).groups, 0, 1, 1, 0};
     const int64_t blocks = (s->n_k + 127) / 128;
+    if (getenv("BG")) r.groups = atoi(getenv("BG"));
     if (s->H_kv == 0 || blocks == 0) return r;
     const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k, group = s->H / s->H_kv;
     r.sink_blocks = (int)((sinks + 127) / 128);
@@ -431,7 +418,7 @@ WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
     // Lists of about a 1,024th of the work (the chip holds 512 workgroups), of 12 tiles at least:
     // shorter ones take more to join than they save (3,001 tokens, 12 heads, 5 sinks: lists of 6 /
     // 8 / 12 / 16 tiles 40.7 / 42.4 / 38.6 / 41.2 us with the join; uncut 232).
-    const int64_t goal = total / 1024 > 12 ? total / 1024 : 12;
+    const int64_t least = getenv("BT") ? atoi(getenv("BT")) : 12; const int64_t goal = total / 1024 > least ? total / 1024 : least;
     auto slices = [&](int64_t t) { return (int)(2 * t <= 3 * goal ? 1 : (t + goal - 1) / goal > 64 ? 64 : (t + goal - 1) / goal); };
     r.sink_slices = slices(t_sink);
     r.slices = slices(t_win);
