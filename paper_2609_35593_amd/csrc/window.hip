@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
     auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
         if (n * G + grp >= tiles_n) return;
         const int key0 = tile_key(n);
-        const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
+        const bool sinks = key0 < s_last.sk, window = s_first.lo < s_last.hi && key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
         const int end = sinks && window ? s_first.lo : 0;  // a tile of both: what lies between them
         load_k(key0, lo, hi, s_last.sk, end, kd);

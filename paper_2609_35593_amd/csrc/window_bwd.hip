@@ -1,6 +1,6 @@
 // Gradients of the windowed attention. The probabilities are formed again from the
 // logarithms of their sums, once for each of two kernels, so that every gradient is a sum
-// in one workgroup's registers, in one order, with no atomics: 7 products of 64 channels
+// in one workgroup's registers, in one order, with no atomics: 8 products of 64 channels
 // per visible pair instead of 5.
 //
 //   dq_kernel     128 queries a workgroup, walking over the key tiles they see, with
@@ -21,7 +21,6 @@
 // In both a lane holds one column of the score tile (a query, a key), so P and dS, rounded
 // to bf16, are the next products' operands as they lie (tiles.h); -delta enters as the
 // initial value of the accumulator.
-#include <stdlib.h>
 #include "tiles.h"
 
 namespace ress {
@@ -100,7 +99,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
     auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
         if (n * G + grp >= tiles_n) return;
         const int key0 = tile_key(n);
-        const bool sinks = key0 < s_last.sk, window = key0 + kTile > s_first.lo && key0 < s_last.hi;
+        const bool sinks = key0 < s_last.sk, window = s_first.lo < s_last.hi && key0 + kTile > s_first.lo && key0 < s_last.hi;
         const int lo = sinks ? 0 : s_first.lo, hi = window ? max(s_last.hi, s_last.sk) : s_last.sk;
         const int end = sinks && window ? s_first.lo : 0;  // a tile of both: what lies between them
         load_k(key0, lo, hi, s_last.sk, end, kd);

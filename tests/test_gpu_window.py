@@ -39,6 +39,7 @@ SHAPES = [
     (8, 1, 150, 150, 0, 1, 50, 1, True),
     (2, 2, 1400, 1400, 0, 300, 2, 300, True),
     (2, 2, 700, 700, 0, 1, 90, 650, True),     # sinks beyond most windows
+    (2, 2, 100, 100, 300, 1, 10, 80, True),    # the sinks only, keys behind them in their last tile
 ]
 
 
@@ -127,6 +128,16 @@ def test_unseen_keys_may_hold_anything(ress):
     for t in (k, v):
         t[:, 5:40] = float("nan")
         t[:, 199:] = float("inf")
+    got = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    grad = ress.ress_window_attn_bwd(do, q, k, v, got["o"], got["lse"], **kw)
+    assert torch.equal(got["o"], ref["o"]) and torch.equal(got["lse"], ref["lse"]) and torch.equal(grad["dq"], gref["dq"])
+    # ... and where every window lies behind the keys, and the sinks end inside the last tile.
+    q, k, v, do = _inputs(6, 2, 2, 60, 100)
+    kw = _kw(300, 1, 10, 80, True)
+    ref = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    gref = ress.ress_window_attn_bwd(do, q, k, v, ref["o"], ref["lse"], **kw)
+    for t in (k, v):
+        t[:, 80:] = float("nan")
     got = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
     grad = ress.ress_window_attn_bwd(do, q, k, v, got["o"], got["lse"], **kw)
     assert torch.equal(got["o"], ref["o"]) and torch.equal(got["lse"], ref["lse"]) and torch.equal(grad["dq"], gref["dq"])
