@@ -95,8 +95,9 @@ ress::WindowParams window_params(const ress_window_shape *s, float scale)
     p.n_q = s->n_q;
     p.n_k = s->n_k;
     p.q_offset = s->q_offset;
-    p.frame = ress::at_most_2_26(s->frame);
-    p.window = ress::at_most_2_26(s->window);
+    ress::sights(s->frame, s->window, p.frame, p.window);
+    p.frames = ress::divider(p.frame);
+    p.groups = ress::divider(p.group);
     p.n_sink = s->n_sink;
     p.causal = s->causal != 0;
     p.n_qb = (s->n_q + 127) / 128;
@@ -361,6 +362,7 @@ int ress_window_attn(const ress_window_shape *shape, const void *q, const void *
     p.lse = lse;
     p.splits = plan.splits;
     p.n_qb = (p.n_q * plan.groups + 127) / 128;
+    p.q_blocks = ress::divider(p.n_qb);
     if (plan.splits > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_row = reinterpret_cast<float2 *>(p.part + (size_t)plan.splits * p.H * p.n_q * 64);
@@ -433,6 +435,7 @@ int ress_window_attn_bwd(const ress_window_shape *shape, const ress_window_grads
     b.items = plan.items;
     b.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * rows);
     b.w.n_qb = (shape->n_q * plan.groups + 127) / 128;
+    if (b.w.n_qb > 0) b.w.q_blocks = ress::divider(b.w.n_qb);
     return ress::launch_window_bwd(b, plan.groups, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }
 
@@ -470,8 +473,8 @@ int ress_window_attn_decode(const ress_decode_shape *shape, const void *q, const
     p.H_kv = s.H_kv;
     p.group = s.H / s.H_kv;
     p.capacity = s.capacity;
-    p.frame = ress::at_most_2_26(s.frame);
-    p.window = ress::at_most_2_26(s.window);
+    ress::sights(s.frame, s.window, p.frame, p.window);
+    p.frames = ress::divider(p.frame);
     p.n_sink = s.n_sink;
     p.splits = ress::decode_splits(shape);
     p.scale_log2 = scale * 1.4426950408889634f;

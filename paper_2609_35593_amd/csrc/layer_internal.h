@@ -35,6 +35,24 @@ struct NormBwdParams {
 // Workgroups of the backward pass at most, each with a row of partial sums.
 int norm_bwd_parts(int64_t rows);
 
+// n / d for 0 <= n < 2^31 by a product and a shift (a division is some 30 instructions, which
+// calls of a few tiles felt). With 2^(l-1) < d <= 2^l and mul = ceil(2^(31+l) / d) < 2^32, the product's
+// excess over n / d, below 2^31 / 2^(31+l) <= 1 / d, reaches no next integer.
+struct Divider {
+    uint32_t mul;
+    int shift;
+    __host__ __device__ int operator()(int n) const
+    {
+        return (int)((uint32_t)((uint64_t)((uint32_t)n << 1) * mul >> 32) >> shift);
+    }
+};
+inline Divider divider(int d)
+{
+    int l = 0;
+    while (((int64_t)1 << l) < d) ++l;
+    return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
+}
+
 constexpr int kMaxPairs = RESS_MAX_ROPE_D / 2;
 
 struct RopeParams {
@@ -57,7 +75,8 @@ struct RopeParams {
 struct WindowParams {
     int H, H_kv, group;  // group = H / H_kv
     int n_q, n_k, q_offset;
-    int frame, window, n_sink;
+    int frame, window, n_sink;  // (window x frame below 2^28, see sights)
+    Divider frames, q_blocks, groups;  // of frame, n_qb, group
     bool causal;
     int n_qb, n_kb;  // blocks of 128 / groups queries, of 128 keys
     int splits;      // workgroups that share a block's keys (forward)
@@ -73,6 +92,14 @@ struct WindowParams {
 // Positions stay below 2^25, so frames and windows beyond 2^26 act as 2^26 does, whose product
 // leaves room in 64 bits.
 inline int at_most_2_26(int x) { return x < (1 << 26) ? x : 1 << 26; }
+// The frame and window that kernels take: positions stay below 2^25, so a window of 2^25 / frame +
+// 2 frames reaches all of them, and its products with frame fit 32 bits.
+inline void sights(int frame, int window, int &f, int &w)
+{
+    f = at_most_2_26(frame);
+    const int most = (1 << 25) / f + 2;
+    w = window < most ? window : most;
+}
 inline int64_t window_tokens(int frame, int window) { return (int64_t)at_most_2_26(frame) * at_most_2_26(window); }
 
 // How the forward pass spreads over the chip: key groups in a workgroup (1, 2, 4),
@@ -103,7 +130,8 @@ WindowBwdPlan window_bwd_plan(const ress_window_shape *s);
 
 struct DecodeParams {
     int B, H, H_kv, group;
-    int capacity, frame, window, n_sink;
+    int capacity, frame, window, n_sink;  // (frame, window: see sights)
+    Divider frames;  // of frame
     int splits;
     float scale_log2;
     int64_t q_batch, q_head, k_batch, v_batch, o_batch, o_head;

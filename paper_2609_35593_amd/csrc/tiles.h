@@ -162,13 +162,10 @@ struct Seen {
 };
 __device__ __forceinline__ Seen seen_by(const WindowParams &p, int pos)
 {
-    const int f = pos / p.frame;
-    // (frame and window are at most 2^26, see the C ABI layer: no overflow.)
-    const int64_t lo = (int64_t)(f - p.window + 1) * p.frame;
-    const int64_t hi = (int64_t)(f + (p.causal ? 1 : p.window)) * p.frame;
+    const int f = p.frames(pos);
     Seen s;
-    s.hi = (int)min(hi, (int64_t)p.n_k);
-    s.lo = (int)min(max(lo, (int64_t)0), (int64_t)s.hi);
+    s.hi = min((f + (p.causal ? 1 : p.window)) * p.frame, p.n_k);
+    s.lo = min(max((f - p.window + 1) * p.frame, 0), s.hi);
     s.sk = min(p.n_sink, p.causal ? s.hi : p.n_k);
     return s;
 }
@@ -217,16 +214,12 @@ struct SeenBy {
 };
 __device__ __forceinline__ SeenBy queries_of(const WindowParams &p, int s)
 {
-    const int f = s / p.frame;
-    int64_t lo = p.causal ? (int64_t)f * p.frame : (int64_t)(f - p.window + 1) * p.frame;
-    int64_t hi = (int64_t)(f + p.window) * p.frame;
-    if (s < p.n_sink) {
-        if (!p.causal) lo = 0;
-        hi = (int64_t)1 << 40;
-    }
+    const int f = p.frames(s);
+    const bool sink = s < p.n_sink;
+    const int lo = p.causal ? f * p.frame : sink ? 0 : (f - p.window + 1) * p.frame;
     SeenBy r;
-    r.lo = (int)min(max(lo - p.q_offset, (int64_t)0), (int64_t)p.n_q);
-    r.hi = (int)min(max(hi - p.q_offset, (int64_t)r.lo), (int64_t)p.n_q);
+    r.lo = min(max(lo - p.q_offset, 0), p.n_q);
+    r.hi = sink ? p.n_q : min(max((f + p.window) * p.frame - p.q_offset, r.lo), p.n_q);
     return r;
 }
 

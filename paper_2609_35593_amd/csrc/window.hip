@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
     const int rows = p.H * p.n_qb, per = (rows + 7) / 8;
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || at >= rows) return;
-    const int h = at / p.n_qb, i = p.n_qb - 1 - (at - h * p.n_qb);
+    const int h = p.q_blocks(at), i = p.n_qb - 1 - (at - h * p.n_qb), hk = p.groups(h);
     const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + kk * 16);
     }
-    const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
-    const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
+    const Loader<QW> load_k(p.k + hk * p.ks.head, p.ks.token, wave, lane);
+    const Loader<QW> load_v(p.v + hk * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
     // Keys outside every row's sight are not read: only [0, sk) and [lo, hi) of the workgroup are.
     auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {

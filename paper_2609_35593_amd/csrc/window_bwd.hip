@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
     const int rows = p.H * p.n_qb, per = (rows + 7) / 8;
     const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || at >= rows) return;
-    const int h = at / p.n_qb, i = p.n_qb - 1 - (at - h * p.n_qb);
+    const int h = p.q_blocks(at), i = p.n_qb - 1 - (at - h * p.n_qb), hk = p.groups(h);
     const int lane = threadIdx.x & 63, wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int hh = lane >> 5, ql = lane & 31;
@@ -93,8 +93,8 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(const WindowBwdParams b)
     }
     // (A query that sees nothing: P = 0.)
     const float lse = p.lse[(int64_t)h * p.n_q + tq], lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    const Loader<QW> load_k(p.k + (h / p.group) * p.ks.head, p.ks.token, wave, lane);
-    const Loader<QW> load_v(p.v + (h / p.group) * p.vs.head, p.vs.token, wave, lane);
+    const Loader<QW> load_k(p.k + hk * p.ks.head, p.ks.token, wave, lane);
+    const Loader<QW> load_v(p.v + hk * p.vs.head, p.vs.token, wave, lane);
     const Reader rd(lane);
     auto fetch = [&](int n, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) {
         if (n * G + grp >= tiles_n) return;

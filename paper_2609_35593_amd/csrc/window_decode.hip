@@ -55,8 +55,7 @@ __device__ __forceinline__ Visible visible(const DecodeParams &p, int b)
     const int len = min(max(p.lens[b], 0), p.capacity);
     Visible v = {0, 0, 0};
     if (len == 0) return v;
-    const int64_t lo = (int64_t)((len - 1) / p.frame - p.window + 1) * p.frame;
-    v.lo = lo > 0 ? (int)lo : 0;
+    v.lo = max((p.frames(len - 1) - p.window + 1) * p.frame, 0);
     v.sk = min(p.n_sink, v.lo);
     v.n = v.sk + len - v.lo;
     return v;

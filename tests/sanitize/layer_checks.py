@@ -71,4 +71,11 @@ for field, value in itertools.product(("B", "H", "H_kv", "capacity", "D", "frame
     n = sz(0)
     legal(lib.ress_window_attn_decode_workspace_size(C.byref(s), C.byref(n)))
     legal(lib.ress_window_attn_decode(C.byref(s), *P[:4], 0.125, P[4], P[5], BIG, None))
+# Divisions by a product and a shift: the ends of every quotient's run, where one off by the least would show.
+top = (1 << 31) - 1
+for d in (1, 2, 3, 5, 7, 63, 64, 65, 641, 1374, 5496, 65535, (1 << 20) + 1, (1 << 26) - 1, 1 << 26, (1 << 30) + 1, top):
+    for q in (0, 1, 2, 3, 1000, 12345, top // d // 2, top // d - 1, top // d):
+        for n in (q * d - 1, q * d, q * d + 1, q * d + d - 1, top):
+            if 0 <= n <= top:
+                assert lib.divided(n, d) == n // d, (n, d)
 print(f"layer checks ok: {checks}", flush=True)

@@ -14,3 +14,5 @@ hipError_t launch_window(const WindowParams &, int, hipStream_t) { return hipErr
 hipError_t launch_window_bwd(const WindowBwdParams &, int, hipStream_t) { return hipErrorInvalidValue; }
 hipError_t launch_decode(const DecodeParams &, hipStream_t) { return hipErrorInvalidValue; }
 }  // namespace ress
+
+extern "C" int divided(int n, int d) { return ress::divider(d)(n); }
