@@ -60,7 +60,8 @@ def _declare():
 
 
 _declare()
-# The current stream of a device as an address, without a Stream object around it where torch offers that.
+# The current device, and its current stream as an address, without a Stream object around it, where torch offers them.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -68,11 +69,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 def _call(fn, device, stream, *args):
     """Calls an entry point on `stream` (default: the device's current one) with the tensors' device
     current, as the C ABI asks."""
+    index = device.index
     if stream is None:
-        stream = _raw_stream(device.index)
+        stream = _raw_stream(index)
     elif hasattr(stream, "cuda_stream"):
         stream = stream.cuda_stream
-    if device.index == torch.cuda.current_device():
+    if index == _current_device():
         st = fn(*args, stream)
     else:
         with torch.cuda.device(device):
@@ -116,15 +118,13 @@ def _empty(shape, dtype, device, stream):
     return t
 
 
-def _check(name, t, dtype, shape, device):
-    """Metadata of a strided tensor whose last dimension is contiguous."""
-    if not (t.dtype is dtype and t.shape == shape and t.device == device and (t.stride(-1) == 1 or t.shape[-1] <= 1)):
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
-
-
-def _check_dense(name, t, dtype, shape, device):
-    if not (t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _dense(name, t, dtype, shape, device):
+    """Address of a contiguous tensor whose metadata must be these; of none without one."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
 def _device(name, t):
@@ -133,39 +133,38 @@ def _device(name, t):
     return t.device
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _all_strides(name, t, dtype, shape, device):
+    """The strides of a tensor whose metadata must be these and whose channels, the last dimension, must be contiguous."""
+    st = t.stride()
+    if t.dtype is dtype and t.shape == shape and t.device == device and (st[-1] == 1 or shape[-1] <= 1):
+        return st
+    raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
 
 
 def _strides(name, t, dtype, shape, device):
-    """The strides (heads, tokens) of a [heads][tokens][channels] tensor whose metadata must be these. (The stride of a
-    dimension of one entry says nothing: torch may give any.)"""
-    if t.dtype is dtype and t.shape == shape and t.device == device:
-        head, token, channel = t.stride()
-        if channel == 1 or shape[2] <= 1:
-            return head if shape[0] > 1 else 0, token if shape[1] > 1 else 0
-    raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous channels")
+    """The strides (heads, tokens) of a [heads][tokens][channels] tensor. (The stride of a dimension of one entry says
+    nothing: torch may give any.)"""
+    head, token, _ = _all_strides(name, t, dtype, shape, device)
+    return head if shape[0] > 1 else 0, token if shape[1] > 1 else 0
 
 
 # ---------------------------------------------------------------- layer norm
 
 
-def _norm_view(name, t, like):
-    """Rows, their stride and the type of [rows][width] with any row stride, or of a contiguous tensor of any rank; of
-    `like`'s shape and device where that is given."""
+def _norm_view(name, t, shape, device):
+    """Rows, their stride and the type of [rows][width] with any row stride, or of a contiguous tensor of any rank."""
     dtype = _DTYPES.get(t.dtype)
-    if dtype is None or (like is not None and (t.shape != like.shape or t.device != like.device)):
-        raise ValueError(f"{name} must be a bfloat16 or float32 CUDA tensor"
-                         + ("" if like is None else f" of shape {tuple(like.shape)} on {like.device}"))
-    if t.dim() == 2:
-        rows, width = t.shape
+    if dtype is None or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be a bfloat16 or float32 tensor of shape {tuple(shape)} on {device}")
+    if len(shape) == 2:
+        rows, width = shape
         stride, channel = t.stride()
         if channel != 1 and width > 1:
             raise ValueError(f"{name}: a row's channels must be contiguous")
         return rows, stride if rows > 1 else width, dtype
-    if t.dim() == 0 or not t.is_contiguous():
+    if not shape or not t.is_contiguous():
         raise ValueError(f"{name}: tensors of other ranks than [rows][width] must be contiguous")
-    return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1], dtype
+    return (t.numel() // shape[-1] if shape[-1] else 0), shape[-1], dtype
 
 
 def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, out_dtype=torch.bfloat16, mean=None,
@@ -174,24 +173,17 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     with any row stride, or contiguous of any rank; gamma, beta: float32 [width] or None; out: as x, of
     out_dtype when it is made here. Returns y and, with want_stats or given buffers, mean and rstd
     (float32, one per row) for ress_layer_norm_bwd."""
-    dev = _device("x", x)
-    rows, xs, xt = _norm_view("x", x, None)
+    dev, dims = _device("x", x), x.shape
+    rows, xs, xt = _norm_view("x", x, dims, dev)
     if out is None:
-        out = _empty(x.shape, out_dtype, dev, stream)
-    _, ys, yt = _norm_view("out", out, x)
-    shape = _NORM(rows, x.shape[-1], xt, yt, xs, ys, eps)
+        out = _empty(dims, out_dtype, dev, stream)
+    _, ys, yt = _norm_view("out", out, dims, dev)
+    width, each = dims[-1:], dims[:-1]
     if want_stats and mean is None and rstd is None:
-        mean, rstd = (_empty(x.shape[:-1], torch.float32, dev, stream) for _ in range(2))
-    if gamma is not None:
-        _check_dense("gamma", gamma, torch.float32, x.shape[-1:], dev)
-    if beta is not None:
-        _check_dense("beta", beta, torch.float32, x.shape[-1:], dev)
-    if mean is not None:
-        _check_dense("mean", mean, torch.float32, x.shape[:-1], dev)
-    if rstd is not None:
-        _check_dense("rstd", rstd, torch.float32, x.shape[:-1], dev)
-    _call(lib.ress_layer_norm, dev, stream, shape, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean),
-          _ptr(rstd))
+        mean, rstd = (_empty(each, torch.float32, dev, stream) for _ in range(2))
+    _call(lib.ress_layer_norm, dev, stream, _NORM(rows, *width, xt, yt, xs, ys, eps), x.data_ptr(),
+          _dense("gamma", gamma, torch.float32, width, dev), _dense("beta", beta, torch.float32, width, dev),
+          out.data_ptr(), _dense("mean", mean, torch.float32, each, dev), _dense("rstd", rstd, torch.float32, each, dev))
     return dict(y=out, mean=mean, rstd=rstd)
 
 
@@ -205,32 +197,29 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     """Gradients of ress_layer_norm (see include/ress_layer.h). dy: of y's type; x, mean, rstd: as given to
     and made by the forward pass. Returns dx (of x's type) and, with want_weights, dgamma and dbeta
     (float32 [width])."""
-    dev = _device("x", x)
-    rows, xs, xt = _norm_view("x", x, None)
-    _, ys, yt = _norm_view("dy", dy, x)
-    width = x.shape[-1]
+    dev, dims = _device("x", x), x.shape
+    rows, xs, xt = _norm_view("x", x, dims, dev)
+    _, ys, yt = _norm_view("dy", dy, dims, dev)
+    width, each = dims[-1:], dims[:-1]
     if dx is None:
-        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev)
+        dx = torch.empty_strided(dims, x.stride(), dtype=x.dtype, device=dev)
         if stream is not None:
             dx.record_stream(_as_stream(stream, dev))
-    if _norm_view("dx", dx, x)[1:] != (xs, xt):
+    if _norm_view("dx", dx, dims, dev)[1:] != (xs, xt):
         raise ValueError("dx must have x's type and row stride")
-    shape = _NORM(rows, width, xt, yt, xs, ys, 1.0)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _check_dense(name, t, torch.float32, x.shape[:-1], dev)
-    if gamma is not None:
-        _check_dense("gamma", gamma, torch.float32, (width,), dev)
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd must be given")
     if want_weights:
         dgamma = _empty(width, torch.float32, dev, stream) if dgamma is None else dgamma
         dbeta = _empty(width, torch.float32, dev, stream) if dbeta is None else dbeta
-    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
-        if t is not None:
-            _check_dense(name, t, torch.float32, (width,), dev)
+    shape = _NORM(rows, *width, xt, yt, xs, ys, 1.0)
+    args = (dy.data_ptr(), x.data_ptr(), _dense("gamma", gamma, torch.float32, width, dev),
+            _dense("mean", mean, torch.float32, each, dev), _dense("rstd", rstd, torch.float32, each, dev), dx.data_ptr(),
+            _dense("dgamma", dgamma, torch.float32, width, dev), _dense("dbeta", dbeta, torch.float32, width, dev))
     ws, ws_bytes = None, 0
     if dgamma is not None or dbeta is not None:
         ws, ws_bytes = _workspace(workspace, "ress_layer_norm_bwd_workspace_size", shape, dev, stream)
-    _call(lib.ress_layer_norm_bwd, dev, stream, shape, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
-          _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws, ws_bytes)
+    _call(lib.ress_layer_norm_bwd, dev, stream, shape, *args, ws, ws_bytes)
     return dict(dx=dx, dgamma=dgamma, dbeta=dbeta)
 
 
@@ -254,26 +243,30 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     axes = len(dims)
     if not 1 <= axes <= 4:
         raise ValueError("one to four axes")
-    _check_dense("pos", pos, torch.int32, (N, axes), dev)
+    if pos is None:
+        raise ValueError("pos must be given")
     H = H_kv = 0
     qs = ks = qo = ko = (0, 0)
+    q_in = k_in = q_to = k_to = None
     if q is not None:
         H = q.shape[0]
         qs = _strides("q", q, first.dtype, (H, N, D), dev)
         q_out = _empty(q.shape, q.dtype, dev, stream) if q_out is None else q_out
-        qo = _strides("q_out", q_out, q.dtype, q.shape, dev)
+        qo = _strides("q_out", q_out, first.dtype, (H, N, D), dev)
+        q_in, q_to = q.data_ptr(), q_out.data_ptr()
     else:
         q_out = None
     if k is not None:
         H_kv = k.shape[0]
         ks = _strides("k", k, first.dtype, (H_kv, N, D), dev)
         k_out = _empty(k.shape, k.dtype, dev, stream) if k_out is None else k_out
-        ko = _strides("k_out", k_out, k.dtype, k.shape, dev)
+        ko = _strides("k_out", k_out, first.dtype, (H_kv, N, D), dev)
+        k_in, k_to = k.data_ptr(), k_out.data_ptr()
     else:
         k_out = None
     shape = _ROPE(H, H_kv, N, D, axes, *dims, *(0,) * (4 - axes), ROPE_LAYOUTS[layout], bool(inverse), _DTYPES[first.dtype],
                   base, *qs, *ks, *qo, *ko)
-    _call(lib.ress_rope, dev, stream, shape, _ptr(pos), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out))
+    _call(lib.ress_rope, dev, stream, shape, _dense("pos", pos, torch.int32, (N, axes), dev), q_in, k_in, q_to, k_to)
     return dict(q=q_out, k=k_out)
 
 
@@ -290,12 +283,11 @@ def _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal,
 
 
 def _qkv_strides(q, k, v):
-    dev = _device("q", q)
-    if q.dim() != 3 or k.dim() != 3:
+    dev, qn, kn = _device("q", q), q.shape, k.shape
+    if len(qn) != 3 or len(kn) != 3 or qn[2] != kn[2]:
         raise ValueError("q, k and v must be [heads][tokens][channels]")
-    return dev, (_strides("q", q, torch.bfloat16, q.shape, dev)
-                 + _strides("k", k, torch.bfloat16, (k.shape[0], k.shape[1], q.shape[2]), dev)
-                 + _strides("v", v, torch.bfloat16, k.shape, dev))
+    return dev, qn, kn, (_strides("q", q, torch.bfloat16, qn, dev) + _strides("k", k, torch.bfloat16, kn, dev)
+                         + _strides("v", v, torch.bfloat16, kn, dev))
 
 
 def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q_offset: int = 0, causal: bool = True,
@@ -303,20 +295,20 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
     """Attention over a sliding window of frames and the first n_sink tokens (see include/ress_layer.h). q: bf16
     [H][n_q][64] at positions q_offset ..; k, v: bf16 [H_kv][n_k][64]; any strides with contiguous channels.
     Returns o (bf16, as q) and, with want_lse or a given buffer, lse (float32 [H][n_q])."""
-    dev, st = _qkv_strides(q, k, v)
-    H, n_q, D = q.shape
+    dev, qn, kn, st = _qkv_strides(q, k, v)
+    H, n_q, D = qn
+    H_kv, n_k, _ = kn
     if out is None:
-        out = _empty(q.shape, torch.bfloat16, dev, stream)
-    st += _strides("out", out, torch.bfloat16, q.shape, dev)
+        out = _empty(qn, torch.bfloat16, dev, stream)
+    st += _strides("out", out, torch.bfloat16, qn, dev)
     if lse is None and want_lse:
         lse = _empty((H, n_q), torch.float32, dev, stream)
-    if lse is not None:
-        _check_dense("lse", lse, torch.float32, (H, n_q), dev)
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, st)
+    lse_to = _dense("lse", lse, torch.float32, (H, n_q), dev)
+    shape = _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, st)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), float(scale), _ptr(out), _ptr(lse), ws,
-          ws_bytes)
+    _call(lib.ress_window_attn, dev, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), float(scale), out.data_ptr(),
+          lse_to, ws, ws_bytes)
     return dict(o=out, lse=lse)
 
 
@@ -337,23 +329,26 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
                          stream=None) -> dict:
     """Gradients of ress_window_attn (see include/ress_layer.h): o and lse as it made them, the other arguments
     as it was given. Returns dq, dk, dv (bf16, as q, k, v)."""
-    dev, st = _qkv_strides(q, k, v)
-    H, n_q, D = q.shape
-    st += _strides("o", o, torch.bfloat16, q.shape, dev)
-    gst = _strides("d_o", d_o, torch.bfloat16, q.shape, dev)
-    _check_dense("lse", lse, torch.float32, (H, n_q), dev)
+    dev, qn, kn, st = _qkv_strides(q, k, v)
+    H, n_q, D = qn
+    H_kv, n_k, _ = kn
+    st += _strides("o", o, torch.bfloat16, qn, dev)
+    gst = _strides("d_o", d_o, torch.bfloat16, qn, dev)
+    if lse is None:
+        raise ValueError("lse must be given")
     grads = []
-    for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-        t = _empty(like.shape, torch.bfloat16, dev, stream) if t is None else t
-        gst += _strides(name, t, torch.bfloat16, like.shape, dev)
+    for name, t, like in (("dq", dq, qn), ("dk", dk, kn), ("dv", dv, kn)):
+        t = _empty(like, torch.bfloat16, dev, stream) if t is None else t
+        gst += _strides(name, t, torch.bfloat16, like, dev)
         grads.append(t)
     dq, dk, dv = grads
-    shape = _window_shape(H, k.shape[0], n_q, k.shape[1], D, q_offset, frame, window, n_sink, causal, st)
+    shape = _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, st)
     g = _GRADS(*gst)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn_bwd, dev, stream, shape, g, _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
-          float(scale), _ptr(dq), _ptr(dk), _ptr(dv), ws, ws_bytes)
+    _call(lib.ress_window_attn_bwd, dev, stream, shape, g, d_o.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          o.data_ptr(), _dense("lse", lse, torch.float32, (H, n_q), dev), float(scale), dq.data_ptr(), dk.data_ptr(),
+          dv.data_ptr(), ws, ws_bytes)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
@@ -368,21 +363,19 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     """One new token per sequence over its cache (see include/ress_layer.h). q: bf16 [B][H][64]; k, v: bf16
     [B][H_kv][capacity][64], any strides with contiguous channels; lens: int32 [B] on the device, the new tokens
     counted. Returns o (bf16 [B][H][64])."""
-    if q.dim() != 3 or k.dim() != 4 or v.dim() != 4:
+    dev, qn, kn = _device("q", q), q.shape, k.shape
+    if len(qn) != 3 or len(kn) != 4 or kn[0] != qn[0] or kn[3] != qn[2]:
         raise ValueError("q must be [B][H][64], k and v [B][H_kv][capacity][64]")
-    dev, (B, H, D) = _device("q", q), q.shape
-    _, H_kv, capacity, _ = k.shape
-    _check("q", q, torch.bfloat16, q.shape, dev)
-    _check("k", k, torch.bfloat16, (B, H_kv, capacity, D), dev)
-    _check("v", v, torch.bfloat16, k.shape, dev)
-    _check_dense("lens", lens, torch.int32, (B,), dev)
+    B, H, D = qn
+    _, H_kv, capacity, _ = kn
+    q_b, q_h, _ = _all_strides("q", q, torch.bfloat16, qn, dev)
+    k_b, k_h, k_t, _ = _all_strides("k", k, torch.bfloat16, kn, dev)
+    v_b, v_h, v_t, _ = _all_strides("v", v, torch.bfloat16, kn, dev)
+    if lens is None:
+        raise ValueError("lens must be given")
     if out is None:
-        out = _empty(q.shape, torch.bfloat16, dev, stream)
-    _check("out", out, torch.bfloat16, q.shape, dev)
-    q_b, q_h, _ = q.stride()
-    k_b, k_h, k_t, _ = k.stride()
-    v_b, v_h, v_t, _ = v.stride()
-    o_b, o_h, _ = out.stride()
+        out = _empty(qn, torch.bfloat16, dev, stream)
+    o_b, o_h, _ = _all_strides("out", out, torch.bfloat16, qn, dev)
     if B <= 1:  # (the stride of a dimension of one entry says nothing)
         q_b = k_b = v_b = o_b = 0
     if H <= 1:
@@ -395,6 +388,6 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
                     v_h, v_t, o_b, o_h)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ws, ws_bytes = _workspace(workspace, "ress_window_attn_decode_workspace_size", shape, dev, stream)
-    _call(lib.ress_window_attn_decode, dev, stream, shape, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), float(scale), _ptr(out), ws,
-          ws_bytes)
+    _call(lib.ress_window_attn_decode, dev, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          _dense("lens", lens, torch.int32, (B,), dev), float(scale), out.data_ptr(), ws, ws_bytes)
     return out
