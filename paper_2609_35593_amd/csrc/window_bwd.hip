@@ -21,6 +21,11 @@
 // In both a lane holds one column of the score tile (a query, a key), so P and dS, rounded
 // to bf16, are the next products' operands as they lie (tiles.h); -delta enters as the
 // initial value of the accumulator.
+//
+// Bound by issue slots beside the matrix unit, as the forward pass: 16 heads of 8 frames of 1,374
+// tokens, window 3 and a frame of sinks, dq 405 us and dkv 427 (the 8 products at 965 TFLOP/s, 81% of
+// a large library product's rate; matrix unit busy 51%, vector unit 46 and 42%). 3,001 tokens, 12
+// heads for 4, 5 sinks: 56-59 us in three launches of short lists.
 #include "tiles.h"
 
 namespace ress {

