@@ -40,6 +40,10 @@ SHAPES = [
     (2, 2, 1400, 1400, 0, 300, 2, 300, True),
     (2, 2, 700, 700, 0, 1, 90, 650, True),     # sinks beyond most windows
     (2, 2, 100, 100, 300, 1, 10, 80, True),    # the sinks only, keys behind them in their last tile
+    (2, 2, 2500, 2500, 0, 1, 100, 5, True),    # the sinks' queries alone cut
+    (64, 16, 2050, 2050, 0, 1, 300, 70, True),  # workgroups for several fillings: one key group a workgroup
+    (64, 64, 2050, 2050, 0, 100, 3, 100, True),
+    (64, 8, 2050, 2050, 0, 1, 90, 3, False),
 ]
 
 
