@@ -34,6 +34,24 @@ bool strides_ok(const ress_strides &s, int64_t multiple)
            s.token % multiple == 0;
 }
 
+// Chunks of `per` channels, aligned to their size in every head and token, that hold whole runs of
+// one side of the pairs (or whole pairs, interleaved).
+bool rope_chunks(const ress_rope_shape &s, int per, int turned, const void *const (&src)[2], void *const (&dst)[2])
+{
+    if (s.D % per || s.D / per > ress::kMaxChunks) return false;
+    const size_t bytes = per * dtype_size(s.dtype);
+    const ress_strides *st[4] = {&s.q, &s.q_out, &s.k, &s.k_out};
+    for (int i = 0; i < 2; ++i)
+        if ((i ? s.H_kv : s.H) > 0 && (!aligned(src[i], bytes) || !aligned(dst[i], bytes) || !strides_ok(*st[2 * i], per) ||
+                                       !strides_ok(*st[2 * i + 1], per)))
+            return false;
+    if (s.layout == RESS_ROPE_SECTIONS) return turned % (2 * per) == 0;
+    if (s.layout == RESS_ROPE_INTERLEAVED) return turned % per == 0;
+    for (int a = 0; a < s.n_axes; ++a)
+        if (s.dims[a] % (2 * per)) return false;
+    return true;
+}
+
 bool same(const ress_strides &a, const ress_strides &b) { return a.head == b.head && a.token == b.token; }
 
 // ---------------------------------------------------------------- layer norm
@@ -256,8 +274,6 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     void *dst[2] = {q_out, k_out};
     const int heads[2] = {s.H, s.H_kv};
     const size_t size = dtype_size(s.dtype);
-    const int per = (int)(16 / size);  // channels of a chunk
-    bool chunks = s.D % per == 0;
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0 || s.N == 0) continue;
         if (!src[i] || !dst[i] || !pos || !aligned(src[i], size) || !aligned(dst[i], size) || !aligned(pos, 4))
@@ -266,15 +282,10 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
         if (!disjoint(heads[i], out[i]->head, s.N, out[i]->token, s.D)) return RESS_E_INVALID_ARG;
         if (src[i] == dst[i] && !same(*in[i], *out[i])) return RESS_E_INVALID_ARG;
         if (dst[i] == pos || (heads[1 - i] && (dst[i] == src[1 - i] || dst[i] == dst[1 - i]))) return RESS_E_INVALID_ARG;
-        chunks = chunks && aligned(src[i], 16) && aligned(dst[i], 16) && strides_ok(*in[i], per) && strides_ok(*out[i], per);
     }
     if (s.H + s.H_kv == 0 || s.N == 0) return RESS_OK;
 
     // The pairs: axis, turns a position, channels. Copied channels pair up behind them.
-    if (s.layout == RESS_ROPE_SECTIONS) chunks = chunks && turned % (2 * per) == 0;
-    if (s.layout == RESS_ROPE_INTERLEAVED) chunks = chunks && turned % per == 0;
-    if (s.layout == RESS_ROPE_SPLIT)
-        for (int a = 0; a < s.n_axes; ++a) chunks = chunks && s.dims[a] % (2 * per) == 0;
     ress::RopeParams p;
     memset(&p, 0, sizeof p);
     int n = 0, at = 0;
@@ -301,11 +312,13 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
         p.ca[n] = (uint8_t)(turned + 2 * i);
         p.cb[n] = (uint8_t)(turned + 2 * i + 1);
     }
-    for (int c = 0; chunks && c < s.D / per; ++c) p.other[c] = (uint8_t)c;
-    for (int i = 0; chunks && i < turned / 2; ++i) {
-        const int a = p.ca[i] / per, b = p.cb[i] / per;
-        if (p.ca[i] % per == 0) p.pair_of[a] = (uint8_t)i, p.other[a] = (uint8_t)b;
-        if (p.cb[i] % per == 0) p.pair_of[b] = (uint8_t)i, p.other[b] = (uint8_t)a;
+    for (int per = (int)(16 / size); per >= (int)(8 / size) && !p.chunk; per /= 2)
+        if (rope_chunks(s, per, turned, src, dst)) p.chunk = per;
+    for (int c = 0; p.chunk && c < s.D / p.chunk; ++c) p.other[c] = (uint8_t)c;
+    for (int i = 0; p.chunk && i < turned / 2; ++i) {
+        const int a = p.ca[i] / p.chunk, b = p.cb[i] / p.chunk;
+        if (p.ca[i] % p.chunk == 0) p.pair_of[a] = (uint8_t)i, p.other[a] = (uint8_t)b;
+        if (p.cb[i] % p.chunk == 0) p.pair_of[b] = (uint8_t)i, p.other[b] = (uint8_t)a;
     }
     p.H = s.H;
     p.H_all = s.H + s.H_kv;
@@ -316,7 +329,6 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     p.turned = turned;
     p.f32 = s.dtype == RESS_DTYPE_F32;
     p.inverse = s.inverse != 0;
-    p.chunks = chunks;
     p.pos = pos;
     p.q_in = q_in;
     p.k_in = k_in;

@@ -54,13 +54,14 @@ inline Divider divider(int d)
 }
 
 constexpr int kMaxPairs = RESS_MAX_ROPE_D / 2;
+constexpr int kMaxChunks = 64;  // of a token: one wave's
 
 struct RopeParams {
     int H, H_all;  // heads of q; of q and k together
     int N, n_axes, n_pairs, D;
     int turned;  // channels that turn, the first ones
     bool f32, inverse, interleaved;
-    bool chunks;  // pairs come in whole 16-byte chunks (see rope.hip)
+    int chunk;  // channels of the chunks that pairs come in (see rope.hip); 0: none
     const int32_t *pos;
     const void *q_in, *k_in;
     void *q_out, *k_out;
@@ -68,8 +69,8 @@ struct RopeParams {
     double turns[kMaxPairs];   // turns per position; < 0: a pair that is copied
     uint8_t axis[kMaxPairs];
     uint8_t ca[kMaxPairs], cb[kMaxPairs];  // the pair's channels
-    // chunks: the first pair of chunk c, and the chunk that holds its pairs' other channels
-    uint8_t pair_of[RESS_MAX_ROPE_D / 4], other[RESS_MAX_ROPE_D / 4];
+    // chunk > 0: the first pair of chunk c, and the chunk that holds its pairs' other channels
+    uint8_t pair_of[kMaxChunks], other[kMaxChunks];
 };
 
 struct WindowParams {
