@@ -37,7 +37,7 @@ def _check(got, x, pos, dims, layout, base, inverse=False):
                                     (48, (16, 16, 16)), (64, (0, 32)), (64, (0,)), (80, (48, 16))])
 def test_layouts(ress, D, dims, layout, dtype):
     say(f"[rope] D {D} {dims} {layout} {dtype}")
-    for H, H_kv, N in ((3, 1, 77), (1, 5, 1), (9, 2, 300), (2, 7, 20000)):
+    for H, H_kv, N in ((3, 1, 77), (1, 5, 1), (9, 2, 300), (2, 7, 20000), (2, 1, 130)):
         q, k, pos = _inputs(D + N, H, H_kv, N, D, len(dims), dtype)
         for inverse in (False, True):
             r = ress.ress_rope(q, k, pos, dims=dims, layout=layout, base=1e4, inverse=inverse)
