@@ -1,23 +1,29 @@
 // Windowed attention of one new token per sequence over its cache.
 //
-// Bound by the read of the visible keys and values (256 bytes a key and head for 4 D = 256
-// flops a query head), so the products run on the vector unit: 8 lanes hold a key's or a
-// value's 64 channels, a wave 8 keys at a time, and the up to R query heads that share a
-// K/V head are formed from one read. The visible keys, sinks and window, are numbered
-// through (j -> key), so no work goes into masked ones and nothing outside them is read.
-// They are cut over `splits` workgroups of 4 or 8 waves, a run of turns of 32 keys each, the next
-// turn's loads under way; every 8 lanes keep an online softmax of their own, joined in a
-// fixed order in the wave, the workgroup, and for more than one split by join_kernel.
+// Bound by the read of the visible keys and values: 256 bytes a key and K/V head. The visible keys,
+// sinks and window, are numbered through (j -> key), so no work goes into masked ones and nothing
+// outside them is read. They are cut over `splits` workgroups and their waves, a run of turns each,
+// the next turn's loads under way; every wave keeps an online softmax of its own, joined in a
+// fixed order in the workgroup, and for more than one split by join_kernel.
 //
-// 24 streams of 1 to 20,000 keys, 4 K/V heads, window 4,096: 26.6 us, 3.3 TB/s; one of 16 heads and
+//   decode_kernel       one head a K/V head: products on the vector unit, 8 lanes a key's or
+//                       a value's 64 channels, a wave 8 keys at a time
+//   decode_tile_kernel  several heads, formed from one read: products on the matrix unit, the heads
+//                       its columns. (On the vector unit, four heads from one read: 24 streams of up
+//                       to 4,160 keys, 16 heads for 4, 28.0 us, here 23.3; 3 of 12,400, 32 heads for 4,
+//                       26.5 / 13.7; 64 of 8,000, 32 for 8, 231 / 190; two heads of 16 x 3,000 15.3 / 14.8;
+//                       one head there: 16 of 6,863 keys 9.1, here 11.2.)
+//
+// 24 streams of 1 to 20,000 keys, 4 K/V heads, window 4,096: 25.1 us, 3.6 TB/s (64 of 8,000: 190, 5.5); one of 16 heads and
 // 6,863 visible keys: 10.9 us. Both kernels are chains of memory round trips (lengths, first turn,
-// partial results), not bandwidth.
-#include "layer_internal.h"
+// partial results) as much as bandwidth.
+#include "tiles.h"
 
 namespace ress {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
+using namespace tiles;
+
 typedef unsigned int u32x4 __attribute__((__vector_size__(16)));
 
 constexpr int kMaxSplits = 32;
@@ -65,48 +71,45 @@ __device__ __forceinline__ Visible visible(const DecodeParams &p, int b)
     return v;
 }
 
-// Waves of a workgroup: one head's lanes leave registers for twice the waves of four heads' (us
-// with 4 / 8: 16 heads of 6,870 keys, one a K/V head, 10.5 / 9.3; 24 streams, four a K/V head, 27 / 34).
-constexpr int waves_of(int heads) { return heads == 1 ? 8 : 4; }
+constexpr int kHeadWaves = 8;  // of decode_kernel (us with 4 / 8: 16 heads of 6,870 keys 10.5 / 9.3)
+constexpr int kTileWaves = 4;  // of decode_tile_kernel: 64 KiB of slots, two workgroups a CU
 
-template <int R>
-__global__ void __launch_bounds__(64 * waves_of(R)) decode_kernel(const DecodeParams p)
+// A head's channel `lane` of a workgroup: the output, or its part of it.
+__device__ __forceinline__ void finish(const DecodeParams &p, int b, int h, int split, int lane, float top, float sum, float o)
 {
-    constexpr int kWaves = waves_of(R);
-    __shared__ float lds[kWaves][R][kPart];
-    const int split = blockIdx.x, b = blockIdx.z;
-    const int tiles = (p.group + R - 1) / R;
-    const int hk = blockIdx.y / tiles, h0 = hk * p.group + (blockIdx.y % tiles) * R;
-    const int heads = min(R, (hk + 1) * p.group - h0);
+    if (p.splits == 1) {
+        const float y = sum == 0.f ? 0.f : o / sum;
+        p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)y);
+    } else {
+        float *d = p.part + (((int64_t)b * p.H + h) * p.splits + split) * kPart;
+        if (lane == 0) d[0] = top, d[1] = sum;
+        d[2 + lane] = o;
+    }
+}
+
+__global__ void __launch_bounds__(64 * kHeadWaves) decode_kernel(const DecodeParams p)
+{
+    __shared__ float lds[kHeadWaves][kPart];
+    const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ch = lane & 7, oct = lane >> 3;
     const Visible vis = visible(p, b);
 
     // Whole turns of 32 keys, evenly over the splits' waves.
-    const int turns = (vis.n + 31) / 32, waves = p.splits * kWaves, each = (turns + waves - 1) / waves;
-    const int first = (split * kWaves + wave) * each, last = min(first + each, turns);
+    const int turns = (vis.n + 31) / 32, waves = p.splits * kHeadWaves, each = (turns + waves - 1) / waves;
+    const int first = (split * kHeadWaves + wave) * each, last = min(first + each, turns);
 
-    u32x4 q[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int h = h0 + min(r, heads - 1);
-        q[r] = *reinterpret_cast<const u32x4 *>(p.q + b * p.q_batch + h * p.q_head + ch * 8);
-    }
-    const uint16_t *kb = p.k + b * p.k_batch + hk * p.ks.head + ch * 8;
-    const uint16_t *vb = p.v + b * p.v_batch + hk * p.vs.head + ch * 8;
+    const u32x4 q = *reinterpret_cast<const u32x4 *>(p.q + b * p.q_batch + h * p.q_head + ch * 8);
+    const uint16_t *kb = p.k + b * p.k_batch + h * p.ks.head + ch * 8;
+    const uint16_t *vb = p.v + b * p.v_batch + h * p.vs.head + ch * 8;
 
-    float m[R], l[R], acc[R][8];
+    float m = kNone, l = 0.f, acc[8];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        m[r] = kNone;
-        l[r] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[r][e] = 0.f;
-    }
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
     u32x4 kx[4], vx[4], kn[4], vn[4];
     auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            // (Past the end: the last key again, its weight 0 and its value left out.)
+            // (Past the end: the last key again, its weight 0.)
             const int j = min(t * 32 + i * 8 + oct, vis.n - 1);
             const int64_t key = j < vis.sk ? j : j - vis.sk + vis.lo;
             kn[i] = *reinterpret_cast<const u32x4 *>(kb + key * p.ks.token);
@@ -118,78 +121,212 @@ __global__ void __launch_bounds__(64 * waves_of(R)) decode_kernel(const DecodePa
 #pragma unroll
         for (int i = 0; i < 4; ++i) kx[i] = kn[i], vx[i] = vn[i];
         if (t + 1 < last) fetch(t + 1);
+        float s[4], top = m;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float s[4], top = m[r];
+        for (int i = 0; i < 4; ++i) {
+            float d = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float d = 0.f;
+            for (int e = 0; e < 4; ++e) d = dot2(kx[i][e], q[e], d);
+            d = sum8(d) * p.scale_log2;
+            s[i] = t * 32 + i * 8 + oct < vis.n ? d : -INFINITY;
+            top = fmaxf(top, s[i]);
+        }
+        const float a = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= a;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d = dot2(kx[i][e], q[r][e], d);
-                d = sum8(d) * p.scale_log2;
-                s[i] = t * 32 + i * 8 + oct < vis.n ? d : -INFINITY;
-                top = fmaxf(top, s[i]);
-            }
-            const float a = __builtin_amdgcn_exp2f(m[r] - top);
-            m[r] = top;
-            l[r] *= a;
+        for (int e = 0; e < 8; ++e) acc[e] *= a;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[r][e] *= a;
+        for (int i = 0; i < 4; ++i) {
+            const float w = __builtin_amdgcn_exp2f(s[i] - top);
+            l += w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = __builtin_amdgcn_exp2f(s[i] - top);
-                l[r] += w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc[r][2 * e] = fmaf(w, lo_f(vx[i][e]), acc[r][2 * e]);
-                    acc[r][2 * e + 1] = fmaf(w, hi_f(vx[i][e]), acc[r][2 * e + 1]);
-                }
+            for (int e = 0; e < 4; ++e) {
+                acc[2 * e] = fmaf(w, lo_f(vx[i][e]), acc[2 * e]);
+                acc[2 * e + 1] = fmaf(w, hi_f(vx[i][e]), acc[2 * e + 1]);
             }
         }
     }
     // The wave's 8 groups of lanes, then the workgroup's waves.
+    float top = m;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float top = m[r];
+    for (int o = 8; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float a = __builtin_amdgcn_exp2f(m - top);
+    l *= a;
 #pragma unroll
-        for (int o = 8; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-        const float a = __builtin_amdgcn_exp2f(m[r] - top);
-        l[r] *= a;
+    for (int e = 0; e < 8; ++e) acc[e] *= a;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[r][e] *= a;
+    for (int o = 8; o < 64; o <<= 1) {
+        l += __shfl_xor(l, o);
 #pragma unroll
-        for (int o = 8; o < 64; o <<= 1) {
-            l[r] += __shfl_xor(l[r], o);
+        for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o);
+    }
+    if (oct == 0) {
+        float *d = lds[wave];
+        if (ch == 0) d[0] = top, d[1] = l;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[r][e] += __shfl_xor(acc[r][e], o);
+        for (int e = 0; e < 8; ++e) d[2 + ch * 8 + e] = acc[e];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float sum = 0.f, o = 0.f;
+    top = kNone;
+#pragma unroll
+    for (int w = 0; w < kHeadWaves; ++w) top = fmaxf(top, lds[w][0]);
+#pragma unroll
+    for (int w = 0; w < kHeadWaves; ++w) {
+        const float x = __builtin_amdgcn_exp2f(lds[w][0] - top);
+        sum = fmaf(lds[w][1], x, sum);
+        o = fmaf(lds[w][2 + lane], x, o);
+    }
+    finish(p, b, h, split, lane, top, sum, o);
+}
+
+// Up to 32 heads of a K/V head a workgroup, the columns of the products (tiles.h). A wave's turn is 64 of the numbered keys, their rows of K straight in
+// registers as the product's operand, those of V through LDS slots of the wave's own, so that no
+// wave waits for another before the join. A weight enters its product as two bf16 numbers, itself
+// rounded and what that leaves (2^-16 of it at most is lost), so that the outputs are those of
+// float32 weights, as in decode_kernel.
+__global__ void __launch_bounds__(64 * kTileWaves, 2) decode_tile_kernel(const DecodeParams p)
+{
+    constexpr int kWaves = kTileWaves, kStep = 33;  // floats between a part's rows in LDS: one of 32 heads each, no conflicts
+    __shared__ __attribute__((aligned(1024))) unsigned char v_0[kWaves * kTileBytes], v_1[kWaves * kTileBytes];
+    static_assert(2 * kPart * kStep * 4 <= (int)sizeof v_0, "two waves' parts fit a slot array");
+    const int split = blockIdx.x, b = blockIdx.z;
+    const int tiles = (p.group + 31) / 32;
+    const int hk = blockIdx.y / tiles, h0 = hk * p.group + (blockIdx.y % tiles) * 32;
+    const int heads = min(32, (hk + 1) * p.group - h0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hh = lane >> 5, ql = lane & 31;
+    const Visible vis = visible(p, b);
+    const int turns = (vis.n + 63) / 64, waves = p.splits * kWaves, each = (turns + waves - 1) / waves;
+    const int first = (split * kWaves + wave) * each, last = min(first + each, turns);
+
+    bf16x8 qf[4];
+    {
+        const uint16_t *q = p.q + b * p.q_batch + (h0 + min(ql, heads - 1)) * p.q_head + hh * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + kk * 16);
+    }
+    const uint16_t *kb = p.k + b * p.k_batch + hk * p.ks.head + hh * 8;
+    const uint16_t *vb = p.v + b * p.v_batch + hk * p.vs.head;
+    // (Past the end: the last key again, its weight 0.)
+    auto key_of = [&](int j) __attribute__((always_inline)) -> int64_t {
+        j = min(j, vis.n - 1);
+        return j < vis.sk ? j : j - vis.sk + vis.lo;
+    };
+    auto fetch = [&](int t, bf16x8 (&k)[2][4], unsigned char *slot) __attribute__((always_inline)) {
+        if (t >= last) return;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint16_t *row = kb + key_of(t * 64 + u * 32 + ql) * p.ks.token;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) k[u][kk] = *reinterpret_cast<const bf16x8 *>(row + kk * 16);
         }
-        if (oct == 0) {
-            float *d = lds[wave][r];
-            if (ch == 0) d[0] = top, d[1] = l[r];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d[2 + ch * 8 + e] = acc[r][e];
+        for (int u = 0; u < 8; ++u) {
+            const int r = u * 8 + (lane >> 3);
+            const uint16_t *row = vb + key_of(t * 64 + r) * p.vs.token + (((lane & 7) ^ swz(r)) << 3);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)row, (lds_void *)(slot + u * 1024),
+                                             16, 0, 0);
         }
+    };
+    const Reader rd(lane);
+    const float c = p.scale_log2;
+    float m = kNone, sum = 0.f;
+    f32x16 acc[2];
+#pragma unroll
+    for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[dh][v] = 0.f;
+    int t = first;
+    auto step = [&](const bf16x8 (&k)[2][4], const unsigned char *vt, bf16x8 (&kn)[2][4], unsigned char *vn)
+                    __attribute__((always_inline)) -> bool {
+        fetch(t + 1, kn, vn);
+        f32x16 s[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[u][v] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) s[u] = mfma(k[u][kk], qf[kk], s[u]);
+            if ((t + 1) * 64 > vis.n)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (t * 64 + u * 32 + (v >> 2) * 8 + hh * 4 + (v & 3) >= vis.n) s[u][v] = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, s[u][v]);
+        }
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)) * c, m);
+        if (__any(top > m)) {
+            const float a = __builtin_amdgcn_exp2f(m - top);
+            sum *= a;
+#pragma unroll
+            for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[dh][v] *= a;
+            m = top;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            bf16x8 pb[2], rest[2];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[u][v] = __builtin_amdgcn_exp2f(fmaf(s[u][v], c, -m));
+                sum += s[u][v];
+            }
+            pack(s[u], pb);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[u][v] -= (float)pb[v >> 3][v & 7];
+            pack(s[u], rest);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dh = 0; dh < 2; ++dh) {
+                    const bf16x8 vc = rd.cols(vt, u, e, dh);
+                    acc[dh] = mfma(vc, pb[e], acc[dh]);
+                    acc[dh] = mfma(vc, rest[e], acc[dh]);
+                }
+        }
+        __builtin_amdgcn_s_waitcnt(0x0070);  // the next turn's loads, and this one's reads of its slot
+        asm volatile("" ::: "memory");
+        return ++t < last;
+    };
+    if (t < last) {
+        unsigned char *const a = v_0 + wave * kTileBytes, *const z = v_1 + wave * kTileBytes;
+        bf16x8 ka[2][4], kz[2][4];
+        fetch(t, ka, a);
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("" ::: "memory");
+        while (step(ka, a, kz, z) && step(kz, z, ka, a)) {
+        }
+    }
+    sum += __shfl_xor(sum, 32);
+    __syncthreads();  // (slots of other waves become parts)
+    auto part = [&](int w) __attribute__((always_inline)) -> float * {
+        return reinterpret_cast<float *>(w < 2 ? v_0 : v_1) + (w & 1) * kPart * kStep;
+    };
+    {
+        float *d = part(wave) + ql;
+        if (hh == 0) d[0] = m, d[kStep] = sum;
+#pragma unroll
+        for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) d[(2 + dh * 32 + (v >> 2) * 8 + hh * 4 + (v & 3)) * kStep] = acc[dh][v];
     }
     __syncthreads();
     for (int r = wave; r < heads; r += kWaves) {
-        float top = kNone, sum = 0.f, o = 0.f;
+        float top = kNone, l = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds[w][r][0]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part(w)[r]);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float a = __builtin_amdgcn_exp2f(lds[w][r][0] - top);
-            sum = fmaf(lds[w][r][1], a, sum);
-            o = fmaf(lds[w][r][2 + lane], a, o);
+            const float a = __builtin_amdgcn_exp2f(part(w)[r] - top);
+            l = fmaf(part(w)[kStep + r], a, l);
+            o = fmaf(part(w)[(2 + lane) * kStep + r], a, o);
         }
-        const int h = h0 + r;
-        if (p.splits == 1) {
-            const float y = sum == 0.f ? 0.f : o / sum;
-            p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)y);
-        } else {
-            float *d = p.part + (((int64_t)b * p.H + h) * p.splits + split) * kPart;
-            if (lane == 0) d[0] = top, d[1] = sum;
-            d[2 + lane] = o;
-        }
+        finish(p, b, h0 + r, split, lane, top, l, o);
     }
 }
 
@@ -224,45 +361,45 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
     p.o[b * p.o_batch + h * p.o_head + lane] = __builtin_bit_cast(uint16_t, (__bf16)(sum == 0.f ? 0.f : o / sum));
 }
 
-template <int R>
-hipError_t go(const DecodeParams &p, hipStream_t s)
-{
-    const dim3 grid((unsigned)p.splits, (unsigned)(p.H_kv * ((p.group + R - 1) / R)), (unsigned)p.B);
-    hipLaunchKernelGGL(decode_kernel<R>, grid, dim3(64 * waves_of(R)), 0, s, p);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (p.splits > 1) {
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.B * p.H + 3) / 4)), dim3(256), 0, s, p);
-        return hipGetLastError();
-    }
-    return hipSuccess;
-}
-
 }  // namespace
 
-// Workgroups per sequence and head: enough for 4 a CU, but none with less than 256 keys, and one
-// up to 512 (us with at least 256 / 512 / 1,024 keys, the join counted: 4 heads of 900 keys for 16
-// 10.1 / 12.2 / 13.5, of 8,000 10.6 / 12.6 / 17.2; 16 heads of 6,870 9.6 / 9.3 / 10.8; 8 streams
-// of 4 heads of 4,000 19.6 / 18.1 / 20.9; 32 heads of 300 7.4 / 5.1 / 5.2; 768 heads of 2,000 in
-// halves 81, whole 74).
+// Workgroups per sequence and K/V head (or 32 of its heads).
 int decode_splits(const ress_decode_shape *s)
 {
     if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
     const int64_t seen = window_tokens(s->frame, s->window) + s->n_sink;
     const int64_t keys = seen < s->capacity ? seen : s->capacity;  // at least 1
-    const int64_t heads = (int64_t)s->B * s->H_kv * ((s->H / s->H_kv + 3) / 4);
-    const int64_t want = 1024 / heads, most = keys <= 512 ? 1 : (keys + 255) / 256;
+    const int group = s->H / s->H_kv;
+    const bool one = group == 1;
+    const int64_t heads = (int64_t)s->B * s->H_kv * ((group + 31) / 32);
+    // One head: enough for 4 workgroups a CU, none with less than 256 keys (us with at least 256 /
+    // 512 / 1,024 keys, the join counted: 16 heads of 6,870 9.6 / 9.3 / 10.8; one of 40,000 10.6 with 32
+    // splits; 32 heads of 300 7.4 / 5.1 / 5.2). Several: one a CU, of at least a turn a wave (us: 96 of
+    // 4,160 keys, 1 / 2 / 5 / 8 splits 29.6 / 23.3 / 23.8 / 25.2; 32 of 4,000, 4 / 8 / 16 14.2 / 11.7 / 12.0;
+    // 4 of 8,000, 8 / 16 / 32 12.4 / 10.0 / 8.9). One workgroup up to 512 keys: a join costs more.
+    const int64_t turns = one ? (keys + 31) / 32 : (keys + 63) / 64, waves = one ? kHeadWaves : kTileWaves;
+    const int64_t want = (one ? 1024 : 256) / heads, most = keys <= 512 ? 1 : (turns + waves - 1) / waves;
     int64_t n = want < most ? want : most;
     n = n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n;
-    // No more than give every wave the same turns (24 streams of up to 4,160 keys: 10 splits of 3.25
-    // turns a wave 29.8 us, 9 of 3.6 27.4: both take 4).
-    const int64_t turns = (keys + 31) / 32, waves = waves_of(s->H == s->H_kv ? 1 : 4);
+    // No more than give every wave the same turns: 10 splits of 3.25 turns a wave take as long as 8 of 4.
     const int64_t each = (turns + n * waves - 1) / (n * waves);
     return (int)((turns + each * waves - 1) / (each * waves));
 }
 
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s)
 {
-    return p.group == 1 ? go<1>(p, s) : p.group == 2 ? go<2>(p, s) : go<4>(p, s);
+    const bool one = p.group == 1;
+    const dim3 grid((unsigned)p.splits, (unsigned)(p.H_kv * ((p.group + 31) / 32)), (unsigned)p.B);
+    if (one)
+        hipLaunchKernelGGL(decode_kernel, grid, dim3(64 * kHeadWaves), 0, s, p);
+    else
+        hipLaunchKernelGGL(decode_tile_kernel, grid, dim3(64 * kTileWaves), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.B * p.H + 3) / 4)), dim3(256), 0, s, p);
+        return hipGetLastError();
+    }
+    return hipSuccess;
 }
 
 }  // namespace ress

@@ -43,7 +43,7 @@ def _reference(q, k, v, lens, frame, window, n_sink):
     return torch.stack(o), torch.stack(b)
 
 
-@pytest.mark.parametrize("H,H_kv", [(1, 1), (4, 4), (8, 4), (6, 2), (8, 1), (10, 2), (64, 4), (12, 1), (32, 2)])
+@pytest.mark.parametrize("H,H_kv", [(1, 1), (4, 4), (8, 4), (6, 2), (8, 1), (10, 2), (64, 4), (12, 1), (32, 2), (40, 1)])
 @pytest.mark.parametrize("cap,frame,window,n_sink", [(1, 1, 1, 0), (63, 1, 1000, 0), (65, 1, 20, 3), (300, 10, 4, 17),
                                                      (1000, 1, 1, 0), (1500, 100, 3, 100), (2000, 1, 5000, 7)])
 def test_lengths(ress, H, H_kv, cap, frame, window, n_sink):
