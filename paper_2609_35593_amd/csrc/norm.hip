@@ -350,20 +350,42 @@ hipError_t go(const NormBwdParams &p, hipStream_t s)
     return hipSuccess;
 }
 
-// The lanes and chunks that hold a row: the fewest lanes left over.
+// The lanes and chunks that hold a row: few lanes left over, and several chunks a lane, which
+// keep more loads in flight and add up in fewer steps; narrow chunks want more of them (10 million
+// float32 channels, forward / backward us: rows of 257 in 256 lanes of 2 40 / 67, in 64 of 5
+// 15 / 33; of 41 in 64 lanes of 1 42 / 60, in 16 of 3 16 / 33; of 701 in 256 of 4 20 / 39, in 64 of 12
+// 15 / 31; but of 1,001 in 256 of 4 16 / 35, in 64 of 16 - / 48: the registers leave few waves).
 template <typename XT, typename YT, int VEC, typename P>
 hipError_t by_width(const P &p, hipStream_t s)
 {
     const int n = (p.width + VEC - 1) / VEC;
     if (n <= 8) return go<XT, YT, VEC, 8, 1>(p, s);
     if (n <= 16) return go<XT, YT, VEC, 16, 1>(p, s);
-    if (n <= 32) return go<XT, YT, VEC, 32, 1>(p, s);
-    if (n <= 64) return go<XT, YT, VEC, 64, 1>(p, s);
-    if (n <= 96) return go<XT, YT, VEC, 32, 3>(p, s);
-    if (n <= 128) return go<XT, YT, VEC, 64, 2>(p, s);
-    if (n <= 192) return go<XT, YT, VEC, 64, 3>(p, s);
-    if (n <= 256) return go<XT, YT, VEC, 64, 4>(p, s);
-    if (n <= 512) return go<XT, YT, VEC, 256, 2>(p, s);
+    if constexpr (VEC <= 2) {
+        if (n <= 24) return go<XT, YT, VEC, 8, 3>(p, s);
+        if (n <= 32) return go<XT, YT, VEC, 8, 4>(p, s);
+        if (n <= 48) return go<XT, YT, VEC, 16, 3>(p, s);
+        if (n <= 64) return go<XT, YT, VEC, 16, 4>(p, s);
+        if (n <= 96) return go<XT, YT, VEC, 32, 3>(p, s);
+        if (n <= 128) return go<XT, YT, VEC, 32, 4>(p, s);
+        if (n <= 160) return go<XT, YT, VEC, 32, 5>(p, s);
+        if (n <= 192) return go<XT, YT, VEC, 32, 6>(p, s);
+        if (n <= 256) return go<XT, YT, VEC, 64, 4>(p, s);
+        if (n <= 320) return go<XT, YT, VEC, 64, 5>(p, s);
+        if (n <= 384) return go<XT, YT, VEC, 64, 6>(p, s);
+        if (n <= 512) return go<XT, YT, VEC, 64, 8>(p, s);
+        if constexpr (VEC == 1) {
+            if (n <= 768) return go<XT, YT, VEC, 64, 12>(p, s);
+        }
+    } else {
+        if (n <= 32) return go<XT, YT, VEC, 32, 1>(p, s);
+        if (n <= 64) return go<XT, YT, VEC, 64, 1>(p, s);
+        if (n <= 96) return go<XT, YT, VEC, 32, 3>(p, s);
+        if (n <= 128) return go<XT, YT, VEC, 64, 2>(p, s);
+        if (n <= 192) return go<XT, YT, VEC, 64, 3>(p, s);
+        if (n <= 256) return go<XT, YT, VEC, 64, 4>(p, s);
+        if (n <= 512) return go<XT, YT, VEC, 256, 2>(p, s);
+    }
     if (n <= 1024) return go<XT, YT, VEC, 256, 4>(p, s);
     if (n <= 2048) return go<XT, YT, VEC, 256, 8>(p, s);
     if constexpr (VEC <= 4) {

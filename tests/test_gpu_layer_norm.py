@@ -43,7 +43,9 @@ def _bounds(x, gamma, beta, y, mean, rstd, out):
 @pytest.mark.parametrize("xt,yt", [(F32, BF), (F32, F32), (BF, BF), (BF, F32)])
 @pytest.mark.parametrize("rows,width", [(1, 1), (3, 2), (33, 7), (257, 64), (1000, 72), (31, 128), (70, 250), (9, 257),
                                         (5, 512), (300, 1024), (66, 1030), (17, 2048), (3, 2049), (2, 4100), (4, 8192),
-                                        (2, 16383), (2, 16384), (70001, 384), (40003, 1024), (140001, 64), (300007, 8)])
+                                        (2, 16383), (2, 16384), (70001, 384), (40003, 1024), (140001, 64), (300007, 8),
+                                        (70, 19), (70, 29), (70, 41), (41, 101), (40, 151), (40, 191), (20, 301), (20, 383),
+                                        (20, 701), (12, 602)])
 def test_forward(ress, rows, width, xt, yt):
     say(f"[norm] {rows} x {width} {xt} -> {yt}")
     gen = torch.Generator(device="cuda").manual_seed(rows * 7 + width)
@@ -111,7 +113,8 @@ def test_in_place_and_ranks(ress):
 @pytest.mark.parametrize("xt,yt", [(F32, BF), (F32, F32), (BF, BF), (BF, F32)])
 @pytest.mark.parametrize("rows,width", [(1, 1), (1, 64), (3, 7), (257, 64), (5000, 64), (700, 72), (31, 128), (70, 250),
                                         (2000, 1024), (300, 1030), (33, 2048), (3, 4100), (5, 8192), (2, 16384),
-                                        (9001, 768), (20003, 384), (150001, 64), (400009, 8)])
+                                        (9001, 768), (20003, 384), (150001, 64), (400009, 8), (700, 19), (700, 29), (700, 41),
+                                        (410, 101), (400, 151), (400, 191), (200, 301), (200, 383), (200, 701), (120, 602)])
 def test_backward(ress, rows, width, xt, yt):
     say(f"[norm bwd] {rows} x {width} {xt}, {yt}")
     gen = torch.Generator(device="cuda").manual_seed(rows * 5 + width)
