@@ -11,6 +11,8 @@
 // float32 rows of 1,024 channels, bf16 out: 43,968 forward 50.5 us (5.35 TB/s, a large copy's
 // rate), 21,984 backward 48.6 (4.6 TB/s, 4-5 us of it the join of the weights' gradients);
 // 175,872 bf16 rows of 64 channels backward 18.5 (3.65 TB/s).
+#include <type_traits>
+
 #include "layer_internal.h"
 
 namespace ress {
@@ -67,6 +69,7 @@ __device__ __forceinline__ float row_sum(float x, float (&lds)[2][WAVES], int &b
         if ((threadIdx.x & 63) == 0) lds[buf][wave] = x;
         __syncthreads();
         x = (lds[buf][w0] + lds[buf][w0 + 1]) + (lds[buf][w0 + 2] + lds[buf][w0 + 3]);
+        if constexpr (LPR == 512) x += (lds[buf][4] + lds[buf][5]) + (lds[buf][6] + lds[buf][7]);
         buf ^= 1;
     }
     return x;
@@ -350,6 +353,18 @@ hipError_t go(const NormBwdParams &p, hipStream_t s)
     return hipSuccess;
 }
 
+// Rows of K chunks in 256 lanes, or in 512 where a lane would hold 32 values and more of each tensor
+// and its kernel has as many lanes (backward, 10 million float32 channels: rows of 16,384 202 -> 54
+// us, of 16,383 303 -> 130, of 8,179 85 -> 59; with 16 values level).
+template <typename XT, typename YT, int VEC, int K, typename P>
+hipError_t wide(const P &p, hipStream_t s)
+{
+    if constexpr (std::is_same<P, NormBwdParams>::value && K * VEC >= 32)
+        return go<XT, YT, VEC, 512, K / 2>(p, s);
+    else
+        return go<XT, YT, VEC, 256, K>(p, s);
+}
+
 // The lanes and chunks that hold a row: few lanes left over, and several chunks a lane, which
 // keep more loads in flight and add up in fewer steps; narrow chunks want more of them (10 million
 // float32 channels, forward / backward us: rows of 257 in 256 lanes of 2 40 / 67, in 64 of 5
@@ -387,14 +402,14 @@ hipError_t by_width(const P &p, hipStream_t s)
         if (n <= 512) return go<XT, YT, VEC, 256, 2>(p, s);
     }
     if (n <= 1024) return go<XT, YT, VEC, 256, 4>(p, s);
-    if (n <= 2048) return go<XT, YT, VEC, 256, 8>(p, s);
+    if (n <= 2048) return wide<XT, YT, VEC, 8>(p, s);
     if constexpr (VEC <= 4) {
-        if (n <= 4096) return go<XT, YT, VEC, 256, 16>(p, s);
+        if (n <= 4096) return wide<XT, YT, VEC, 16>(p, s);
     }
     if constexpr (VEC <= 2) {
-        if (n <= 8192) return go<XT, YT, VEC, 256, 32>(p, s);
+        if (n <= 8192) return wide<XT, YT, VEC, 32>(p, s);
     }
-    if constexpr (VEC == 1) return go<XT, YT, VEC, 256, 64>(p, s);
+    if constexpr (VEC == 1) return wide<XT, YT, VEC, 64>(p, s);
     return hipErrorInvalidValue;  // (not reached: RESS_MAX_NORM_WIDTH)
 }
 
