@@ -163,13 +163,14 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormParams p, int reps)
 constexpr int kBwdThreads = 512, kBwdWaves = kBwdThreads / 64;
 
 // Rows that a group of lanes has in flight: two where that keeps a lane's values of a tensor at
-// 16 (400,000 rows of 64 channels 50.6 -> 47.7 us; 175,872 bf16 ones level).
-constexpr int bwd_rows(int values) { return values <= 8 ? 2 : 1; }
+// 16 (400,000 rows of 64 channels 50.6 -> 47.7 us; 175,872 bf16 ones level), or at 8 for a group of
+// several waves (7,457 float32 rows of 1,341 59 us with 16, 36 with 8).
+constexpr int bwd_rows(int values, int lanes) { return values <= (lanes > 64 ? 4 : 8) ? 2 : 1; }
 
 template <typename XT, typename YT, int VEC, int LPR, int K>
 __global__ void __launch_bounds__(kBwdThreads) norm_bwd_kernel(const NormBwdParams p)
 {
-    constexpr int RPW = kBwdThreads / LPR, RU = bwd_rows(K * VEC);
+    constexpr int RPW = kBwdThreads / LPR, RU = bwd_rows(K * VEC, LPR);
     constexpr int SUMS = LPR <= 64 ? kBwdWaves : kBwdThreads / LPR;  // sums of a channel to add up
     constexpr int COLS = (LPR <= 64 ? 64 : LPR) * VEC;
     __shared__ float lds[2][kBwdWaves];
@@ -340,7 +341,7 @@ hipError_t go(const NormParams &p, hipStream_t s)
 template <typename XT, typename YT, int VEC, int LPR, int K>
 hipError_t go(const NormBwdParams &p, hipStream_t s)
 {
-    constexpr int64_t SET = kBwdThreads / LPR * bwd_rows(K * VEC);
+    constexpr int64_t SET = kBwdThreads / LPR * bwd_rows(K * VEC, LPR);
     const int64_t sets = (p.rows + SET - 1) / SET;
     const int grid = (int)(sets < p.parts ? sets : p.parts);
     hipLaunchKernelGGL((norm_bwd_kernel<XT, YT, VEC, LPR, K>), dim3(grid), dim3(kBwdThreads), 0, s, p);
@@ -353,16 +354,20 @@ hipError_t go(const NormBwdParams &p, hipStream_t s)
     return hipSuccess;
 }
 
-// Rows of K chunks in 256 lanes, or in 512 where a lane would hold 32 values and more of each tensor
-// and its kernel has as many lanes (backward, 10 million float32 channels: rows of 16,384 202 -> 54
-// us, of 16,383 303 -> 130, of 8,179 85 -> 59; with 16 values level).
+// Rows of K chunks in 256 lanes, or backward in 512 where a lane would hold 32 values and more of
+// each tensor (10 million float32 channels: rows of 16,384 202 -> 54 us, of 16,383 303 -> 130, of 8,179
+// 85 -> 59), or 16 and more with rows enough for a few a workgroup (4,878 rows of 2,050 44 -> 34, but
+// 487 14 -> 18: twice the partial sums).
 template <typename XT, typename YT, int VEC, int K, typename P>
 hipError_t wide(const P &p, hipStream_t s)
 {
-    if constexpr (std::is_same<P, NormBwdParams>::value && K * VEC >= 32)
+    if constexpr (std::is_same<P, NormBwdParams>::value && K * VEC >= 32) {
         return go<XT, YT, VEC, 512, K / 2>(p, s);
-    else
+    } else {
+        if constexpr (std::is_same<P, NormBwdParams>::value && K * VEC >= 16)
+            if (p.rows >= 2048) return go<XT, YT, VEC, 512, K / 2>(p, s);
         return go<XT, YT, VEC, 256, K>(p, s);
+    }
 }
 
 // The lanes and chunks that hold a row: few lanes left over, and several chunks a lane, which

@@ -114,7 +114,8 @@ def test_in_place_and_ranks(ress):
 @pytest.mark.parametrize("rows,width", [(1, 1), (1, 64), (3, 7), (257, 64), (5000, 64), (700, 72), (31, 128), (70, 250),
                                         (2000, 1024), (300, 1030), (33, 2048), (3, 4100), (5, 8192), (2, 16384),
                                         (9001, 768), (20003, 384), (150001, 64), (400009, 8), (700, 19), (700, 29), (700, 41),
-                                        (410, 101), (400, 151), (400, 191), (200, 301), (200, 383), (200, 701), (120, 602)])
+                                        (410, 101), (400, 151), (400, 191), (200, 301), (200, 383), (200, 701), (120, 602), (2051, 2053), (4099, 2050),
+                                        (2500, 8179)])
 def test_backward(ress, rows, width, xt, yt):
     say(f"[norm bwd] {rows} x {width} {xt}, {yt}")
     gen = torch.Generator(device="cuda").manual_seed(rows * 5 + width)
