@@ -408,12 +408,14 @@ __global__ void __launch_bounds__(256) join_kernel(const WindowBwdParams b, int 
 WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
 {
     WindowBwdPlan r = {1, 0, 1, 1, 0};
-    // dq: four key groups where the forward pass takes them, else two while there are fewer blocks
-    // than fill the chip four times over (whole pass in us with 1 / 2 / 4 groups: 63 blocks over
-    // 2,000 keys 76 / 56 / 52, 128 over 1,000 65 / 53 / 65, 640 over 512 116 / 107 / 173, 1,376 over
-    // three frames of 1,374 848 / 850 / 1,183).
+    // dq: four key groups where their workgroups still are one a CU and see 8 tiles, else two while
+    // there are fewer blocks than fill the chip four times over (whole pass in us with 1 / 2 / 4 groups:
+    // 63 blocks over 2,000 keys 76 / 56 / 52, 128 over 1,000 65 / 53 / 65, 640 over 512 116 / 107 / 173,
+    // 1,376 over three frames of 1,374 848 / 850 / 1,183).
+    const int64_t window = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2);
     const int64_t q_blocks = (int64_t)s->H * (((int64_t)s->n_q + 127) / 128);
-    r.groups = window_plan(s).groups == 4 ? 4 : q_blocks < 1024 ? 2 : 1;
+    const int64_t seen = window + 128 + s->n_sink < s->n_k ? window + 128 + s->n_sink : s->n_k;
+    r.groups = q_blocks <= 64 && seen > 7 * 64 ? 4 : q_blocks < 1024 ? 2 : 1;
     const int64_t blocks = (s->n_k + 127) / 128;
     if (s->H_kv == 0 || blocks == 0) return r;
     const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k, group = s->H / s->H_kv;

@@ -41,6 +41,9 @@ SHAPES = [
     (2, 2, 700, 700, 0, 1, 90, 650, True),     # sinks beyond most windows
     (2, 2, 100, 100, 300, 1, 10, 80, True),    # the sinks only, keys behind them in their last tile
     (2, 2, 2500, 2500, 0, 1, 100, 5, True),    # the sinks' queries alone cut
+    (8, 4, 1100, 4800, 3700, 1, 3650, 10, True),  # long lists, cut over workgroups
+    (16, 4, 1100, 4800, 3700, 1, 3650, 10, True),
+    (3, 3, 1000, 3900, 2900, 1, 3000, 5, True),
     (64, 16, 2050, 2050, 0, 1, 300, 70, True),  # workgroups for several fillings: one key group a workgroup
     (64, 64, 2050, 2050, 0, 100, 3, 100, True),
     (64, 8, 2050, 2050, 0, 1, 90, 3, False),
