@@ -150,8 +150,9 @@ typedef struct {
  * and may hold anything; a NaN or infinity in one that some of them see may also
  * reach the others of the block. */
 
-/* Bytes of device workspace ress_window_attn needs (0 but for few queries over long
- * windows, whose keys are split over workgroups; strides do not matter). */
+/* Bytes of device workspace ress_window_attn needs (0 but for long windows over too few
+ * queries to fill the chip, whose keys are split over workgroups: at most 69 MB; strides
+ * do not matter). */
 int ress_window_attn_workspace_size(const ress_window_shape *shape, size_t *bytes);
 
 /* o = softmax over the visible keys of (scale q . k) v, bf16 [H][n_q][64] by the
