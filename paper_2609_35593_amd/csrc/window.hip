@@ -6,8 +6,8 @@
 // tiles.h), so a lane holds one query's scores, its softmax needs one exchange (with lane
 // l^32, which holds the other half of the keys), and the probabilities are the next
 // product's operand as they lie. A wave masks only the tiles that some of its queries see
-// in part, by two comparisons a score against its lane's range, and passes over those
-// that none sees.
+// in part, by a comparison a score against its lane's range (two among sinks), and passes
+// over those that none sees.
 //
 // Small calls: a wave's tiles come one after the other, and a chip of 1,024 SIMDs wants more
 // waves than there are rows. With G > 1 a workgroup's waves split into G groups over the same

@@ -231,9 +231,10 @@ def test_offsets_beyond_32_bits(ress):
         far.append(view)
     assert torch.equal(ress.ress_window_attn(q, *far, **kw)["o"], ref)
     lens = torch.tensor([40000], dtype=torch.int32, device="cuda")
-    a = ress.ress_window_attn_decode(q[:, -1][None], k[None], v[None], lens, window=500, n_sink=70)
-    b = ress.ress_window_attn_decode(q[:, -1][None], far[0][None], far[1][None], lens, window=500, n_sink=70)
-    assert torch.equal(a, b)
+    for heads in (2, 1):
+        a = ress.ress_window_attn_decode(q[:heads, -1][None], k[None], v[None], lens, window=500, n_sink=70)
+        b = ress.ress_window_attn_decode(q[:heads, -1][None], far[0][None], far[1][None], lens, window=500, n_sink=70)
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("shape", SHAPES)

@@ -75,9 +75,10 @@ def test_large_logits(ress):
     R.within(o, *_reference(q, k, v, [800, 333], 1, 10 ** 9, 0), "o")
 
 
-def test_unseen_keys_and_rows_around_the_output(ress):
+@pytest.mark.parametrize("H_kv", [2, 8])
+def test_unseen_keys_and_rows_around_the_output(ress, H_kv):
     """NaN behind the lengths and outside the windows has no part; an output inside a larger buffer leaves the rest."""
-    q, k, v = _inputs(2, 3, 8, 2, 500)
+    q, k, v = _inputs(2, 3, 8, H_kv, 500)
     lens = [0, 140, 431]
     t = torch.tensor(lens, dtype=torch.int32, device="cuda")
     kw = dict(window=60, n_sink=5)
@@ -94,9 +95,10 @@ def test_unseen_keys_and_rows_around_the_output(ress):
     assert bool((buf == 3).all())
 
 
-def test_cache_layouts(ress):
+@pytest.mark.parametrize("H_kv", [2, 8])
+def test_cache_layouts(ress, H_kv):
     """[B][capacity][heads][64] and slices of a buffer that holds keys and values."""
-    q, k, v = _inputs(3, 4, 8, 2, 300)
+    q, k, v = _inputs(3, 4, 8, H_kv, 300)
     t = torch.tensor([300, 5, 77, 120], dtype=torch.int32, device="cuda")
     ref = ress.ress_window_attn_decode(q, k, v, t, window=100, n_sink=2)
     kv = torch.stack([k, v], 0).permute(1, 3, 0, 2, 4).contiguous()  # [B][capacity][2][heads][64]
@@ -117,9 +119,10 @@ def test_matches_the_prefill(ress):
     assert bool(((a.double() - b.double()).abs() <= 2 * R.window_bound(o, w, mag)[:, 0]).all())
 
 
-def test_captured_call_follows_the_lengths(ress):
+@pytest.mark.parametrize("H,H_kv", [(8, 2), (4, 4)])
+def test_captured_call_follows_the_lengths(ress, H, H_kv):
     """One graph, replayed while the cache grows: eager and replayed outputs are equal at every length."""
-    B, H, H_kv, cap = 3, 8, 2, 4000
+    B, cap = 3, 4000
     q, k, v = _inputs(5, B, H, H_kv, cap)
     lens = torch.tensor([3990, 1, 700], dtype=torch.int32, device="cuda")
     kw = dict(frame=1, window=3500, n_sink=8)
