@@ -92,18 +92,19 @@ def _size(name, shape) -> int:
 
 
 def _workspace(workspace, size, shape, device, stream):
-    """Address and bytes of the caller's workspace, or of one of torch's (marked as in use on a stream that is not its
-    own), or none where the call needs none."""
+    """The caller's workspace, or one of torch's (marked as in use on a stream that is not its own), or none where the
+    call needs none; its address; its bytes. Callers hold the tensor until their kernels are enqueued: only then may
+    torch give the block to another call."""
     if workspace is None:
         n = _size(size, shape)
         if n == 0:
-            return None, 0
+            return None, None, 0
         workspace = torch.empty(n, dtype=torch.uint8, device=device)
         if stream is not None:
             workspace.record_stream(_as_stream(stream, device))
     elif not (workspace.is_cuda and workspace.device == device and workspace.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _as_stream(stream, device):
@@ -218,7 +219,7 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
             _dense("dgamma", dgamma, torch.float32, width, dev), _dense("dbeta", dbeta, torch.float32, width, dev))
     ws, ws_bytes = None, 0
     if dgamma is not None or dbeta is not None:
-        ws, ws_bytes = _workspace(workspace, "ress_layer_norm_bwd_workspace_size", shape, dev, stream)
+        workspace, ws, ws_bytes = _workspace(workspace, "ress_layer_norm_bwd_workspace_size", shape, dev, stream)
     _call(lib.ress_layer_norm_bwd, dev, stream, shape, *args, ws, ws_bytes)
     return dict(dx=dx, dgamma=dgamma, dbeta=dbeta)
 
@@ -306,7 +307,7 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
     lse_to = _dense("lse", lse, torch.float32, (H, n_q), dev)
     shape = _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, st)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
+    workspace, ws, ws_bytes = _workspace(workspace, "ress_window_attn_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn, dev, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), float(scale), out.data_ptr(),
           lse_to, ws, ws_bytes)
     return dict(o=out, lse=lse)
@@ -345,7 +346,7 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
     shape = _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, st)
     g = _GRADS(*gst)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
+    workspace, ws, ws_bytes = _workspace(workspace, "ress_window_attn_bwd_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn_bwd, dev, stream, shape, g, d_o.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
           o.data_ptr(), _dense("lse", lse, torch.float32, (H, n_q), dev), float(scale), dq.data_ptr(), dk.data_ptr(),
           dv.data_ptr(), ws, ws_bytes)
@@ -387,7 +388,7 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     shape = _DECODE(B, H, H_kv, capacity, D, _int32(frame), _int32(window), _int32(n_sink), q_b, q_h, k_b, v_b, k_h, k_t,
                     v_h, v_t, o_b, o_h)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    ws, ws_bytes = _workspace(workspace, "ress_window_attn_decode_workspace_size", shape, dev, stream)
+    workspace, ws, ws_bytes = _workspace(workspace, "ress_window_attn_decode_workspace_size", shape, dev, stream)
     _call(lib.ress_window_attn_decode, dev, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           _dense("lens", lens, torch.int32, (B,), dev), float(scale), out.data_ptr(), ws, ws_bytes)
     return out
