@@ -3,7 +3,9 @@ axes, and attention over a sliding window of frames with sink tokens.
 
 As in the package's other functions, a function carries its C entry point's name,
 checks tensor metadata, allocates outputs (and workspaces) with torch when the caller
-passes none, and passes pointers and the current stream of the tensors' device."""
+passes none, and passes pointers and the current stream of the tensors' device, or the
+caller's `stream` (a torch stream or an address; that its inputs are ready there, and its
+outputs before they are used elsewhere, is the caller's to order)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -13,6 +15,7 @@ import struct
 import torch
 
 from . import RESS_OK, RessError, lib
+from .memory import empty, raw_stream
 
 DTYPE_BF16, DTYPE_F32 = 0, 1
 MAX_NORM_WIDTH = 16384
@@ -60,10 +63,8 @@ def _declare():
 
 
 _declare()
-# The current device, and its current stream as an address, without a Stream object around it, where torch offers them.
+# The current device, without a check, where torch offers that.
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _call(fn, device, stream, *args):
@@ -71,7 +72,7 @@ def _call(fn, device, stream, *args):
     current, as the C ABI asks."""
     index = device.index
     if stream is None:
-        stream = _raw_stream(index)
+        stream = raw_stream(index)
     elif hasattr(stream, "cuda_stream"):
         stream = stream.cuda_stream
     if index == _current_device():
@@ -92,31 +93,16 @@ def _size(name, shape) -> int:
 
 
 def _workspace(workspace, size, shape, device, stream):
-    """The caller's workspace, or one of torch's (marked as in use on a stream that is not its own), or none where the
-    call needs none; its address; its bytes. Callers hold the tensor until their kernels are enqueued: only then may
-    torch give the block to another call."""
+    """The caller's workspace, or one of torch's, or none where the call needs none; its address; its bytes. Callers hold
+    the tensor until their kernels are enqueued: only then may torch give the block to another call."""
     if workspace is None:
         n = _size(size, shape)
         if n == 0:
             return None, None, 0
-        workspace = torch.empty(n, dtype=torch.uint8, device=device)
-        if stream is not None:
-            workspace.record_stream(_as_stream(stream, device))
+        workspace = empty(n, torch.uint8, device, stream, output=False)
     elif not (workspace.is_cuda and workspace.device == device and workspace.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def _as_stream(stream, device):
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
-
-
-def _empty(shape, dtype, device, stream):
-    """An output, marked as in use on a stream that is not torch's current one."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(_as_stream(stream, device))
-    return t
 
 
 def _dense(name, t, dtype, shape, device):
@@ -177,11 +163,11 @@ def ress_layer_norm(x, gamma=None, beta=None, *, eps: float = 1e-5, out=None, ou
     dev, dims = _device("x", x), x.shape
     rows, xs, xt = _norm_view("x", x, dims, dev)
     if out is None:
-        out = _empty(dims, out_dtype, dev, stream)
+        out = empty(dims, out_dtype, dev, stream)
     _, ys, yt = _norm_view("out", out, dims, dev)
     width, each = dims[-1:], dims[:-1]
     if want_stats and mean is None and rstd is None:
-        mean, rstd = (_empty(each, torch.float32, dev, stream) for _ in range(2))
+        mean, rstd = (empty(each, torch.float32, dev, stream) for _ in range(2))
     _call(lib.ress_layer_norm, dev, stream, _NORM(rows, *width, xt, yt, xs, ys, eps), x.data_ptr(),
           _dense("gamma", gamma, torch.float32, width, dev), _dense("beta", beta, torch.float32, width, dev),
           out.data_ptr(), _dense("mean", mean, torch.float32, each, dev), _dense("rstd", rstd, torch.float32, each, dev))
@@ -203,16 +189,14 @@ def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta
     _, ys, yt = _norm_view("dy", dy, dims, dev)
     width, each = dims[-1:], dims[:-1]
     if dx is None:
-        dx = torch.empty_strided(dims, x.stride(), dtype=x.dtype, device=dev)
-        if stream is not None:
-            dx.record_stream(_as_stream(stream, dev))
+        dx = empty(dims, x.dtype, dev, stream, x.stride())
     if _norm_view("dx", dx, dims, dev)[1:] != (xs, xt):
         raise ValueError("dx must have x's type and row stride")
     if mean is None or rstd is None:
         raise ValueError("mean and rstd must be given")
     if want_weights:
-        dgamma = _empty(width, torch.float32, dev, stream) if dgamma is None else dgamma
-        dbeta = _empty(width, torch.float32, dev, stream) if dbeta is None else dbeta
+        dgamma = empty(width, torch.float32, dev, stream) if dgamma is None else dgamma
+        dbeta = empty(width, torch.float32, dev, stream) if dbeta is None else dbeta
     shape = _NORM(rows, *width, xt, yt, xs, ys, 1.0)
     args = (dy.data_ptr(), x.data_ptr(), _dense("gamma", gamma, torch.float32, width, dev),
             _dense("mean", mean, torch.float32, each, dev), _dense("rstd", rstd, torch.float32, each, dev), dx.data_ptr(),
@@ -252,7 +236,7 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     if q is not None:
         H = q.shape[0]
         qs = _strides("q", q, first.dtype, (H, N, D), dev)
-        q_out = _empty(q.shape, q.dtype, dev, stream) if q_out is None else q_out
+        q_out = empty(q.shape, q.dtype, dev, stream) if q_out is None else q_out
         qo = _strides("q_out", q_out, first.dtype, (H, N, D), dev)
         q_in, q_to = q.data_ptr(), q_out.data_ptr()
     else:
@@ -260,7 +244,7 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     if k is not None:
         H_kv = k.shape[0]
         ks = _strides("k", k, first.dtype, (H_kv, N, D), dev)
-        k_out = _empty(k.shape, k.dtype, dev, stream) if k_out is None else k_out
+        k_out = empty(k.shape, k.dtype, dev, stream) if k_out is None else k_out
         ko = _strides("k_out", k_out, first.dtype, (H_kv, N, D), dev)
         k_in, k_to = k.data_ptr(), k_out.data_ptr()
     else:
@@ -300,10 +284,10 @@ def ress_window_attn(q, k, v, *, window: int, frame: int = 1, n_sink: int = 0, q
     H, n_q, D = qn
     H_kv, n_k, _ = kn
     if out is None:
-        out = _empty(qn, torch.bfloat16, dev, stream)
+        out = empty(qn, torch.bfloat16, dev, stream)
     st += _strides("out", out, torch.bfloat16, qn, dev)
     if lse is None and want_lse:
-        lse = _empty((H, n_q), torch.float32, dev, stream)
+        lse = empty((H, n_q), torch.float32, dev, stream)
     lse_to = _dense("lse", lse, torch.float32, (H, n_q), dev)
     shape = _window_shape(H, H_kv, n_q, n_k, D, q_offset, frame, window, n_sink, causal, st)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
@@ -339,7 +323,7 @@ def ress_window_attn_bwd(d_o, q, k, v, o, lse, *, window: int, frame: int = 1, n
         raise ValueError("lse must be given")
     grads = []
     for name, t, like in (("dq", dq, qn), ("dk", dk, kn), ("dv", dv, kn)):
-        t = _empty(like, torch.bfloat16, dev, stream) if t is None else t
+        t = empty(like, torch.bfloat16, dev, stream) if t is None else t
         gst += _strides(name, t, torch.bfloat16, like, dev)
         grads.append(t)
     dq, dk, dv = grads
@@ -375,7 +359,7 @@ def ress_window_attn_decode(q, k, v, lens, *, window: int, frame: int = 1, n_sin
     if lens is None:
         raise ValueError("lens must be given")
     if out is None:
-        out = _empty(qn, torch.bfloat16, dev, stream)
+        out = empty(qn, torch.bfloat16, dev, stream)
     o_b, o_h, _ = _all_strides("out", out, torch.bfloat16, qn, dev)
     if B <= 1:  # (the stride of a dimension of one entry says nothing)
         q_b = k_b = v_b = o_b = 0

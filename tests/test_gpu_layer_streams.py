@@ -1,0 +1,70 @@
+"""Calls on a stream of the caller's: where their memory comes from, and results beside work pending on the current one."""
+import pytest
+import torch
+
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ress():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2609_35593_amd as r
+
+    return r
+
+
+def _mk(*shape, dtype=BF, seed=0):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(dtype)
+
+
+def _cases(ress):
+    """Calls that make outputs of 8 MB and more, and workspaces; inputs are ready before."""
+    x, w = _mk(4096, 1024, dtype=F32), torch.ones(1024, device="cuda")
+    st = ress.ress_layer_norm(x, w, want_stats=True)
+    q, k, v, do = _mk(8, 9000, 64, seed=1), _mk(8, 9000, 64, seed=2), _mk(8, 9000, 64, seed=3), _mk(8, 9000, 64, seed=4)
+    pos = torch.arange(9000, device="cuda", dtype=torch.int32)[:, None]
+    kw = dict(window=9000, n_sink=3)
+    f = ress.ress_window_attn(q, k, v, want_lse=True, **kw)
+    lens, q1 = torch.full((8,), 9000, device="cuda", dtype=torch.int32), q[:, :8].contiguous()
+    return {
+        "norm": lambda **s: ress.ress_layer_norm(x, w, want_stats=True, out_dtype=F32, **s),
+        "norm_bwd": lambda **s: ress.ress_layer_norm_bwd(st["y"], x, w, st["mean"], st["rstd"], **s),
+        "rope": lambda **s: ress.ress_rope(q, k, pos, dims=(64,), **s),
+        "window": lambda **s: ress.ress_window_attn(q, k, v, want_lse=True, **kw, **s),
+        "window_bwd": lambda **s: ress.ress_window_attn_bwd(do, q, k, v, f["o"], f["lse"], **kw, **s),
+        "decode": lambda **s: {"o": ress.ress_window_attn_decode(q1, k[:, None], v[:, None], lens, **kw, **s)},
+    }
+
+
+def test_results_beside_pending_work(ress):
+    """Blocks just returned by the current stream, whose queue still writes them, are not given to a call on another stream:
+    their addresses are others, and results are those of a call alone. (The queue is kept busy by products of known length.)"""
+    cases = _cases(ress)
+    alone = {n: {k: t.clone() for k, t in f().items() if t is not None} for n, f in cases.items()}
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    m = torch.randn(4096, 4096, device="cuda")
+    for n, f in cases.items():
+        torch.cuda.synchronize()
+        blocks = {}
+        for size in (1 << 14, 1 << 16, 9 << 20, 10 << 20, 17 << 20, 34 << 20, 80 << 20):
+            blocks[size] = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        for _ in range(3):
+            m @ m
+        for ts in blocks.values():
+            for t in ts:
+                t.fill_(255)
+        taken = [(t.data_ptr(), t.data_ptr() + t.numel()) for ts in blocks.values() for t in ts]
+        del blocks, ts, t  # back in the current stream's pool, their fills still queued
+        got = f(stream=side)
+        for k, t in got.items():
+            if t is not None:
+                assert not any(a <= t.data_ptr() < b for a, b in taken), (n, k)
+        torch.cuda.synchronize()
+        for k, t in alone[n].items():
+            assert torch.equal(got[k], t), (n, k)
+        say(f"[streams] {n}")

@@ -1,5 +1,6 @@
 """What the binding of include/ress_layer.h does with memory, on the CPU: its calls are followed up to the C entry point,
 which is replaced, with host tensors in the place of the device's."""
+import contextlib
 import weakref
 
 import pytest
@@ -15,17 +16,56 @@ def layer():
     return layer
 
 
-class _Torch:
-    """The binding's torch: `made` notes what it allocates."""
+@pytest.fixture
+def memory():
+    from paper_2609_35593_amd import memory
+
+    return memory
+
+
+class _Stream:
+    def __init__(self, address):
+        self.cuda_stream = address
+
+    def __eq__(self, other):
+        return self.cuda_stream == other.cuda_stream
+
+
+class _Cuda:
+    """Streams by address, 7 the current one outside every context."""
 
     def __init__(self):
-        self.made = []
+        self.current = 7
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        before, self.current = self.current, s.cuda_stream
+        yield
+        self.current = before
+
+    def current_stream(self, device=None):
+        return _Stream(self.current)
+
+    def ExternalStream(self, address, device=None):
+        return _Stream(address)
+
+
+class _Torch:
+    """The binding's torch: `made` notes what it allocates, `on` the stream that was current then, `used` what the tensors
+    are marked as in use on."""
+
+    def __init__(self):
+        self.made, self.on, self.used, self.cuda = [], [], [], _Cuda()
 
     def __getattr__(self, name):
         return getattr(torch, name)
 
     def _note(self, t):
         self.made.append((weakref.ref(t), t.data_ptr(), t.dtype))
+        self.on.append(self.cuda.current)
+        used = []
+        self.used.append(used)
+        t.record_stream = lambda s: used.append(s.cuda_stream)
         return t
 
     def empty(self, *a, **kw):
@@ -36,16 +76,17 @@ class _Torch:
 
 
 @pytest.fixture
-def traced(layer, monkeypatch):
+def traced(layer, memory, monkeypatch):
     """(torch's stand-in, list that each call's address arguments are appended to)."""
     fake, calls = _Torch(), []
 
     def call(fn, device, stream, *args):
         calls.append((fn.__name__, [a for a in args if isinstance(a, int)], [(p, r() is not None) for r, p, _ in fake.made]))
 
-    monkeypatch.setattr(layer, "torch", fake)
+    monkeypatch.setattr(memory, "torch", fake)
     monkeypatch.setattr(layer, "_device", lambda name, t: t.device)
     monkeypatch.setattr(layer, "_call", call)
+    monkeypatch.setattr(memory, "raw_stream", lambda index: fake.cuda.current)
     return fake, calls
 
 
@@ -78,3 +119,31 @@ def test_workspace_lives_until_its_kernels_are_enqueued(layer, traced, name):
     assert len(workspaces) == 1
     (address, alive), = workspaces
     assert address in addresses and alive
+
+
+CALLS_ALL = dict(
+    CALLS,
+    ress_layer_norm=lambda b, **kw: b.ress_layer_norm(_z(40, 64), want_stats=True, **kw),
+    ress_rope=lambda b, **kw: b.ress_rope(_z(2, 5, 64), _z(1, 5, 64), torch.zeros(5, 2, dtype=torch.int32), dims=(32, 32), **kw),
+    lse=lambda b, **kw: b.ress_window_attn(_z(1, 5, 64), _z(1, 5, 64), _z(1, 5, 64), window=5, want_lse=True, **kw))
+
+
+@pytest.mark.parametrize("name", CALLS_ALL)
+@pytest.mark.parametrize("stream", [_Stream(9), 9], ids=["object", "address"])
+def test_memory_for_another_stream_is_that_streams(layer, traced, name, stream):
+    """Outputs and workspaces of a call on a stream that is not the current one are allocated with that stream current: a
+    block of the current stream's may still be in use by work queued there, which the other does not wait for. Outputs are
+    marked as in use on the current stream, where the caller goes on with them."""
+    fake, _ = traced
+    CALLS_ALL[name](layer, stream=stream)
+    assert fake.made and fake.on == [9] * len(fake.made) and fake.cuda.current == 7
+    for (_, _, dtype), used in zip(fake.made, fake.used):
+        assert used == ([] if dtype == torch.uint8 else [7])
+
+
+@pytest.mark.parametrize("name", CALLS_ALL)
+@pytest.mark.parametrize("stream", [None, _Stream(7), 7], ids=["none", "object", "address"])
+def test_memory_on_the_current_stream(layer, traced, name, stream):
+    fake, _ = traced
+    CALLS_ALL[name](layer, stream=stream)
+    assert fake.made and fake.on == [7] * len(fake.made) and not any(fake.used)
