@@ -15,6 +15,8 @@ import os
 import numpy as np
 import torch
 
+from .memory import empty
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libress.so")
 
@@ -157,16 +159,16 @@ def ress_select(q, k, v, gram, keep_budget, *, bq: int, bk: int, n_special_tail:
     if budget.shape[0] != H:
         raise ValueError("keep_budget must hold one int per head")
     if kept_count is None:
-        kept_count = torch.empty((H, n_qb), dtype=torch.int32, device=dev)
+        kept_count = empty((H, n_qb), torch.int32, dev, stream)
     if kept_idx is None:
-        kept_idx = torch.empty((H, n_qb, n_kb), dtype=torch.int32, device=dev)
+        kept_idx = empty((H, n_qb, n_kb), torch.int32, dev, stream)
     if drift is None and want_drift:
-        drift = torch.empty((H, n_qb, 2), dtype=torch.float64, device=dev)
+        drift = empty((H, n_qb, 2), torch.float64, dev, stream)
     if want_debug:
         if key_out is None:
-            key_out = torch.empty((H, n_qb, n_kb), dtype=torch.float64, device=dev)
+            key_out = empty((H, n_qb, n_kb), torch.float64, dev, stream)
         if prob_out is None:
-            prob_out = torch.empty((H, n_qb, n_kb), dtype=torch.float64, device=dev)
+            prob_out = empty((H, n_qb, n_kb), torch.float64, dev, stream)
     _check_out("kept_count", kept_count, torch.int32, (H, n_qb), dev)
     _check_out("kept_idx", kept_idx, torch.int32, (H, n_qb, n_kb), dev)
     for name, t, shp in (("drift", drift, (H, n_qb, 2)), ("key_out", key_out, (H, n_qb, n_kb)),
@@ -175,7 +177,7 @@ def ress_select(q, k, v, gram, keep_budget, *, bq: int, bk: int, n_special_tail:
             _check_out(name, t, torch.float64, shp, dev)
     need = ress_select_workspace_size(shape)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        workspace = empty(max(need, 1), torch.uint8, dev, stream, output=False)
     ws_bytes = _workspace_bytes(workspace, dev)
     params = ress_select_params(int(rounds), float(rho), float(eps), int(swap_floor), int(bool(dense_special_queries)),
                                 int(criterion), float(cdf_tau), int(bool(pooled_in_workspace)))
@@ -230,7 +232,7 @@ def _sparse_call(fn, name, q, k, v, kept_count, kept_idx, bq, bk, n_special_tail
     if kept_count.numel() != H * n_qb or kept_idx.numel() != H * n_qb * n_kb:
         raise ValueError("kept_count must be [H][n_qb] and kept_idx [H][n_qb][n_kb]")
     if out is None:
-        out = torch.empty(q.shape, dtype=out_dtype, device=q.device)
+        out = empty(q.shape, out_dtype, q.device, stream)
     _check_out("out", out, out_dtype, q.shape, q.device)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     st = fn(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(kept_count), _ptr(kept_idx), float(scale), _ptr(out),
@@ -261,7 +263,7 @@ def ress_dense_attn(q, k, v, *, bq: int, bk: int, n_special_tail: int = 0, scale
     H, N, D = q.shape
     shape = make_shape(H, N, bq=bq, bk=bk, n_special_tail=n_special_tail, D=D)
     if out is None:
-        out = torch.empty_like(q)
+        out = empty(q.shape, q.dtype, q.device, stream)
     _check_out("out", out, torch.bfloat16, q.shape, q.device)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     st = lib.ress_dense_attn(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), float(scale), _ptr(out),
@@ -291,14 +293,14 @@ def ress_qkv_proj_pool(x, w_qkv, gram, *, bq: int, bk: int, n_special_tail: int 
         raise ValueError("x and w_qkv must share a device")
     _check_out("gram", gram, torch.float32, (H, D, D), dev)
     shape = make_shape(H, N, bq=bq, bk=bk, n_special_tail=n_special_tail, D=D)
-    q = torch.empty((H, N, D), dtype=torch.bfloat16, device=dev) if q is None else q
-    k = torch.empty((H, N, D), dtype=torch.bfloat16, device=dev) if k is None else k
-    v = torch.empty((H, N, D), dtype=torch.bfloat16, device=dev) if v is None else v
+    q = empty((H, N, D), torch.bfloat16, dev, stream) if q is None else q
+    k = empty((H, N, D), torch.bfloat16, dev, stream) if k is None else k
+    v = empty((H, N, D), torch.bfloat16, dev, stream) if v is None else v
     for name, t in (("q", q), ("k", k), ("v", v)):
         _check_out(name, t, torch.bfloat16, (H, N, D), dev)
     need = ress_select_workspace_size(shape)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        workspace = empty(max(need, 1), torch.uint8, dev, stream)
     ws_bytes = _workspace_bytes(workspace, dev)
     st = lib.ress_qkv_proj_pool(C.byref(shape), _ptr(x), _ptr(w_qkv), _ptr(q), _ptr(k), _ptr(v), _ptr(gram),
                                 _ptr(workspace), ws_bytes, _stream(stream, dev))
@@ -314,7 +316,7 @@ def ress_out_proj_residual(o, w_o, resid_in, *, resid_out=None, stream=None):
     _check_bf16("o", o, (H, N, D))
     _check_bf16("w_o", w_o, (H * D, H * D))
     _check_bf16("resid_in", resid_in, (N, H * D))
-    resid_out = torch.empty_like(resid_in) if resid_out is None else resid_out
+    resid_out = empty(resid_in.shape, resid_in.dtype, resid_in.device, stream) if resid_out is None else resid_out
     _check_bf16("resid_out", resid_out, (N, H * D))
     if not (w_o.device == resid_in.device == resid_out.device == o.device):
         raise ValueError("o, w_o, resid_in and resid_out must share a device")
@@ -335,7 +337,7 @@ def ress_out_proj_residual_f32(o, w_o, resid_in, *, resid_out=None, stream=None)
     _check_bf16("w_o", w_o, (H * D, H * D))
     dev = o.device
     _check_out("resid_in", resid_in, torch.float32, (N, H * D), dev)
-    resid_out = torch.empty_like(resid_in) if resid_out is None else resid_out
+    resid_out = empty(resid_in.shape, resid_in.dtype, resid_in.device, stream) if resid_out is None else resid_out
     _check_out("resid_out", resid_out, torch.float32, (N, H * D), dev)
     if w_o.device != dev:
         raise ValueError("o and w_o must share a device")
@@ -357,7 +359,7 @@ def ress_block_drift_sq(a, b, gram, *, bq: int, out=None, stream=None):
         _check_out(name, t, torch.float32, (H, N, D), dev)
     _check_out("gram", gram, torch.float32, (H, D, D), dev)
     n_qb = (N + bq - 1) // bq
-    out = torch.empty((H, n_qb), dtype=torch.float64, device=dev) if out is None else out
+    out = empty((H, n_qb), torch.float64, dev, stream) if out is None else out
     _check_out("out", out, torch.float64, (H, n_qb), dev)
     shape = make_shape(H, N, bq=bq, bk=bq, D=D)
     st = lib.ress_block_drift_sq(C.byref(shape), _ptr(a), _ptr(b), _ptr(gram), _ptr(out), _stream(stream, dev))

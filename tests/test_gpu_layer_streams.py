@@ -40,10 +40,32 @@ def _cases(ress):
     }
 
 
-def test_results_beside_pending_work(ress):
+def _base_cases(ress):
+    """The same of the attention path's functions (include/ress.h)."""
+    H, N, kw = 16, 8192, dict(bq=128, bk=128)
+    q, k, v = (_mk(H, N, 64, seed=s) for s in (5, 6, 7))
+    gram = torch.eye(64, device="cuda").expand(H, 64, 64).contiguous()
+    x, wq, wo = _mk(N, H * 64, seed=8), _mk(3 * H * 64, H * 64, seed=9), _mk(H * 64, H * 64, seed=10)
+    xf, a, b = x.float(), q.float(), k.float()
+    sel = ress.ress_select(q, k, v, gram, [20] * H, **kw)
+    kept = sel["kept_count"], sel["kept_idx"]
+    return {
+        "select": lambda **s: ress.ress_select(q, k, v, gram, [20] * H, want_debug=True, **kw, **s),
+        "sparse": lambda **s: {"o": ress.ress_sparse_attn(q, k, v, *kept, **kw, **s)},
+        "sparse_f32": lambda **s: {"o": ress.ress_sparse_attn_out_f32(q, k, v, *kept, **kw, **s)},
+        "dense": lambda **s: {"o": ress.ress_dense_attn(q, k, v, **kw, **s)},
+        "qkv": lambda **s: {n: t for n, t in ress.ress_qkv_proj_pool(x, wq, gram, **kw, **s).items() if n != "workspace"},
+        "out": lambda **s: {"r": ress.ress_out_proj_residual(q, wo, x, **s)},
+        "out_f32": lambda **s: {"r": ress.ress_out_proj_residual_f32(q, wo, xf, **s)},
+        "drift": lambda **s: {"d": ress.ress_block_drift_sq(a, b, gram, bq=128, **s)},
+    }
+
+
+@pytest.mark.parametrize("path", [_cases, _base_cases], ids=["layer", "attention"])
+def test_results_beside_pending_work(ress, path):
     """Blocks just returned by the current stream, whose queue still writes them, are not given to a call on another stream:
     their addresses are others, and results are those of a call alone. (The queue is kept busy by products of known length.)"""
-    cases = _cases(ress)
+    cases = path(ress)
     alone = {n: {k: t.clone() for k, t in f().items() if t is not None} for n, f in cases.items()}
     torch.cuda.synchronize()
     side = torch.cuda.Stream()

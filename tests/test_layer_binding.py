@@ -147,3 +147,60 @@ def test_memory_on_the_current_stream(layer, traced, name, stream):
     fake, _ = traced
     CALLS_ALL[name](layer, stream=stream)
     assert fake.made and fake.on == [7] * len(fake.made) and not any(fake.used)
+
+
+# ----------------------------------------------------- the functions of include/ress.h
+
+
+def _select(r, **kw):
+    q = _z(4, 200, 64)
+    return r.ress_select(q, q, q, _z(4, 64, 64, dtype=F32), [1] * 4, bq=128, bk=128, want_debug=True, **kw)
+
+
+BASE = {
+    "ress_select": _select,
+    "ress_sparse_attn": lambda r, **kw: r.ress_sparse_attn(*[_z(4, 200, 64)] * 3, _z(4, 2, dtype=torch.int32),
+                                                           _z(4, 2, 2, dtype=torch.int32), bq=128, bk=128, **kw),
+    "ress_sparse_attn_out_f32": lambda r, **kw: r.ress_sparse_attn_out_f32(*[_z(4, 200, 64)] * 3, _z(4, 2, dtype=torch.int32),
+                                                                           _z(4, 2, 2, dtype=torch.int32), bq=128, bk=128, **kw),
+    "ress_dense_attn": lambda r, **kw: r.ress_dense_attn(*[_z(4, 200, 64)] * 3, bq=128, bk=128, **kw),
+    "ress_qkv_proj_pool": lambda r, **kw: r.ress_qkv_proj_pool(_z(200, 256), _z(768, 256), _z(4, 64, 64, dtype=F32), bq=128,
+                                                               bk=128, **kw),
+    "ress_out_proj_residual": lambda r, **kw: r.ress_out_proj_residual(_z(4, 200, 64), _z(256, 256), _z(200, 256), **kw),
+    "ress_out_proj_residual_f32": lambda r, **kw: r.ress_out_proj_residual_f32(_z(4, 200, 64), _z(256, 256),
+                                                                               _z(200, 256, dtype=F32), **kw),
+    "ress_block_drift_sq": lambda r, **kw: r.ress_block_drift_sq(_z(4, 200, 64, dtype=F32), _z(4, 200, 64, dtype=F32),
+                                                                 _z(4, 64, 64, dtype=F32), bq=128, **kw),
+}
+
+
+class _Lib:
+    """Entry points that enqueue nothing, and the real sizes."""
+
+    def __init__(self, real):
+        self.real = real
+
+    def __getattr__(self, name):
+        return getattr(self.real, name) if name.endswith("_size") else lambda *a: 0
+
+
+@pytest.mark.parametrize("name", BASE)
+@pytest.mark.parametrize("stream", [_Stream(9), 9], ids=["object", "address"])
+def test_memory_of_the_attention_path_is_the_streams(memory, monkeypatch, name, stream):
+    """The same for the functions of include/ress.h: all that they return is marked as in use on the current stream, the
+    projection's workspace too; the selection's own workspace is not returned."""
+    import paper_2609_35593_amd as r
+
+    fake = _Torch()
+    monkeypatch.setattr(memory, "torch", fake)
+    monkeypatch.setattr(memory, "raw_stream", lambda index: fake.cuda.current)
+    monkeypatch.setattr(r, "lib", _Lib(r.lib))
+    for check in ("_check_qkv", "_check_out", "_check_bf16"):
+        monkeypatch.setattr(r, check, lambda *a: None)
+    monkeypatch.setattr(r, "_workspace_bytes", lambda t, dev: t.numel())
+    if "sparse" in name:
+        monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    BASE[name](r, stream=stream)
+    assert fake.made and fake.on == [9] * len(fake.made) and fake.cuda.current == 7
+    for (_, _, dtype), used in zip(fake.made, fake.used):
+        assert used == ([] if dtype == torch.uint8 and name == "ress_select" else [7])
