@@ -20,7 +20,13 @@ from . import ress_block_drift_sq, ress_sparse_attn_out_f32
 
 def block_masking_change(q, k, v, gram, *, bq: int, bk: int, blocks=None, stream=None) -> np.ndarray:
     """float64 [H][n_qb][len(blocks)]: the masking change of every (head, query
-    block) for each key block in `blocks` (default: every key block)."""
+    block) for each key block in `blocks` (default: every key block). The inputs
+    are ready on `stream` (a torch stream or an address; default: the current one),
+    to which everything here belongs."""
+    if stream is not None:
+        side = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=q.device)
+        with torch.cuda.stream(side):
+            return block_masking_change(q, k, v, gram, bq=bq, bk=bk, blocks=blocks)
     H, N, D = q.shape
     n_qb, n_kb = (N + bq - 1) // bq, (N + bk - 1) // bk
     blocks = list(range(n_kb)) if blocks is None else [int(j) for j in blocks]
@@ -29,7 +35,7 @@ def block_masking_change(q, k, v, gram, *, bq: int, bk: int, blocks=None, stream
     kept_all = every.expand(H, n_qb, n_kb).contiguous()
     count_all = torch.full((H, n_qb), n_kb, dtype=torch.int32, device=dev)
     count_drop = torch.full((H, n_qb), n_kb - 1, dtype=torch.int32, device=dev)
-    base = ress_sparse_attn_out_f32(q, k, v, count_all, kept_all, bq=bq, bk=bk, stream=stream)
+    base = ress_sparse_attn_out_f32(q, k, v, count_all, kept_all, bq=bq, bk=bk)
     masked = torch.empty_like(base)
     M = gram.to(device=dev, dtype=torch.float32).contiguous()
     sq = torch.empty((H, n_qb), dtype=torch.float64, device=dev)
@@ -37,8 +43,8 @@ def block_masking_change(q, k, v, gram, *, bq: int, bk: int, blocks=None, stream
     for col, j in enumerate(blocks):
         lst = torch.cat([every[:j], every[j + 1:], torch.full((1,), -1, dtype=torch.int32, device=dev)])
         kept = lst.expand(H, n_qb, n_kb).contiguous()
-        ress_sparse_attn_out_f32(q, k, v, count_drop, kept, bq=bq, bk=bk, out=masked, stream=stream)
-        ress_block_drift_sq(masked, base, M, bq=bq, out=sq, stream=stream)
+        ress_sparse_attn_out_f32(q, k, v, count_drop, kept, bq=bq, bk=bk, out=masked)
+        ress_block_drift_sq(masked, base, M, bq=bq, out=sq)
         out[:, :, col] = np.sqrt(np.maximum(sq.cpu().numpy(), 0.0))
     return out
 

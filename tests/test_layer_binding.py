@@ -204,3 +204,39 @@ def test_memory_of_the_attention_path_is_the_streams(memory, monkeypatch, name, 
     assert fake.made and fake.on == [9] * len(fake.made) and fake.cuda.current == 7
     for (_, _, dtype), used in zip(fake.made, fake.used):
         assert used == ([] if dtype == torch.uint8 and name == "ress_select" else [7])
+
+
+def test_masking_reference_stays_on_its_stream(monkeypatch):
+    """Lists made, kernels' calls and the copy to the host of block_masking_change all belong to the stream that it is
+    given: made on the current one, its lists and the copy would not wait for the kernels, nor they for the lists."""
+    from paper_2609_35593_amd import masking
+
+    fake, on = _Torch(), []
+
+    def made(name):
+        def f(*a, **kw):
+            on.append((name, fake.cuda.current))
+            return getattr(torch, name)(*a, **kw)
+        return f
+
+    for name in ("arange", "full", "cat", "empty_like"):
+        setattr(fake, name, made(name))
+
+    def attention(q, k, v, count, kept, *, bq, bk, out=None, stream=None):
+        on.append(("attention", stream.cuda_stream if stream is not None else fake.cuda.current))
+        return torch.zeros(q.shape) if out is None else out
+
+    def drift(a, b, gram, *, bq, out, stream=None):
+        on.append(("drift", stream.cuda_stream if stream is not None else fake.cuda.current))
+        return out.fill_(4.0)
+
+    monkeypatch.setattr(masking, "torch", fake)
+    monkeypatch.setattr(masking, "ress_sparse_attn_out_f32", attention)
+    monkeypatch.setattr(masking, "ress_block_drift_sq", drift)
+    q = _z(2, 300, 64)
+    for stream, where in ((_Stream(9), 9), (9, 9), (None, 7)):
+        on.clear()
+        fake.on.clear()
+        r = masking.block_masking_change(q, q, q, _z(2, 64, 64, dtype=F32), bq=128, bk=128, stream=stream)
+        assert r.shape == (2, 3, 3) and (r == 2).all() and fake.cuda.current == 7
+        assert {s for _, s in on} == {where} and set(fake.on) == {where} and len(on) > 10
