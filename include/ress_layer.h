@@ -162,7 +162,8 @@ int ress_window_attn_workspace_size(const ress_window_shape *shape, size_t *byte
  *   lse  device float32 [H][n_q] out, or NULL: the natural logarithm of the sum of
  *        exp(scale q . k) over the visible keys, -inf where there are none
  *   workspace  256-byte aligned; may be NULL where none is needed
- * Pointers 16-byte aligned; scale > 0 and finite. */
+ * Pointers 16-byte aligned; 0 < scale <= 2^120. Logits (scale q . k) may be as large as float32
+ * holds (2^126): a row's weights are those of its largest ones. */
 int ress_window_attn(const ress_window_shape *shape, const void *q, const void *k, const void *v, float scale, void *o,
                      float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
 

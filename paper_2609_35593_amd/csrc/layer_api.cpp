@@ -103,6 +103,9 @@ int check_window(const ress_window_shape *s, bool strides)
     return RESS_OK;
 }
 
+// (Up to 2^120, which leaves the references' unit and most scores room in float32.)
+bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p120f; }
+
 ress::WindowParams window_params(const ress_window_shape *s, float scale)
 {
     ress::WindowParams p;
@@ -122,14 +125,13 @@ ress::WindowParams window_params(const ress_window_shape *s, float scale)
     p.n_kb = (s->n_k + 127) / 128;
     p.scale = scale;
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.refs = ress::references(p.scale_log2);
     p.qs = s->q;
     p.ks = s->k;
     p.vs = s->v;
     p.os = s->o;
     return p;
 }
-
-bool scale_ok(float scale) { return scale > 0.f && isfinite(scale); }
 
 size_t window_workspace(const ress_window_shape *s)
 {

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -73,6 +74,31 @@ struct RopeParams {
     uint8_t pair_of[kMaxChunks], other[kMaxChunks];
 };
 
+// References of softmax rows: the base-2 logit s `scale` of a score s, in one of two forms. A near one
+// is that product, rounded. A far one, from 2^24 on, is s `unit`, the power of two at or above the scale: exact, so that
+// differences from it are, and never below 2^24 itself, so that it tells its form, and references compare as their logits do.
+struct References {
+    float scale, unit, rest;  // rest = scale / unit, in (1/2, 1]
+#ifdef __HIPCC__
+    __device__ __forceinline__ bool far(float ref) const { return !(fabsf(ref) < 0x1p24f); }
+    __device__ __forceinline__ float of(float score) const { return far(score * unit) ? score * unit : score * scale; }
+    __device__ __forceinline__ float base2(float ref) const { return far(ref) ? ref * rest : ref; }
+    // a - b in base 2, each as its form holds it: one rounding, or two of far ones.
+    __device__ __forceinline__ float difference(float a, float b) const
+    {
+        if (far(a)) return far(b) ? (a - b) * rest : fmaf(a, rest, -b);
+        return far(b) ? fmaf(-b, rest, a) : a - b;
+    }
+#endif
+};
+
+inline References references(float scale)
+{
+    int e;
+    const float f = frexpf(scale, &e);  // scale = f 2^e, f in [1/2, 1)
+    return f == 0.5f ? References{scale, scale, 1.f} : References{scale, ldexpf(1.f, e), f};
+}
+
 struct WindowParams {
     int H, H_kv, group;  // group = H / H_kv
     int n_q, n_k, q_offset;
@@ -82,12 +108,13 @@ struct WindowParams {
     int n_qb, n_kb;  // blocks of 128 / groups queries, of 128 keys
     int splits;      // workgroups that share a block's keys (forward)
     float scale, scale_log2;  // of dq and dk; of the logits, in base 2
+    References refs;          // (forward)
     ress_strides qs, ks, vs, os;
     const uint16_t *q, *k, *v;
     uint16_t *o;
     float *lse;
     float *part;        // splits > 1: [splits][H][n_q][64], unnormalised outputs,
-    float2 *part_row;   // and [splits][H][n_q], references and sums
+    float2 *part_row;   // and [splits][H][n_q], references (scores) and sums
 };
 
 // Positions stay below 2^25, so frames and windows beyond 2^26 act as 2^26 does, whose product

@@ -26,6 +26,12 @@
 // row with a key has a sum of at least 1 against its first reference. The running sum is of
 // the float32 probabilities where the logarithm is wanted, else of the bf16-rounded ones
 // that the product with V takes (packed dot products, half the instructions).
+//
+// A weight is exp2(s c - ref), one fma of the score s and its scale c against the scaled reference.
+// That one is rounded, by up to half its step; all weights of a row see the same, and their quotient
+// does not, but from 2^31 on half a step passes the 2^127 that float32 holds. So references of 2^24
+// and more are kept as score times a power of two, exactly, and taken from the scores before the rest
+// of the scale (References in layer_internal.h).
 #include "tiles.h"
 
 namespace ress {
@@ -34,14 +40,13 @@ namespace {
 using namespace tiles;
 
 constexpr float kSumLimit = 0x1p50f;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxSplits = 32;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// exp2(a - top) for a part that holds mass, 0 for one that holds none.
-__device__ __forceinline__ float share(float ref, float sum, float top)
+// exp2(ref - top) for a part that holds mass, 0 for one that holds none.
+__device__ __forceinline__ float share(const References &r, float ref, float sum, float top)
 {
-    return sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+    return sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.difference(ref, top));
 }
 
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
@@ -118,8 +123,8 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
         load_v(key0, lo, hi, s_last.sk, end, vd);
     };
 
-    const float c = p.scale_log2;
-    float ref = 0.f, sum = 0.f;  // reference (base 2) and the lane's half of the row's sum
+    const References r = p.refs;
+    float ref = 0.f, sum = 0.f;  // reference and the lane's half of the row's sum
     bool has = false;            // the row has a reference
     f32x16 acc[2];
 #pragma unroll
@@ -135,7 +140,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
         for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
         if (part) hide(s, key0 + u * 32, sl.lo, (unsigned int)(sl.hi - sl.lo), key0 < sb.sk, sl.sk);
     };
-    // The row's largest logit in the tile.
+    // The row's largest score in the tile, as a reference.
     auto top = [&](bool part, const unsigned char *kt, int key0) __attribute__((always_inline)) {
         float m = -INFINITY;
 #pragma unroll
@@ -145,17 +150,26 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
 #pragma unroll
             for (int v = 0; v < 16; ++v) m = fmaxf(m, s[v]);
         }
-        return fmaxf(m, __shfl_xor(m, 32)) * c;
+        return r.of(fmaxf(m, __shfl_xor(m, 32)));
     };
-    // Probabilities against the row's reference, and the lane's part of their sum.
-    auto probs = [&](bool part, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2]) __attribute__((always_inline)) {
+    // Probabilities against the row's reference, and the lane's part of their sum. (any_far: some rows'
+    // references may be far.)
+    auto probs = [&](bool any_far, bool part, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2])
+                     __attribute__((always_inline)) {
         float l0 = 0.f, l1 = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x16 s;
             scores(part, kt, u, key0, s);
+            if (any_far) {
+                const bool far = r.far(ref);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -ref));
+                for (int v = 0; v < 16; ++v)
+                    s[v] = __builtin_amdgcn_exp2f(far ? fmaf(s[v], r.unit, -ref) * r.rest : fmaf(s[v], r.scale, -ref));
+            } else {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], r.scale, -ref));
+            }
             pack(s, pb[u]);
             if constexpr (LSE) {
 #pragma unroll
@@ -172,14 +186,14 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
         float l;
         // (Rare: a row's first tile, or logits far above those so far. Lanes l and l^32 share the
         // row and decide together.)
-        bool look = __any(!has), far = false;
+        bool look = __any(!has), over = false;
 #pragma nounroll
         for (bool again = false;; again = true) {
             if (look) {
                 const float m = top(part, kt, key0);
-                if (has ? far : m > -INFINITY) {
+                if (has ? over : m > -INFINITY) {
                     const float to = has ? fmaxf(ref, m) : m;
-                    const float a = has ? __builtin_amdgcn_exp2f(ref - to) : 0.f;
+                    const float a = has ? __builtin_amdgcn_exp2f(r.difference(ref, to)) : 0.f;
                     sum *= a;
 #pragma unroll
                     for (int dh = 0; dh < 2; ++dh)
@@ -189,11 +203,18 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
                     has = true;
                 }
             }
-            l = probs(part, kt, key0, pb);
-            far = !(l <= kSumLimit);
-            look = __any(far);
+            l = probs(false, part, kt, key0, pb);
+            over = !(l <= kSumLimit);
+            const bool far = r.far(ref);
+            if (!__any(over || far)) break;
+            if (__any(far)) {
+                asm volatile("" ::: "memory");  // (code of its own: the ordinary form stays in one piece)
+                l = probs(true, part, kt, key0, pb);
+                over = !(l <= kSumLimit);
+            }
+            look = __any(over);
             if (!look || again) break;
-            far = ((int)far | __shfl_xor((int)far, 32)) != 0;
+            over = ((int)over | __shfl_xor((int)over, 32)) != 0;
         }
         sum += l;
 #pragma unroll
@@ -248,14 +269,14 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
             const float *m = area((g - 1) * QW + wave);
             if (m[64] != 0.f) to = fmaxf(to, m[0]);
         }
-        const float a0 = share(ref, sum, to);
+        const float a0 = share(r, ref, sum, to);
         sum *= a0;
 #pragma unroll
         for (int v = 0; v < 32; ++v) acc[v >> 4][v & 15] *= a0;
 #pragma unroll
         for (int g = 1; g < G; ++g) {
             const float *m = area((g - 1) * QW + wave);
-            const float a = share(m[0], m[64], to);
+            const float a = share(r, m[0], m[64], to);
             sum = fmaf(m[64], a, sum);
 #pragma unroll
             for (int v = 0; v < 32; ++v) acc[v >> 4][v & 15] = fmaf(m[(2 + v) * 64], a, acc[v >> 4][v & 15]);
@@ -275,7 +296,7 @@ __global__ void __launch_bounds__(256, G > 1 ? 2 : 4) window_kernel(const Window
         return;
     }
     store_row(p.o + h * p.os.head + (int64_t)t * p.os.token, acc, inverse(sum), hh);
-    if (LSE && hh == 0) p.lse[(int64_t)h * p.n_q + t] = sum == 0.f ? -INFINITY : ref * kLn2 + logf(sum);
+    if (LSE && hh == 0) p.lse[(int64_t)h * p.n_q + t] = sum == 0.f ? -INFINITY : r.base2(ref) * kLn2 + logf(sum);
 }
 
 // A wave a row, a channel a lane: its parts in order, their weights one a lane first. (All of them
@@ -295,7 +316,7 @@ __global__ void __launch_bounds__(256) join_kernel(const WindowParams p)
     float top = r.y == 0.f ? -INFINITY : r.x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float w = share(r.x, r.y, top);
+    const float w = share(p.refs, r.x, r.y, top);
     float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
@@ -305,7 +326,7 @@ __global__ void __launch_bounds__(256) join_kernel(const WindowParams p)
             o = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s)), x[s], o);
     const int64_t h = row / p.n_q, t = row - h * p.n_q;
     p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(o * inverse(sum));
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : p.refs.base2(top) * kLn2 + logf(sum);
 }
 
 template <int G>
