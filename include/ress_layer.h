@@ -213,6 +213,7 @@ int ress_window_attn_decode_workspace_size(const ress_decode_shape *shape, size_
  *              zero output.
  *   q, o       bf16 [B][H][64]
  *   k, v       bf16 caches; nothing at or behind lens[b] has a part in the result
+ *   scale      as for ress_window_attn, logits too
  *   workspace  256-byte aligned */
 int ress_window_attn_decode(const ress_decode_shape *shape, const void *q, const void *k, const void *v,
                             const int32_t *lens, float scale, void *o, void *workspace, size_t workspace_bytes,

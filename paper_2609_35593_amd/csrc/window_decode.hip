@@ -17,6 +17,8 @@
 // 24 streams of 1 to 20,000 keys, 4 K/V heads, window 4,096: 25.1 us, 3.6 TB/s (64 of 8,000: 190, 5.5); one of 16 heads and
 // 6,863 visible keys: 10.9 us. Both kernels are chains of memory round trips (lengths, first turn,
 // partial results) as much as bandwidth.
+#include <float.h>
+
 #include "tiles.h"
 
 namespace ress {
@@ -39,9 +41,10 @@ __device__ __forceinline__ float dot2(unsigned int a, unsigned int b, float c)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
 }
 
-// The reference of a part without keys: below every logit, and finite, so that its weight and
-// that of a masked key are 0 without a test.
-constexpr float kNone = -1e30f;
+// References are scores before their scale: what a scaled one's rounding takes, all of a weight from 2^31 on, is
+// not taken here. A part without keys has one at or below every score, and finite: its sums are 0 without a
+// test, whatever their weight, and masked keys (-inf) have none.
+constexpr float kNone = -FLT_MAX;
 
 // Sum over the 8 lanes of a key, the same in each.
 template <int CTRL>
@@ -102,6 +105,7 @@ __global__ void __launch_bounds__(64 * kHeadWaves) decode_kernel(const DecodePar
     const uint16_t *kb = p.k + b * p.k_batch + h * p.ks.head + ch * 8;
     const uint16_t *vb = p.v + b * p.v_batch + h * p.vs.head + ch * 8;
 
+    const float c = p.scale_log2;
     float m = kNone, l = 0.f, acc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
@@ -127,18 +131,18 @@ __global__ void __launch_bounds__(64 * kHeadWaves) decode_kernel(const DecodePar
             float d = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) d = dot2(kx[i][e], q[e], d);
-            d = sum8(d) * p.scale_log2;
+            d = sum8(d);
             s[i] = t * 32 + i * 8 + oct < vis.n ? d : -INFINITY;
             top = fmaxf(top, s[i]);
         }
-        const float a = __builtin_amdgcn_exp2f(m - top);
+        const float a = __builtin_amdgcn_exp2f((m - top) * c);
         m = top;
         l *= a;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] *= a;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float w = __builtin_amdgcn_exp2f(s[i] - top);
+            const float w = __builtin_amdgcn_exp2f((s[i] - top) * c);
             l += w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -151,7 +155,7 @@ __global__ void __launch_bounds__(64 * kHeadWaves) decode_kernel(const DecodePar
     float top = m;
 #pragma unroll
     for (int o = 8; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float a = __builtin_amdgcn_exp2f(m - top);
+    const float a = __builtin_amdgcn_exp2f((m - top) * c);
     l *= a;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= a;
@@ -175,7 +179,7 @@ __global__ void __launch_bounds__(64 * kHeadWaves) decode_kernel(const DecodePar
     for (int w = 0; w < kHeadWaves; ++w) top = fmaxf(top, lds[w][0]);
 #pragma unroll
     for (int w = 0; w < kHeadWaves; ++w) {
-        const float x = __builtin_amdgcn_exp2f(lds[w][0] - top);
+        const float x = __builtin_amdgcn_exp2f((lds[w][0] - top) * c);
         sum = fmaf(lds[w][1], x, sum);
         o = fmaf(lds[w][2 + lane], x, o);
     }
@@ -258,9 +262,9 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) decode_tile_kernel(const D
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, s[u][v]);
         }
-        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)) * c, m);
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
         if (__any(top > m)) {
-            const float a = __builtin_amdgcn_exp2f(m - top);
+            const float a = __builtin_amdgcn_exp2f((m - top) * c);
             sum *= a;
 #pragma unroll
             for (int dh = 0; dh < 2; ++dh)
@@ -273,7 +277,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) decode_tile_kernel(const D
             bf16x8 pb[2], rest[2];
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                s[u][v] = __builtin_amdgcn_exp2f(fmaf(s[u][v], c, -m));
+                s[u][v] = __builtin_amdgcn_exp2f((s[u][v] - m) * c);
                 sum += s[u][v];
             }
             pack(s[u], pb);
@@ -322,7 +326,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) decode_tile_kernel(const D
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part(w)[r]);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float a = __builtin_amdgcn_exp2f(part(w)[r] - top);
+            const float a = __builtin_amdgcn_exp2f((part(w)[r] - top) * c);
             l = fmaf(part(w)[kStep + r], a, l);
             o = fmaf(part(w)[(2 + lane) * kStep + r], a, o);
         }
@@ -349,7 +353,7 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
     float top = m;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) top = fmaxf(top, __shfl_xor(top, e));
-    const float w = __builtin_amdgcn_exp2f(m - top);
+    const float w = __builtin_amdgcn_exp2f((m - top) * p.scale_log2);
     sum *= w;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);

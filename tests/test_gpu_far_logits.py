@@ -109,3 +109,44 @@ def test_forward_scales(ress, scale):
     o, _, w = _reference(q, k, v, vis, scale)
     R.within(ress.ress_window_attn(q, k, v, window=200, n_sink=5, scale=scale)["o"], o,
              2.0 ** -8 * (w + 2 * o.abs()) + 2.0 ** -12 * w, "o")
+
+
+def _decode(ress, q, k, v, lens, kw, scale=None):
+    """The output, and o and sum p |v| of every sequence's last position."""
+    t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = ress.ress_window_attn_decode(q, k, v, t, scale=scale, **kw)
+    ref = []
+    for i, n in enumerate(lens):
+        vis = R.visible(1, n, n - 1, 1, kw["window"], kw["n_sink"], True, device="cuda")
+        o, _, w = _reference(q[i][:, None], k[i, :, :n], v[i, :, :n], vis, 0.125 if scale is None else scale)
+        ref.append((o[:, 0], w[:, 0]))
+    return got, torch.stack([o for o, _ in ref]), torch.stack([w for _, w in ref])
+
+
+# B, H, H_kv, capacity, window, n_sink: a head a K/V head and shared ones, in one workgroup and cut over several
+CACHES = [(3, 2, 2, 400, 300, 5), (1, 4, 4, 9000, 9000, 0), (3, 8, 2, 400, 300, 5), (1, 40, 1, 9000, 5000, 64)]
+
+
+@pytest.mark.parametrize("power", [8, 20, 28, 32, 40, 64, 110])
+@pytest.mark.parametrize("cache", CACHES)
+def test_decode(ress, cache, power):
+    """As in the forward pass; references are taken from the scores, so weights are 1 at any size, and no weight is rounded
+    to bf16 (2^-16 of it at most is lost)."""
+    B, H, H_kv, cap, window, n_sink = cache
+    say(f"[far decode] {cache} 2^{power}")
+    q, k, v = _whole(11, power // 2, B, H), _whole(12, power - power // 2, B, H_kv, cap), _values(13, B, H_kv, cap)
+    got, o, w = _decode(ress, q, k, v, [cap - 7 * i for i in range(B)], dict(window=window, n_sink=n_sink))
+    R.within(got, o, 2.0 ** -8 * o.abs() + 2.0 ** -16 * w, "o")
+    # All logits far below zero: the least of them are the largest.
+    got, o, w = _decode(ress, -q.abs(), k.abs() + k.abs().amax(), v, [cap - 7 * i for i in range(B)],
+                        dict(window=window, n_sink=n_sink))
+    R.within(got, o, 2.0 ** -8 * o.abs() + 2.0 ** -16 * w, "o, all far below zero")
+
+
+@pytest.mark.parametrize("scale", [1e35, 2e30, 2.0 ** 27, 1e-38, 1e-44])
+@pytest.mark.parametrize("cache", CACHES)
+def test_decode_scales(ress, cache, scale):
+    B, H, H_kv, cap, window, n_sink = cache
+    q, k, v = _whole(14, 0, B, H), _whole(15, 0, B, H_kv, cap), _values(16, B, H_kv, cap)
+    got, o, w = _decode(ress, q, k, v, [cap - 7 * i for i in range(B)], dict(window=window, n_sink=n_sink), scale)
+    R.within(got, o, 2.0 ** -8 * o.abs() + 2.0 ** -12 * w, "o")
