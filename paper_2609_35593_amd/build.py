@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libress.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_api.cpp",
-           "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_api.cpp"]
+           "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_plan.cpp", "layer_api.cpp"]
 HEADERS = [os.path.join(CSRC, "ress_internal.h"), os.path.join(CSRC, "layer_internal.h"), os.path.join(CSRC, "tiles.h"),
            os.path.join(HERE, "..", "include", "ress.h"), os.path.join(HERE, "..", "include", "ress_layer.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -99,6 +99,8 @@ inline References references(float scale)
     return f == 0.5f ? References{scale, scale, 1.f} : References{scale, ldexpf(1.f, e), f};
 }
 
+constexpr int kMaxSplits = 32;  // workgroups that share a block's or sequence's keys, whose parts one wave joins
+
 struct WindowParams {
     int H, H_kv, group;  // group = H / H_kv
     int n_q, n_k, q_offset;
@@ -170,6 +172,8 @@ struct DecodeParams {
     float *part;  // [B][H][splits][66]: reference, sum, output
 };
 
+constexpr int kHeadWaves = 8;  // of decode_kernel (us with 4 / 8: 16 heads of 6,870 keys 10.5 / 9.3)
+constexpr int kTileWaves = 4;  // of decode_tile_kernel: 64 KiB of slots, two workgroups a CU
 int decode_splits(const ress_decode_shape *s);
 
 hipError_t launch_norm(const NormParams &p, hipStream_t s);

@@ -446,10 +446,6 @@ hipError_t by_type(const P &p, const void *xs, const void *xs2, const void *ys, 
 
 }  // namespace
 
-// 512 workgroups of 8 waves fill the chip (128 registers a lane), and their partial sums of
-// 1,024 channels are 4 MB. (1,024 for narrow rows: 175,872 of 64 bf16 channels 19.9 -> 22.8 us.)
-int norm_bwd_parts(int64_t rows) { return (int)(rows < 1 ? 1 : rows < 512 ? rows : 512); }
-
 hipError_t launch_norm(const NormParams &p, hipStream_t s) { return by_type(p, p.x, p.x, p.y, p.gamma, p.beta, s); }
 
 hipError_t launch_norm_bwd(const NormBwdParams &p, hipStream_t s)

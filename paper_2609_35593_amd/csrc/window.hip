@@ -40,7 +40,6 @@ namespace {
 using namespace tiles;
 
 constexpr float kSumLimit = 0x1p50f;
-constexpr int kMaxSplits = 32;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // exp2(ref - top) for a part that holds mass, 0 for one that holds none.
@@ -346,54 +345,6 @@ hipError_t go(const WindowParams &p, hipStream_t s)
 }
 
 }  // namespace
-
-WindowPlan window_plan(const ress_window_shape *s)
-{
-    // Tiles a block sees at most, and one in the middle of the queries.
-    const int64_t window = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2);
-    const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k;
-    const int64_t keys = window + 128 + sinks < s->n_k ? window + 128 + sinks : s->n_k;
-    const int64_t middle = (int64_t)s->q_offset + s->n_q / 2, reach = s->causal && middle < s->n_k ? middle : s->n_k;
-    const int64_t tiles = (keys + 63) / 64, tiles_mid = (window + sinks < reach ? window + sinks : reach) / 64;
-    auto blocks = [&](int g) { return (int64_t)s->H * (((int64_t)s->n_q * g + 127) / 128); };
-    const int64_t n = blocks(1);
-    // (In the comments, G/S us: with G key groups, blocks cut over S workgroups.)
-    WindowPlan plan = {1, 1};
-    if (tiles < 2 || n >= 1200) return plan;
-    // From 512 workgroups of 128 queries on, two a CU, key groups only cost (640 blocks of 18 tiles 1/1
-    // 44, 2/1 47; 1,264 80 / 97), but for frames of many tiles: blocks on a frame's edge see one frame
-    // more and finish late (688 blocks of one frame of 1,374 104 / 81, 1,032 140 / 113, 1,376 148 / 133 and
-    // with sinks 186 / 192; of frames of 250 752 30 / 41).
-    if (n >= 512) {
-        if (s->frame >= 768) plan.groups = 2;
-        return plan;
-    }
-    plan.groups = 2;  // (352 blocks of 87 1/1 197, 2/1 155, 4/1 243; 18 of 3 13 / 7.3 / 8.5)
-    if (n > 64) {
-        // Long lists: cut, to balance the load of four workgroups a CU, where that outweighs the partial
-        // results (268 blocks of 65 2/1 109, 1/4 83; 176 of 118 96 / 76; 88 of 172 119, 1/8 62; 192 of 58
-        // 49, 1/4 49; 142 of 47 42 / 42).
-        if (tiles_mid >= 56) plan = {1, n >= 128 ? 4 : 8};
-        return plan;
-    }
-    if (n >= 8 && tiles >= 40) {
-        // About a workgroup a CU, of 8 tiles at least (47 blocks of 94 4/1 38, 2/5 25; 22 of 63 4/2 23, 2/8
-        // 19; 24 of 47 18, 2/5 15).
-        const int64_t want = 240 / n;
-        plan.splits = (int)(want < tiles / 8 ? want : tiles / 8);
-    } else if (tiles >= 8) {
-        // Four groups (one workgroup a CU, by its LDS), with tiles enough for each: 64 blocks of 9 13.4 /
-        // 9.4 / 9.2. Few blocks: workgroups to fill the CUs, each with two tiles a group at least: one
-        // of 625 203 -> 22 with 32.
-        plan.groups = 4;
-        if (n > 0) {
-            int64_t want = 256 / blocks(4);
-            if (want > tiles / 8) want = tiles / 8;
-            plan.splits = (int)(want < 1 ? 1 : want > kMaxSplits ? kMaxSplits : want);
-        }
-    }
-    return plan;
-}
 
 hipError_t launch_window(const WindowParams &p, int groups, hipStream_t s)
 {

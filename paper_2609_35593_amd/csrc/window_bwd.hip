@@ -405,52 +405,6 @@ __global__ void __launch_bounds__(256) join_kernel(const WindowBwdParams b, int 
 
 }  // namespace
 
-WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
-{
-    WindowBwdPlan r = {1, 0, 1, 1, 0};
-    // dq: four key groups where their workgroups still are one a CU and see 8 tiles, else two while
-    // there are fewer blocks than fill the chip four times over (whole pass in us with 1 / 2 / 4 groups:
-    // 63 blocks over 2,000 keys 76 / 56 / 52, 128 over 1,000 65 / 53 / 65, 640 over 512 116 / 107 / 173,
-    // 1,376 over three frames of 1,374 848 / 850 / 1,183).
-    const int64_t window = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2);
-    const int64_t q_blocks = (int64_t)s->H * (((int64_t)s->n_q + 127) / 128);
-    const int64_t seen = window + 128 + s->n_sink < s->n_k ? window + 128 + s->n_sink : s->n_k;
-    r.groups = q_blocks <= 64 && seen > 7 * 64 ? 4 : q_blocks < 1024 ? 2 : 1;
-    const int64_t blocks = (s->n_k + 127) / 128;
-    if (s->H_kv == 0 || blocks == 0) return r;
-    const int64_t sinks = s->n_sink < s->n_k ? s->n_sink : s->n_k, group = s->H / s->H_kv;
-    r.sink_blocks = (int)((sinks + 127) / 128);
-    // Tiles of queries in a list at most: of sinks, and of other keys.
-    const int64_t span = window_tokens(s->frame, s->window) * (s->causal ? 1 : 2) + at_most_2_26(s->frame) + 127;
-    const int64_t all = ((int64_t)s->n_q + 63) / 64;
-    const int64_t some = span < s->n_q ? (span + 63) / 64 + 1 : all;
-    const int64_t t_sink = group * all, t_win = group * (some < all ? some : all);
-    const int64_t sb = r.sink_blocks, wb = blocks - sb;
-    const double total = (double)s->H_kv * (sb * t_sink + wb * t_win);
-    // The slices that the following estimate (us) favours: a tile takes 1.3 in a workgroup that has
-    // a CU to itself, 1.8 in one of two, the chip 1 / 290 per tile when full; a slice's sums cost
-    // 0.03 to write and add up, the join 4. Measured, whole pass, uncut / as chosen here: 12 heads
-    // for 4 of 3,001 tokens, 5 sinks, 225 / 62; 16 for 4 of 5,000, 4 sinks, 474 / 100; 6 for 2 of 700,
-    // 20 sinks, 63 / 28; 16 of 1,374, uncut 64, in halves 69.
-    double best = 1e30;
-    for (int ss = 1; ss <= (sb ? 64 : 1); ss *= 2)
-        for (int ws = 1; ws <= (wb ? 16 : 1); ws *= 2) {
-            if (ss > t_sink || ws > t_win) continue;
-            const double items = (double)s->H_kv * (sb * ss + wb * ws);
-            const double cut = (double)s->H_kv * ((ss > 1 ? sb * ss : 0) + (ws > 1 ? wb * ws : 0));
-            const int64_t l_sink = sb ? (t_sink + ss - 1) / ss : 0, l_win = wb ? (t_win + ws - 1) / ws : 0;
-            const double alone = (double)(l_sink > l_win ? l_sink : l_win) * (items <= 256 ? 1.3 : 1.8);
-            const double cost = (alone > total / 290 ? alone : total / 290) + (cut > 0 ? 4 + 0.03 * cut : 0);
-            if (cost < best) {
-                best = cost;
-                r.sink_slices = ss;
-                r.slices = ws;
-            }
-        }
-    r.items = (int)(sb * r.sink_slices + wb * r.slices);
-    return r;
-}
-
 hipError_t launch_window_bwd(const WindowBwdParams &b, int groups, hipStream_t s)
 {
     const WindowParams &p = b.w;

@@ -28,7 +28,6 @@ using namespace tiles;
 
 typedef unsigned int u32x4 __attribute__((__vector_size__(16)));
 
-constexpr int kMaxSplits = 32;
 constexpr int kPart = 66;  // floats of a partial result: reference, sum, 64 channels
 
 __device__ __forceinline__ float lo_f(unsigned int x) { return __builtin_bit_cast(float, x << 16); }
@@ -73,9 +72,6 @@ __device__ __forceinline__ Visible visible(const DecodeParams &p, int b)
     v.n = v.sk + len - v.lo;
     return v;
 }
-
-constexpr int kHeadWaves = 8;  // of decode_kernel (us with 4 / 8: 16 heads of 6,870 keys 10.5 / 9.3)
-constexpr int kTileWaves = 4;  // of decode_tile_kernel: 64 KiB of slots, two workgroups a CU
 
 // A head's channel `lane` of a workgroup: the output, or its part of it.
 __device__ __forceinline__ void finish(const DecodeParams &p, int b, int h, int split, int lane, float top, float sum, float o)
@@ -366,29 +362,6 @@ __global__ void __launch_bounds__(256) join_kernel(const DecodeParams p)
 }
 
 }  // namespace
-
-// Workgroups per sequence and K/V head (or 32 of its heads).
-int decode_splits(const ress_decode_shape *s)
-{
-    if (s->B == 0 || s->H == 0 || s->capacity == 0) return 1;
-    const int64_t seen = window_tokens(s->frame, s->window) + s->n_sink;
-    const int64_t keys = seen < s->capacity ? seen : s->capacity;  // at least 1
-    const int group = s->H / s->H_kv;
-    const bool one = group == 1;
-    const int64_t heads = (int64_t)s->B * s->H_kv * ((group + 31) / 32);
-    // One head: enough for 4 workgroups a CU, none with less than 256 keys (us with at least 256 /
-    // 512 / 1,024 keys, the join counted: 16 heads of 6,870 9.6 / 9.3 / 10.8; one of 40,000 10.6 with 32
-    // splits; 32 heads of 300 7.4 / 5.1 / 5.2). Several: one a CU, of at least a turn a wave (us: 96 of
-    // 4,160 keys, 1 / 2 / 5 / 8 splits 29.6 / 23.3 / 23.8 / 25.2; 32 of 4,000, 4 / 8 / 16 14.2 / 11.7 / 12.0;
-    // 4 of 8,000, 8 / 16 / 32 12.4 / 10.0 / 8.9). One workgroup up to 512 keys: a join costs more.
-    const int64_t turns = one ? (keys + 31) / 32 : (keys + 63) / 64, waves = one ? kHeadWaves : kTileWaves;
-    const int64_t want = (one ? 1024 : 256) / heads, most = keys <= 512 ? 1 : (turns + waves - 1) / waves;
-    int64_t n = want < most ? want : most;
-    n = n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n;
-    // No more than give every wave the same turns: 10 splits of 3.25 turns a wave take as long as 8 of 4.
-    const int64_t each = (turns + n * waves - 1) / (n * waves);
-    return (int)((turns + each * waves - 1) / (each * waves));
-}
 
 hipError_t launch_decode(const DecodeParams &p, hipStream_t s)
 {
