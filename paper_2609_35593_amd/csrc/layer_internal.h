@@ -157,6 +157,8 @@ struct WindowBwdPlan {
     int sink_blocks, sink_slices, slices, items;
 };
 WindowBwdPlan window_bwd_plan(const ress_window_shape *s);
+// Of `blocks` blocks of keys those whose lists are cut: how many, from block `first` on.
+int window_bwd_joined(const WindowBwdPlan &p, int blocks, int &first);
 
 struct DecodeParams {
     int B, H, H_kv, group;

@@ -106,6 +106,12 @@ WindowBwdPlan window_bwd_plan(const ress_window_shape *s)
     return r;
 }
 
+int window_bwd_joined(const WindowBwdPlan &p, int blocks, int &first)
+{
+    first = p.sink_slices > 1 ? 0 : p.sink_blocks;
+    return (p.slices > 1 ? blocks : p.sink_slices > 1 ? p.sink_blocks : first) - first;
+}
+
 // ---------------------------------------------------------------- decode
 
 // Workgroups per sequence and K/V head (or 32 of its heads).

@@ -376,11 +376,11 @@ __global__ void __launch_bounds__(256, 2) dkv_kernel(const WindowBwdParams b)
 }
 
 // Blocks of keys whose list was cut: a workgroup 32 keys of dk (even) or dv, 2 x 4 channels a
-// thread, the slices in order. blockIdx.y counts the cut blocks of all heads.
-__global__ void __launch_bounds__(256) join_kernel(const WindowBwdParams b, int cut)
+// thread, the slices in order. blockIdx.y counts the cut blocks of all heads, `cut` of a head from `first` on.
+__global__ void __launch_bounds__(256) join_kernel(const WindowBwdParams b, int first, int cut)
 {
     const WindowParams &p = b.w;
-    const int hk = blockIdx.y / cut, block = blockIdx.y % cut;
+    const int hk = blockIdx.y / cut, block = first + blockIdx.y % cut;
     const int slices = block < b.sink_blocks ? b.sink_slices : b.slices;
     const int at = hk * b.items + (block < b.sink_blocks
                                        ? block * b.sink_slices
@@ -421,9 +421,10 @@ hipError_t launch_window_bwd(const WindowBwdParams &b, int groups, hipStream_t s
     if (p.n_k > 0) {
         hipLaunchKernelGGL(dkv_kernel, dim3(8u * (unsigned)((p.H_kv * b.items + 7) / 8)), dim3(256), 0, s, b);
         if (hipError_t e = hipGetLastError()) return e;
-        const int cut = b.slices > 1 ? p.n_kb : b.sink_slices > 1 ? b.sink_blocks : 0;
-        if (cut) {
-            hipLaunchKernelGGL(join_kernel, dim3(8, (unsigned)(p.H_kv * cut)), dim3(256), 0, s, b, cut);
+        int first = 0;
+        const int cut = window_bwd_joined({groups, b.sink_blocks, b.sink_slices, b.slices, b.items}, p.n_kb, first);
+        if (cut > 0) {
+            hipLaunchKernelGGL(join_kernel, dim3(8, (unsigned)(p.H_kv * cut)), dim3(256), 0, s, b, first, cut);
             return hipGetLastError();
         }
     }

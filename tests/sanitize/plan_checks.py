@@ -28,6 +28,13 @@ def size(fn, s):
     return n.value
 
 
+def joined(sinks, sink_slices, slices, blocks):
+    """The blocks whose slices the join adds up."""
+    first = C.c_int(0)
+    n = lib.plan_joined(sinks, sink_slices, slices, blocks, C.byref(first))
+    return range(first.value, first.value + n)
+
+
 def window(H, H_kv, n_q, n_k, off, frame, win, sink, causal):
     x = ress_strides(64 << 24, 64)
     s = ress_window_shape(H, H_kv, n_q, n_k, 64, off, frame, win, sink, causal, x, x, x, x)
@@ -56,8 +63,8 @@ def window(H, H_kv, n_q, n_k, off, frame, win, sink, causal):
     # Every slice of a list that was cut has a tile; blocks that were cut fit a grid's second dimension.
     all_tiles = (n_q + 63) // 64 * (H // H_kv)
     assert sink_slices <= max(all_tiles, 1) and slices <= max(all_tiles, 1), what
-    cut = blocks if slices > 1 else sinks if sink_slices > 1 else 0
-    assert H_kv * cut <= 65535, what
+    cut = joined(sinks, sink_slices, slices, blocks)
+    assert H_kv * len(cut) <= 65535, what
     need = size(lib.ress_window_attn_bwd_workspace_size, s)
     rows = (H * n_q * 4 + 255) // 256 * 256
     assert need == 2 * rows + (H_kv * items * 2 * 128 * 64 * 4 if sink_slices > 1 or slices > 1 else 0), what
@@ -111,6 +118,11 @@ for (H, H_kv), B, cap in itertools.product(HEADS, (0, 1, 24, 65535), (0,) + edge
 for _ in range(20000):
     H, H_kv = rng.choice(HEADS)
     decode(spread(65535), H, H_kv, spread(TOKENS), max(spread(TOP), 1), max(spread(TOP), 1), spread(TOP))
+# The join reads the sums that a cut block's slices left, so it covers the blocks that were cut and no other, of any plan:
+# the others' gradients are written at once, and their part of the workspace is not.
+for sinks, rest, sink_slices, slices in itertools.product((0, 1, 3), (0, 1, 5), (1, 2, 64), (1, 2, 16)):
+    cut = [b for b in range(sinks + rest) if (sink_slices if b < sinks else slices) > 1]
+    assert list(joined(sinks, sink_slices, slices, sinks + rest)) == cut, (sinks, rest, sink_slices, slices)
 for rows in (0, 1, 2, 511, 512, 513, TOP):
     assert lib.plan_norm_bwd(rows) == min(max(rows, 1), 512)
 assert seen["groups"] == {(1, False), (1, True), (2, False), (2, True), (4, False), (4, True)}, seen["groups"]

@@ -23,6 +23,10 @@ void plan_window_bwd(const ress_window_shape *s, int *out)
     const ress::WindowBwdPlan p = ress::window_bwd_plan(s);
     out[0] = p.groups, out[1] = p.sink_blocks, out[2] = p.sink_slices, out[3] = p.slices, out[4] = p.items;
 }
+int plan_joined(int sink_blocks, int sink_slices, int slices, int blocks, int *first)
+{
+    return ress::window_bwd_joined({1, sink_blocks, sink_slices, slices, 0}, blocks, *first);
+}
 int plan_decode(const ress_decode_shape *s) { return ress::decode_splits(s); }
 int plan_norm_bwd(int64_t rows) { return ress::norm_bwd_parts(rows); }
 }
