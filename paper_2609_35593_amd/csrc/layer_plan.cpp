@@ -23,12 +23,19 @@ WindowPlan window_plan(const ress_window_shape *s)
     // (In the comments, G/S us: with G key groups, blocks cut over S workgroups.)
     WindowPlan plan = {1, 1};
     if (tiles < 2 || n >= 1200) return plan;
-    // From 512 workgroups of 128 queries on, two a CU, key groups only cost (640 blocks of 18 tiles 1/1
-    // 44, 2/1 47; 1,264 80 / 97), but for frames of many tiles: blocks on a frame's edge see one frame
-    // more and finish late (688 blocks of one frame of 1,374 104 / 81, 1,032 140 / 113, 1,376 148 / 133 and
-    // with sinks 186 / 192; of frames of 250 752 30 / 41).
+    // From 512 workgroups of 128 queries on, two a CU, key groups cost (640 blocks of 18 tiles 1/1 44, 2/1
+    // 47; 688 of 172 308 / 354), but where a few blocks see much more than the others and finish late:
+    // those on the edge of a large frame, one frame more. For that, edges lie inside blocks (688 blocks,
+    // one frame of 1,024 36 / 43, of 1,000 78 / 68), not every key is in reach (688, two of 3,000 and
+    // 2,504 158 / 121, both in reach 126 / 143), and the frame is long beside what all the blocks take:
+    //   516-528 blocks: one of 776 48-49 / 44-50, of 850 53 / 46-52, of 900 54-56 / 50, of 1,374 93 / 67
+    //   784-864: ratios, of 900 1.03-1.11, of 1,000 0.90-0.97, of 1,374 0.83-0.94
+    //   992-1,120: of 1,000 0.95-1.09, of 1,200 1.02-1.11, of 1,374 0.79-1.00
+    // and from 1,200 blocks on no more (1,264, three of 1,374 212 / 217, 1,632 279 / 287).
     if (n >= 512) {
-        if (s->frame >= 768) plan.groups = 2;
+        const bool edges = s->frame % 128 || s->q_offset % 128;
+        const int least = n < 768 ? 850 : n < 896 ? 1000 : 1300;
+        if (edges && window + sinks < s->n_k && s->frame >= least) plan.groups = 2;
         return plan;
     }
     plan.groups = 2;  // (352 blocks of 87 1/1 197, 2/1 155, 4/1 243; 18 of 3 13 / 7.3 / 8.5)

@@ -123,6 +123,23 @@ for _ in range(20000):
 for sinks, rest, sink_slices, slices in itertools.product((0, 1, 3), (0, 1, 5), (1, 2, 64), (1, 2, 16)):
     cut = [b for b in range(sinks + rest) if (sink_slices if b < sinks else slices) > 1]
     assert list(joined(sinks, sink_slices, slices, sinks + rest)) == cut, (sinks, rest, sink_slices, slices)
+def groups_of(H, n, frame, win, off=0, sink=0, causal=1, n_k=None):
+    x = ress_strides(64, 64)
+    out = (C.c_int * 5)()
+    lib.plan_window(C.byref(ress_window_shape(H, H, n, n_k or n + off, 64, off, frame, win, sink, causal, x, x, x, x)), out)
+    return out[0]
+
+
+# Two key groups from 512 blocks on are for blocks on a frame's edge, which see a frame more than the others: not without
+# edges inside blocks, nor where every key is in reach (there they cost 5 to 26%).
+for H, n in ((16, 4200), (8, 11008), (16, 5504), (16, 7904), (16, 8960)):
+    assert groups_of(H, n, 1374, 1) == 2 and groups_of(H, n, 1374, 1, off=1374, n_k=n + 1374) == 2, (H, n)
+    for frame in (768, 896, 1024, 1280, 2048):
+        assert groups_of(H, n, frame, 1) == 1, (H, n, frame)
+    assert groups_of(H, n, 2048, 1, off=100) == 2, (H, n)  # (edges inside blocks)
+    for frame, win, causal in ((TOP, TOP, 0), (TOP, 1, 1), (n, 1, 0), (n // 2, 2, 1), (3000, 4, 1), (1374, n, 0)):
+        assert groups_of(H, n, frame, win, causal=causal) == 1, (H, n, frame, win)
+    assert groups_of(H, n, 1374, 1, sink=n - 1000) == 1, (H, n)
 for rows in (0, 1, 2, 511, 512, 513, TOP):
     assert lib.plan_norm_bwd(rows) == min(max(rows, 1), 512)
 assert seen["groups"] == {(1, False), (1, True), (2, False), (2, True), (4, False), (4, True)}, seen["groups"]

@@ -24,11 +24,13 @@ CUTS = [
     (12, 4, 1374, 5496, 4122, 1374, 4, 1374, True),  # a view over three others, one key group, over 4
     (16, 16, 1374, 6870, 5496, 1374, 4, 1374, True),
 ]
-# Two key groups at 512 to 1,199 blocks: frames of 768 tokens and more.
+# 512 to 1,199 blocks: two key groups where edges of large frames lie inside blocks, else one (frames of 768, all in reach).
 FRAMES = [
     (64, 16, 1100, 1100, 0, 1000, 1, 0, True),
-    (64, 64, 1100, 2500, 1100, 800, 2, 100, True),
-    (64, 64, 1600, 1600, 0, 800, 1, 5, False),
+    (64, 64, 1100, 2500, 1100, 930, 2, 100, True),
+    (32, 8, 2100, 2900, 500, 1010, 1, 5, False),
+    (64, 64, 1100, 2500, 1024, 768, 2, 100, True),
+    (64, 64, 1600, 1600, 0, 1600, 1, 5, False),
     (64, 8, 1000, 2000, 1000, 1000, 1, 700, True),
 ]
 # Lists of queries in many slices: of sinks alone, of all.
