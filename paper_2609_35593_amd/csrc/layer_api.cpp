@@ -424,8 +424,9 @@ int ress_window_attn_bwd(const ress_window_shape *shape, const ress_window_grads
     if (need && (!workspace || ws_bytes < need || !aligned(workspace, 256))) return RESS_E_WORKSPACE;
     ress::WindowBwdParams b;
     b.w = window_params(shape, scale);
-    // Where no query sees more than one key, its probability is 1 whatever the logit: dq and dk are
-    // 0, not what rounding leaves of d_o v^T - delta.
+    // A query that sees one key has a probability of 1 whatever the logit, and dq and dk are 0 by the
+    // formula. In these two calls, of no other query, they are written so; elsewhere such a query leaves in
+    // them what float32 leaves of d_o v^T - delta.
     if (shape->n_k == 1 || (shape->frame == 1 && shape->window == 1 && shape->n_sink == 0)) b.w.scale = 0.f;
     b.w.q = static_cast<const uint16_t *>(q);
     b.w.k = static_cast<const uint16_t *>(k);

@@ -90,3 +90,32 @@ def test_results_beside_pending_work(ress, path):
         for k, t in alone[n].items():
             assert torch.equal(got[k], t), (n, k)
         say(f"[streams] {n}")
+
+
+def test_captured_on_a_forked_stream(ress):
+    """Calls on a second stream inside a capture, outputs and workspaces made inside: replays, with eager calls of the same
+    between them, give the eager bits."""
+    cases = _cases(ress)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(**s):
+        return [(n, k, t) for n, f in cases.items() for k, t in f(**s).items() if t is not None]
+
+    for s in (main, side):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=main):
+        side.wait_stream(main)
+        out = step(stream=side)
+        main.wait_stream(side)
+    for rep in range(3):
+        for _, _, t in out:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for (n, k, t), (_, _, e) in zip(out, step()):
+            assert torch.equal(t, e), (n, k, rep)

@@ -41,6 +41,8 @@ SLICES = [
     (4, 1, 2000, 200, 0, 1, 2000, 64, True),
     (2, 1, 5000, 600, 0, 1, 6000, 0, True),
 ]
+# One key a query, by the sinks or the first position alone: dq and dk are what float32 leaves of 0.
+ONE = [(2, 2, 100, 64, 500, 1, 3, 1, True), (4, 2, 1, 50, 0, 1, 7, 0, True)]
 
 
 @pytest.fixture(scope="module")
@@ -70,7 +72,7 @@ def test_forward(ress, shape):
     assert torch.equal(ress.ress_window_attn(q, k, v, workspace=ws, **kw)["o"], r2)
 
 
-@pytest.mark.parametrize("shape", CUTS[-2:] + FRAMES + SLICES)
+@pytest.mark.parametrize("shape", CUTS[-2:] + FRAMES + SLICES + ONE)
 def test_backward(ress, shape):
     H, H_kv, n_q, n_k = shape[:4]
     say(f"[plans bwd] {shape}")
