@@ -56,7 +56,8 @@ typedef struct {
 
 /* y = (x - mean) rstd gamma + beta over the channels of every row, with
  * mean = sum(x) / width and rstd = 1 / sqrt(sum((x - mean)^2) / width + eps), in
- * float32 (the variance from centred values), rounded once to y's type. For
+ * float32 (the variance from centred values), rounded once to y's type (values up to
+ * 2^56: float32 holds no sum of squares of larger ones). For
  * instance the residual stream before ress_qkv_proj_pool, or the heads of Q and K
  * (width 64).
  *   gamma, beta  device float32 [width], or NULL (1, 0)
@@ -121,7 +122,8 @@ typedef struct {
  *   q_in, q_out   [H][N][D] by shape->q and shape->q_out; NULL where H is 0
  *   k_in, k_out   [H_kv][N][D] likewise; NULL where H_kv is 0
  * An output may be its input where the strides are equal (in place); strides may
- * place k_out in a cache. */
+ * place k_out in a cache. The pooled state that ress_qkv_proj_pool leaves is of Q and K as
+ * they were projected: ress_select of turned ones takes pooled_in_workspace = 0. */
 int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in, const void *k_in, void *q_out,
               void *k_out, hipStream_t stream);
 
@@ -181,7 +183,9 @@ int ress_window_attn_bwd_workspace_size(const ress_window_shape *shape, size_t *
  * dk and dv summed over the query heads that share them. bf16 products, float32
  * accumulation; p and ds rounded to bf16 for their products, outputs once. (delta is
  * first taken from d_o . o; what the rounding of o leaves in it is summed beside dq
- * in float32 and taken out of all three.)
+ * in float32 and taken out of all three. p is off by some 2^-22 |lse| of itself, as lse is
+ * float32: less than its rounding for logits up to 10^4; from some 10^7 on, where lse no longer
+ * tells one key from another, gradients mean nothing and may be infinite or NaN.)
  *   o, lse      as ress_window_attn wrote them (o by shape->o)
  *   dq, dk, dv  bf16 out by the strides of `grads`; dk and dv of keys that no query
  *               sees are zero

@@ -328,7 +328,7 @@ hipError_t go_rows(const NormParams &p, hipStream_t s)
 }
 
 // Two rows of float32 in flight where that still leaves workgroups for two fillings of the chip
-// (43,968 rows of 1,024 channels 48.0 -> 44.8 us; 21,984 bf16 ones 16.2 -> 19.2).
+// (43,968 rows of 1,024 channels 55.0 -> 52.1 us; 100,000 bf16 ones 88.8 -> 100.3).
 template <typename XT, typename YT, int VEC, int LPR, int K>
 hipError_t go(const NormParams &p, hipStream_t s)
 {

@@ -16,16 +16,19 @@
 // joins take the parts in order.
 //
 // Bound by issue slots beside the matrix unit: 16 heads of 32 frames of 1,374 tokens, window 4 and
-// a frame of sinks, 1,236 us (939 TFLOP/s, 79% of a large library product's rate; matrix unit
-// busy 48% of the cycles, vector unit 63%; no bank conflicts). 10,001 tokens, window 1,024, 16 heads
-// for 4: 67-75 us, of which some 25 are the last fifth of a filling (1,264 workgroups for 1,024 places).
+// a frame of sinks, 1,239-1,300 us (892-936 TFLOP/s, 75-78% of a large library product's rate; matrix unit
+// busy 48% of the cycles, vector unit 62%; no bank conflicts). 10,001 tokens, window 1,024, 16 heads
+// for 4: 67-77 us, of which some 25 are the last fifth of a filling (1,264 workgroups for 1,024 places).
 //
 // Softmax: base 2, against a reference per row that is the row's largest logit in the
 // first tile where it sees a key, and moves (O and the sum rescaled) only when a tile's
 // sum exceeds 2^50; so a tile costs no maximum, float32 keeps every digit of the sum, and a
 // row with a key has a sum of at least 1 against its first reference. The running sum is of
 // the float32 probabilities where the logarithm is wanted, else of the bf16-rounded ones
-// that the product with V takes (packed dot products, half the instructions).
+// that the product with V takes (packed dot products, half the instructions). Those are rounded because
+// the matrix unit takes bf16: outputs are 7e-4 to 1e-3 off in norm for it, up to 2e-3 where rows see few
+// keys, beside 1.7e-3 by their own rounding; a second product for what is left of each weight, as
+// decode affords, would make the products half again as many.
 //
 // A weight is exp2(s c - ref), one fma of the score s and its scale c against the scaled reference.
 // That one is rounded, by up to half its step; all weights of a row see the same, and their quotient

@@ -23,9 +23,10 @@
 // initial value of the accumulator.
 //
 // Bound by issue slots beside the matrix unit, as the forward pass: 16 heads of 8 frames of 1,374
-// tokens, window 3 and a frame of sinks, dq 405 us and dkv 427 (the 8 products at 965 TFLOP/s, 81% of
-// a large library product's rate; matrix unit busy 51%, vector unit 46 and 42%). 3,001 tokens, 12
-// heads for 4, 5 sinks: 56-59 us in three launches of short lists.
+// tokens, window 3 and a frame of sinks, 833-855 us, dq and dkv about half each (the 8 products at 941-966
+// TFLOP/s, 79-81% of a large library product's rate; matrix unit busy 51%, vector unit 46 and 42%). 3,001
+// tokens, 12 heads for 4, 5 sinks: 56-60 us in three launches of short lists. P and dS are rounded to
+// bf16 for the matrix unit: gradients are 2.3e-3 off in norm, 1.7e-3 by their own rounding alone.
 #include "tiles.h"
 
 namespace ress {

@@ -5,7 +5,8 @@ As in the package's other functions, a function carries its C entry point's name
 checks tensor metadata, allocates outputs (and workspaces) with torch when the caller
 passes none, and passes pointers and the current stream of the tensors' device, or the
 caller's `stream` (a torch stream or an address; that its inputs are ready there, and its
-outputs before they are used elsewhere, is the caller's to order)."""
+outputs before they are used elsewhere, is the caller's to order). Nothing is recorded
+for autograd: gradients are the calls ending in _bwd and the inverse of ress_rope."""
 from __future__ import annotations
 
 import ctypes as C
@@ -182,8 +183,8 @@ def ress_layer_norm_bwd_workspace_size(rows: int, width: int) -> int:
 def ress_layer_norm_bwd(dy, x, gamma, mean, rstd, *, dx=None, dgamma=None, dbeta=None, want_weights: bool = True,
                         workspace=None, stream=None) -> dict:
     """Gradients of ress_layer_norm (see include/ress_layer.h). dy: of y's type; x, mean, rstd: as given to
-    and made by the forward pass. Returns dx (of x's type) and, with want_weights, dgamma and dbeta
-    (float32 [width])."""
+    and made by the forward pass. Returns dx (of x's type and with its row stride; given, it may be a slice of
+    a packed gradient) and, with want_weights, dgamma and dbeta (float32 [width])."""
     dev, dims = _device("x", x), x.shape
     rows, xs, xt = _norm_view("x", x, dims, dev)
     _, ys, yt = _norm_view("dy", dy, dims, dev)
@@ -216,7 +217,8 @@ def ress_rope(q, k, pos, *, dims, layout: str = "split", base: float = 100.0, in
     """Rotary positions of q [H][N][D] and k [H_kv][N][D] (either may be None; any strides with contiguous
     channels) by pos int32 [N][axes] (see include/ress_layer.h). dims: channels of each axis; layout: "split",
     "interleaved" or "sections"; inverse: turn back (the pass of the gradients). Outputs may be the inputs (in
-    place). Returns q and k."""
+    place). Returns q and k. (ress_select of turned ones pools them itself: the state in ress_qkv_proj_pool's
+    workspace is of those that it wrote.)"""
     first = q if q is not None else k
     if first is None:
         raise ValueError("one of q and k must be given")
