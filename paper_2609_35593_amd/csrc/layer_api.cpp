@@ -4,55 +4,26 @@
 #include <math.h>
 #include <string.h>
 
-#include "layer_internal.h"
+#include "checks.h"
 
 namespace {
 
-constexpr int64_t kMaxTokenStride = 1 << 22;       // 63 rows of it in bytes fit 31 bits
-constexpr int64_t kMaxStride = (int64_t)1 << 46;   // times 2^16 rows stays in 63 bits
+using namespace ress;
+
 constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int kHead = 64;
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-bool aligned(const void *ptr, size_t to) { return ((uintptr_t)ptr & (to - 1)) == 0; }
-bool dtype_ok(int t) { return t == RESS_DTYPE_BF16 || t == RESS_DTYPE_F32; }
-size_t dtype_size(int t) { return t == RESS_DTYPE_F32 ? 4 : 2; }
-
-// [n][m] rows of `width` elements, `outer` and `inner` apart, that do not overlap: one
-// dimension lies whole between two steps of the other.
-bool disjoint(int64_t n, int64_t outer, int64_t m, int64_t inner, int64_t width)
+// Chunks of `per` channels, aligned to their size in every head and token.
+bool rope_aligned(const ress_rope_shape &s, int per, const void *const (&src)[2], void *const (&dst)[2])
 {
-    if (n <= 1 && m <= 1) return true;
-    if (m <= 1) return outer >= width;
-    if (n <= 1) return inner >= width;
-    return (inner >= width && outer >= (m - 1) * inner + width) || (outer >= width && inner >= (n - 1) * outer + width);
-}
-
-bool strides_ok(const ress_strides &s, int64_t multiple)
-{
-    return s.head >= 0 && s.head <= kMaxStride && s.token >= 0 && s.token <= kMaxTokenStride && s.head % multiple == 0 &&
-           s.token % multiple == 0;
-}
-
-// Chunks of `per` channels, aligned to their size in every head and token, that hold whole runs of
-// one side of the pairs (or whole pairs, interleaved).
-bool rope_chunks(const ress_rope_shape &s, int per, int turned, const void *const (&src)[2], void *const (&dst)[2])
-{
-    if (s.D % per || s.D / per > ress::kMaxChunks) return false;
     const size_t bytes = per * dtype_size(s.dtype);
     const ress_strides *st[4] = {&s.q, &s.q_out, &s.k, &s.k_out};
     for (int i = 0; i < 2; ++i)
         if ((i ? s.H_kv : s.H) > 0 && (!aligned(src[i], bytes) || !aligned(dst[i], bytes) || !strides_ok(*st[2 * i], per) ||
                                        !strides_ok(*st[2 * i + 1], per)))
             return false;
-    if (s.layout == RESS_ROPE_SECTIONS) return turned % (2 * per) == 0;
-    if (s.layout == RESS_ROPE_INTERLEAVED) return turned % per == 0;
-    for (int a = 0; a < s.n_axes; ++a)
-        if (s.dims[a] % (2 * per)) return false;
     return true;
 }
-
-bool same(const ress_strides &a, const ress_strides &b) { return a.head == b.head && a.token == b.token; }
 
 // ---------------------------------------------------------------- layer norm
 
@@ -80,15 +51,6 @@ bool norm_alias_ok(const void *out, int out_dtype, int64_t out_stride, const voi
 
 // ------------------------------------------------------------------- windows
 
-int check_heads(int H, int H_kv)
-{
-    if (H < 0 || H_kv < 0) return RESS_E_INVALID_ARG;
-    if (H > RESS_MAX_HEADS) return RESS_E_UNSUPPORTED;
-    if (H_kv == 0 ? H != 0 : H % H_kv != 0) return RESS_E_INVALID_ARG;
-    if (H == 0 && H_kv != 0) return RESS_E_INVALID_ARG;
-    return RESS_OK;
-}
-
 int check_window(const ress_window_shape *s, bool strides)
 {
     if (!s) return RESS_E_INVALID_ARG;
@@ -102,9 +64,6 @@ int check_window(const ress_window_shape *s, bool strides)
         return RESS_E_INVALID_ARG;
     return RESS_OK;
 }
-
-// (Up to 2^120, which leaves the references' unit and most scores room in float32.)
-bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p120f; }
 
 ress::WindowParams window_params(const ress_window_shape *s, float scale)
 {
@@ -259,18 +218,8 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
 {
     if (!shape) return RESS_E_INVALID_ARG;
     const ress_rope_shape &s = *shape;
-    if (s.H < 0 || s.H_kv < 0 || s.N < 0 || s.D < 2 || s.D % 2 || s.n_axes < 1 || !dtype_ok(s.dtype) ||
-        s.layout < RESS_ROPE_SPLIT || s.layout > RESS_ROPE_SECTIONS || !(s.base >= 1.0) || !isfinite(s.base))
-        return RESS_E_INVALID_ARG;
-    if (s.H > RESS_MAX_HEADS || s.H_kv > RESS_MAX_HEADS || s.N > RESS_MAX_TOKENS || s.D > RESS_MAX_ROPE_D ||
-        s.n_axes > RESS_MAX_ROPE_AXES)
-        return RESS_E_UNSUPPORTED;
-    int turned = 0;
-    for (int a = 0; a < s.n_axes; ++a) {
-        if (s.dims[a] < 0 || s.dims[a] % 2 || s.dims[a] > s.D) return RESS_E_INVALID_ARG;
-        turned += s.dims[a];
-    }
-    if (turned > s.D) return RESS_E_INVALID_ARG;
+    int turned = 0, st = check_rope(s, turned);
+    if (st != RESS_OK) return st;
     const ress_strides *in[2] = {&s.q, &s.k}, *out[2] = {&s.q_out, &s.k_out};
     const void *src[2] = {q_in, k_in};
     void *dst[2] = {q_out, k_out};
@@ -287,50 +236,11 @@ int ress_rope(const ress_rope_shape *shape, const int32_t *pos, const void *q_in
     }
     if (s.H + s.H_kv == 0 || s.N == 0) return RESS_OK;
 
-    // The pairs: axis, turns a position, channels. Copied channels pair up behind them.
     ress::RopeParams p;
     memset(&p, 0, sizeof p);
-    int n = 0, at = 0;
-    const double two_pi = 6.283185307179586476925;
-    for (int a = 0; a < s.n_axes; ++a) {
-        for (int i = 0; i < s.dims[a] / 2; ++i, ++n) {
-            p.axis[n] = (uint8_t)a;
-            if (s.layout == RESS_ROPE_SECTIONS) {
-                p.turns[n] = pow(s.base, -2.0 * n / turned) / two_pi;
-                p.ca[n] = (uint8_t)n;
-                p.cb[n] = (uint8_t)(n + turned / 2);
-            } else {
-                const bool inter = s.layout == RESS_ROPE_INTERLEAVED;
-                p.turns[n] = pow(s.base, -2.0 * i / s.dims[a]) / two_pi;
-                p.ca[n] = (uint8_t)(at + (inter ? 2 * i : i));
-                p.cb[n] = (uint8_t)(at + (inter ? 2 * i + 1 : i + s.dims[a] / 2));
-            }
-        }
-        at += s.dims[a];
-    }
-    p.interleaved = s.layout == RESS_ROPE_INTERLEAVED;
-    for (int i = 0; n < s.D / 2; ++i, ++n) {
-        p.turns[n] = -1.0;
-        p.ca[n] = (uint8_t)(turned + 2 * i);
-        p.cb[n] = (uint8_t)(turned + 2 * i + 1);
-    }
     for (int per = (int)(16 / size); per >= (int)(8 / size) && !p.chunk; per /= 2)
-        if (rope_chunks(s, per, turned, src, dst)) p.chunk = per;
-    for (int c = 0; p.chunk && c < s.D / p.chunk; ++c) p.other[c] = (uint8_t)c;
-    for (int i = 0; p.chunk && i < turned / 2; ++i) {
-        const int a = p.ca[i] / p.chunk, b = p.cb[i] / p.chunk;
-        if (p.ca[i] % p.chunk == 0) p.pair_of[a] = (uint8_t)i, p.other[a] = (uint8_t)b;
-        if (p.cb[i] % p.chunk == 0) p.pair_of[b] = (uint8_t)i, p.other[b] = (uint8_t)a;
-    }
-    p.H = s.H;
-    p.H_all = s.H + s.H_kv;
-    p.N = s.N;
-    p.n_axes = s.n_axes;
-    p.n_pairs = s.D / 2;
-    p.D = s.D;
-    p.turned = turned;
-    p.f32 = s.dtype == RESS_DTYPE_F32;
-    p.inverse = s.inverse != 0;
+        if (rope_chunks(s, per, turned) && rope_aligned(s, per, src, dst)) p.chunk = per;
+    rope_tables(s, turned, p);
     p.pos = pos;
     p.q_in = q_in;
     p.k_in = k_in;
