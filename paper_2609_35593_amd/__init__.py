@@ -378,3 +378,7 @@ def bf16_from_bits(bits: np.ndarray, device) -> torch.Tensor:
 from .layer import (ress_layer_norm, ress_layer_norm_bwd, ress_layer_norm_bwd_workspace_size, ress_rope,  # noqa: E402
                     ress_window_attn, ress_window_attn_bwd, ress_window_attn_bwd_workspace_size,
                     ress_window_attn_decode, ress_window_attn_decode_workspace_size, ress_window_attn_workspace_size)
+# Keys and values in pages (include/ress_pages.h).
+from .pages import (ress_page_tables, ress_paged_attn, ress_paged_attn_workspace_size, ress_pages_release,  # noqa: E402
+                    ress_pages_release_workspace_size, ress_qk_norm_rope, ress_qk_norm_rope_bwd,
+                    ress_qk_norm_rope_bwd_workspace_size, ress_qk_norm_rope_pages)

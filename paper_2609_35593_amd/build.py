@@ -11,9 +11,11 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libress.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_api.cpp",
-           "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_plan.cpp", "layer_api.cpp"]
-HEADERS = [os.path.join(CSRC, "ress_internal.h"), os.path.join(CSRC, "layer_internal.h"), os.path.join(CSRC, "tiles.h"),
-           os.path.join(HERE, "..", "include", "ress.h"), os.path.join(HERE, "..", "include", "ress_layer.h")]
+           "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_plan.cpp", "layer_api.cpp",
+           "heads.hip", "pages.hip", "paged_tile.hip", "pages_plan.cpp", "pages_api.cpp"]
+HEADERS = [os.path.join(CSRC, h) for h in ("ress_internal.h", "layer_internal.h", "tiles.h", "checks.h", "pages_internal.h",
+                                            "paged_device.h")]
+HEADERS += [os.path.join(HERE, "..", "include", h) for h in ("ress.h", "ress_layer.h", "ress_pages.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-ffp-contract=fast",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,121 @@
+// What the kernels of attention over pages share: which sequence a block of rows is of, what its
+// rows see, and how its keys are cut.
+#pragma once
+
+#include "pages_internal.h"
+#include "tiles.h"
+
+namespace ress {
+namespace paged {
+
+using namespace tiles;
+
+// Rows that keys which are not to be read come from.
+__device__ const uint16_t zero_row[64] __attribute__((aligned(128))) = {};
+
+// A block: `left` rows (token t, head hk group + g; t outer) of sequence b from head g0 of its token t0 on. The
+// sequence's tokens begin at row cu of q, the first one's position is pos0.
+struct Block {
+    int b, t0, g0, left, cu, pos0, len;
+};
+// Row j of a block: token of the sequence, head of the K/V head's.
+struct Row {
+    int t, g;
+};
+__device__ __forceinline__ Row row_of(const PagedParams &p, const Block &x, int j)
+{
+    const int n = p.groups(x.g0 + j);
+    return {x.t0 + n, x.g0 + j - n * p.group};
+}
+
+// Block `index` of all sequences' blocks of ROWS rows; false behind the last. Every thread of a
+// workgroup of 256 calls it. (Offsets are clamped, so a block's rows lie in [0, N) whatever they hold.)
+template <int ROWS>
+__device__ __forceinline__ bool find_block(const PagedParams &p, int index, Block &x)
+{
+    __shared__ int found[3], ends[4];
+    constexpr int kMost = 1 << 29;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int before = 0;
+    if (threadIdx.x == 0) found[0] = -1;
+    for (int b0 = 0; b0 < p.B; b0 += 256) {
+        const int b = b0 + threadIdx.x;
+        int cu = 0, blocks = 0;
+        if (b < p.B) {
+            cu = min(max(p.cu_q[b], 0), p.N);
+            const int end = min(max(p.cu_q[b + 1], cu), p.N);
+            blocks = (int)(((int64_t)(end - cu) * p.group + ROWS - 1) / ROWS);
+        }
+        int sum = blocks;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(sum, o);
+            if (lane >= o) sum = min(sum + y, kMost);
+        }
+        if (lane == 63) ends[wave] = sum;
+        __syncthreads();
+        int head = before;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) head = min(head + ends[w], kMost);
+            before = min(before + ends[w], kMost);
+        }
+        sum = min(sum + head, kMost);
+        if (blocks > 0 && index < sum && index >= sum - blocks) {
+            found[0] = b;
+            found[1] = index - (sum - blocks);
+            found[2] = cu;
+        }
+        __syncthreads();
+        if (before > index) break;
+    }
+    if (p.B > 0) x.b = __builtin_amdgcn_readfirstlane(found[0]);
+    if (p.B == 0 || x.b < 0) return false;
+    x.cu = __builtin_amdgcn_readfirstlane(found[2]);
+    const int end = min(max(p.cu_q[x.b + 1], x.cu), p.N), n = end - x.cu;
+    x.len = min(max(p.lens[x.b], 0), p.capacity);
+    x.pos0 = x.len - n;
+    const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane(found[1]) * ROWS, rows = (int64_t)n * p.group;
+    x.t0 = (int)((uint32_t)first / (uint32_t)p.group);  // (2^24 tokens of 256 heads at most)
+    x.g0 = (int)(first - (int64_t)x.t0 * p.group);
+    x.left = (int)(rows - first < ROWS ? rows - first : ROWS);
+    return true;
+}
+
+// The keys that position pos of a sequence of len tokens sees: [lo, hi) and [0, sk). (Before its first: none.)
+__device__ __forceinline__ Seen seen_at(const PagedParams &p, int pos, int len)
+{
+    Seen s = {0, 0, 0};
+    if (pos < 0) return s;
+    const int f = p.frames(pos);
+    s.hi = min((f + 1) * p.frame, len);
+    s.lo = min(max((f - p.window + 1) * p.frame, 0), s.hi);
+    s.sk = min(p.n_sink, s.hi);
+    return s;
+}
+
+// The 64-key tiles that any row of a block sees, numbered through: [0, ns) and [w0, w1).
+struct Tiles {
+    int ns, w0, n;
+    __device__ __forceinline__ int key(int i) const { return (i < ns ? i : i - ns + w0) * kTile; }
+};
+__device__ __forceinline__ Tiles tiles_of(const Seen &first, const Seen &last)
+{
+    Tiles t;
+    t.ns = (last.sk + kTile - 1) / kTile;
+    int w1 = (last.hi + kTile - 1) / kTile;
+    t.w0 = first.lo / kTile;
+    if (first.lo >= last.hi) t.w0 = w1 = t.ns;
+    if (t.w0 < t.ns) t.w0 = t.ns;
+    if (w1 < t.w0) w1 = t.w0;
+    t.n = t.ns + w1 - t.w0;
+    return t;
+}
+
+// Workgroups that share a block of n tiles, each with `least` at least.
+__device__ __forceinline__ int cuts_of(const PagedParams &p, int n, int least)
+{
+    return max(1, min(p.splits, n / least));
+}
+
+}  // namespace paged
+}  // namespace ress

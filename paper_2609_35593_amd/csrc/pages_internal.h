@@ -1,0 +1,101 @@
+// Internal declarations shared by the kernels and the C ABI layer of ress_pages.h.
+#pragma once
+
+#include "layer_internal.h"
+#include "ress_pages.h"
+
+namespace ress {
+
+// The norm of heads with the rotation. r: tables, sizes, pos and strides as in rope.hip (q_in, k_in,
+// q_out, k_out are this pass's inputs and outputs; r.chunk: 0 for pairs).
+struct HeadNormParams {
+    RopeParams r;
+    bool layer;  // subtract the mean
+    float eps;
+    const float *gamma[2], *beta[2];  // of Q and K; null: 1, 0
+    // Into pages (slots not null): k_out and v_out are pages, behind K's heads come V's.
+    const int32_t *slots;
+    int n_slots;
+    Divider pages;  // of the tokens of a page
+    int page;
+    const void *v_in;
+    void *v_out;
+    ress_strides vi;
+    ress_page_strides kp, vp;
+};
+
+struct HeadNormBwdParams {
+    RopeParams r;  // q_in, k_in: the gradients of the outputs; q_out, k_out: those of the inputs
+    bool layer;
+    float eps;
+    const float *gamma[2];
+    const void *x[2];  // the forward pass's inputs
+    ress_strides xs[2];
+    float *part;    // [parts][4][D]: gamma and beta of Q, of K; null: not wanted
+    int parts;
+    float *sums[4]; // outputs, each may be null
+};
+
+// Workgroups of the backward pass: over tokens, over heads. A function of the shape alone, whatever
+// the alignment: both kinds of its kernels take 256 / lanes tokens a workgroup in turn.
+constexpr int kHeadParts = 1024;
+struct HeadBwdPlan {
+    int tokens, heads;  // workgroups over tokens; heads a workgroup
+    int parts;
+};
+HeadBwdPlan head_bwd_plan(int H_all, int N, int D);
+
+struct TableParams {
+    int B, N, page, n_pages, max_pages;
+    Divider pages;  // of page
+    int64_t stride;
+    const int32_t *lens, *new_lens, *free_pages, *n_free;
+    int32_t *tables, *lens_out, *n_free_out, *cu_q, *slots, *pos, *n_refused;
+};
+
+struct ReleaseParams {
+    int B, n_pages, max_pages;
+    int64_t stride;
+    bool clear;
+    const int32_t *first, *last, *n_free;
+    int32_t *tables, *free_pages, *n_free_out;
+    int32_t *counts;  // [B + 1]: entries given back, then the stack's height
+};
+
+// Attention over pages. A block is `rows` rows (new token, query head of a K/V head) of one
+// sequence, computed together: 128 by paged_wide.hip's kernel, 32 by paged_tile.hip's.
+struct PagedParams {
+    int B, N, H, H_kv, group;
+    int page, n_pages, max_pages, capacity;  // capacity: tokens that a table holds
+    int frame, window, n_sink;               // (frame, window: see sights)
+    Divider frames, pages, groups;           // of frame, page, group
+    int64_t table_stride;
+    int blocks;  // of all sequences, at most
+    int splits;  // workgroups that share a block's keys, at most
+    References refs;
+    float scale, scale_log2;
+    ress_strides qs, os;
+    ress_page_strides ks, vs;
+    const uint16_t *q, *k, *v;
+    const int32_t *cu_q, *lens, *tables;
+    uint16_t *o;
+    float *lse;
+    float *part;      // splits > 1: [splits][H][N][64], unnormalised outputs,
+    float2 *part_row; // [splits][H][N], references and sums,
+    int32_t *cuts;    // and [H][N], the workgroups that share a row's keys
+};
+
+struct PagedPlan {
+    int rows;    // of a block
+    int blocks, splits;
+};
+PagedPlan paged_plan(const ress_paged_shape *s);
+constexpr int kMaxPagedSplits = 64;
+
+hipError_t launch_head_norm(const HeadNormParams &p, hipStream_t s);
+hipError_t launch_head_norm_bwd(const HeadNormBwdParams &p, hipStream_t s);
+hipError_t launch_tables(const TableParams &p, hipStream_t s);
+hipError_t launch_release(const ReleaseParams &p, hipStream_t s);
+hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s);
+
+}  // namespace ress

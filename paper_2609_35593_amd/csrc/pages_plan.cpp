@@ -1,0 +1,37 @@
+// How the kernels of ress_pages.h spread over the chip: functions of a shape alone. Plain host code,
+// apart from the kernels, so that it runs without a GPU.
+#include "pages_internal.h"
+
+namespace ress {
+
+HeadBwdPlan head_bwd_plan(int H_all, int N, int D)
+{
+    HeadBwdPlan r = {0, 0, 0};
+    if (H_all == 0 || N == 0) return r;
+    // Workgroups over tokens, of 2,048 channels of a head at least, and over heads while there are few.
+    const int64_t tokens = ((int64_t)N * D + 2047) / 2048;
+    r.tokens = (int)(tokens < kHeadParts ? tokens : kHeadParts);
+    int cuts = kHeadParts / r.tokens;
+    if (cuts > H_all) cuts = H_all;
+    r.heads = (H_all + cuts - 1) / cuts;
+    r.parts = r.tokens * ((H_all + r.heads - 1) / r.heads);
+    return r;
+}
+
+PagedPlan paged_plan(const ress_paged_shape *s)
+{
+    PagedPlan r = {32, 0, 1};
+    if (s->B == 0 || s->N == 0 || s->H == 0) return r;
+    // A sequence leaves at most one block that is not full.
+    const int64_t group = s->H / s->H_kv, rows = s->N * group, some = s->B < s->N ? s->B : s->N;
+    r.blocks = (int)((rows + some * (r.rows - 1)) / r.rows);
+    const int64_t capacity = (int64_t)s->max_pages * s->page;
+    int64_t keys = window_tokens(s->frame, s->window) + s->n_sink + r.rows / group;
+    if (keys > capacity) keys = capacity;
+    const int64_t tiles = (keys + 63) / 64, most = tiles / 4, want = 1024 / ((int64_t)r.blocks * s->H_kv);
+    const int64_t n = want < most ? want : most;
+    r.splits = (int)(n < 1 ? 1 : n > kMaxPagedSplits ? kMaxPagedSplits : n);
+    return r;
+}
+
+}  // namespace ress
