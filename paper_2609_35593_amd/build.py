@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libress.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_api.cpp",
            "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_plan.cpp", "layer_api.cpp",
-           "heads.hip", "pages.hip", "paged_tile.hip", "pages_plan.cpp", "pages_api.cpp"]
+           "heads.hip", "pages.hip", "paged_tile.hip", "paged_wide.hip", "pages_plan.cpp", "pages_api.cpp"]
 HEADERS = [os.path.join(CSRC, h) for h in ("ress_internal.h", "layer_internal.h", "tiles.h", "checks.h", "pages_internal.h",
                                             "paged_device.h")]
 HEADERS += [os.path.join(HERE, "..", "include", h) for h in ("ress.h", "ress_layer.h", "ress_pages.h")]

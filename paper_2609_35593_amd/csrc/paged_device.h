@@ -111,6 +111,19 @@ __device__ __forceinline__ Tiles tiles_of(const Seen &first, const Seen &last)
     return t;
 }
 
+// Scores of keys that are not there become -inf: bit 8 (v / 4) + v % 4 of `bits` tells of score v. (By masks in vector registers:
+// sixteen conditions held as scalars made the kernels spill.)
+__device__ __forceinline__ void drop(f32x16 &s, unsigned int bits)
+{
+    asm volatile("" : "+v"(bits));  // (formed here each time, else the masks are kept over the caller's loops)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int there = (int)(bits << (31 - ((v >> 2) * 8 + (v & 3)))) >> 31;
+        const float x = s[v];  // (the bit cast of a vector's element in place reads its first one)
+        s[v] = __builtin_bit_cast(float, (__builtin_bit_cast(int, x) & there) | (~there & (int)0xff800000));
+    }
+}
+
 // Workgroups that share a block of n tiles, each with `least` at least.
 __device__ __forceinline__ int cuts_of(const PagedParams &p, int n, int least)
 {

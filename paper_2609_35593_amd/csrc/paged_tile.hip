@@ -112,12 +112,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams 
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) s[u] = mfma(k[u][kk], qf[kk], s[u]);
             if (part) hide(s[u], key0 + u * 32, sl.lo, (unsigned int)(sl.hi - sl.lo), key0 < sb.sk, sl.sk);
-            if (keys != ~(uint64_t)0) {
-                const unsigned int bits = (unsigned int)(keys >> (32 * u)) >> (4 * hh);
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (!(bits >> ((v >> 2) * 8 + (v & 3)) & 1)) s[u][v] = -INFINITY;
-            }
+            if (keys != ~(uint64_t)0) drop(s[u], (unsigned int)(keys >> (32 * u)) >> (4 * hh));
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, s[u][v]);
         }
@@ -206,8 +201,16 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams 
     }
 }
 
+// References of parts: scores (WIDE = false), or in wide_kernel's form.
+template <bool WIDE>
+__device__ __forceinline__ float share(const PagedParams &p, float ref, float top)
+{
+    return __builtin_amdgcn_exp2f(WIDE ? p.refs.difference(ref, top) : (ref - top) * p.scale_log2);
+}
+
 // A wave a row, a channel a lane: its parts in order, their weights one a lane first. Rows outside every
 // sequence, and those that one workgroup finished, are left as they are.
+template <bool WIDE>
 __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
 {
     const int64_t rows = (int64_t)p.H * p.N, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -221,7 +224,7 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
     float top = r.y == 0.f ? kNone : r.x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float w = r.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((r.x - top) * p.scale_log2);
+    const float w = r.y == 0.f ? 0.f : share<WIDE>(p, r.x, top);
     float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
@@ -234,21 +237,27 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
             if (s0 + s < n) o = fmaf(__shfl(w, s0 + s), y[s], o);
     }
     p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(sum == 0.f ? 0.f : o / sum);
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : top * p.scale + logf(sum);
+    if (p.lse && lane == 0)
+        p.lse[row] = sum == 0.f ? -INFINITY : (WIDE ? p.refs.base2(top) * 0.6931471805599453f : top * p.scale) + logf(sum);
 }
 
 }  // namespace
 
 hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
 {
-    (void)rows;
-    hipLaunchKernelGGL(tile_kernel, dim3((unsigned)p.blocks, (unsigned)p.H_kv, (unsigned)p.splits), dim3(64 * kWaves), 0, s, p);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (p.splits > 1) {
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(((int64_t)p.H * p.N + 3) / 4)), dim3(256), 0, s, p);
-        return hipGetLastError();
+    if (rows == 128) {
+        if (hipError_t e = launch_paged_wide(p, s)) return e;
+    } else {
+        hipLaunchKernelGGL(tile_kernel, dim3((unsigned)p.blocks, (unsigned)p.H_kv, (unsigned)p.splits), dim3(64 * kWaves), 0, s, p);
+        if (hipError_t e = hipGetLastError()) return e;
     }
-    return hipSuccess;
+    if (p.splits == 1) return hipSuccess;
+    const dim3 grid((unsigned)(((int64_t)p.H * p.N + 3) / 4));
+    if (rows == 128)
+        hipLaunchKernelGGL((join_kernel<true>), grid, dim3(256), 0, s, p);
+    else
+        hipLaunchKernelGGL((join_kernel<false>), grid, dim3(256), 0, s, p);
+    return hipGetLastError();
 }
 
 }  // namespace ress

@@ -1,0 +1,277 @@
+// Attention of new tokens over pages, blocks of 128 rows.
+//
+// A workgroup owns 128 rows (new token, query head of a K/V head) of a sequence, a wave 32 of them, and walks over
+// the 64-key tiles that any of them sees, as window.hip's does: score tiles S^T = K Q^T, probabilities
+// that are the next product's operand as they lie, one softmax reference a row that moves only when a
+// tile's sum passes 2^50. What differs is where keys come from. Lane l of every wave finds the page of key l of a
+// tile in the table, two tiles ahead; a wave's 8 rows of a load lie in one page where pages are multiples of 8
+// tokens, so that their address is scalar, read from that lane's registers, and costs the vector unit nothing.
+// Other pages, and tiles that are not seen whole, take an address a lane. Keys on a page
+// outside the cache, and keys that no row of the block sees, come from a row of zeros, their scores hidden.
+#include "paged_device.h"
+
+namespace ress {
+namespace {
+
+using namespace paged;
+
+constexpr int kRows = 128;
+constexpr float kSumLimit = 0x1p50f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kLeast = 8;  // tiles of a workgroup at least where keys are split
+
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+typedef const __attribute__((address_space(1))) void global_void;
+
+template <bool LSE>
+__global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char k_0[kTileBytes], k_1[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_0[kTileBytes], v_1[kTileBytes];
+
+    // Contiguous runs of (K/V head, block) per XCD, last blocks first.
+    const int items = p.H_kv * p.blocks, per = (items + 7) / 8;
+    const int id = blockIdx.x + gridDim.x * blockIdx.y, at = (id & 7) * per + (id >> 3);
+    if ((id >> 3) >= per || at >= items) return;
+    const int hk = at / p.blocks, split = blockIdx.z;
+    Block x;
+    if (!find_block<kRows>(p, p.blocks - 1 - (at - hk * p.blocks), x)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hh = lane >> 5, ql = lane & 31;
+
+    const Seen s_first = seen_at(p, x.pos0 + x.t0, x.len), s_last = seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len);
+    const Tiles tl = tiles_of(s_first, s_last);
+    const int cuts = cuts_of(p, tl.n, kLeast);
+    if (split >= cuts) return;
+    const int begin = (int)((int64_t)tl.n * split / cuts), end = (int)((int64_t)tl.n * (split + 1) / cuts);
+
+    // What the wave's rows and this lane's row see (rows behind the last repeat it), the lane's against its first key
+    // of a tile.
+    const int j = min(wave * 32 + ql, x.left - 1);
+    const Row r = row_of(p, x, j);
+    const Seen sa = seen_at(p, x.pos0 + row_of(p, x, min(wave * 32, x.left - 1)).t, x.len);
+    const Seen sb = seen_at(p, x.pos0 + row_of(p, x, min(wave * 32 + 31, x.left - 1)).t, x.len);
+    Seen sl = seen_at(p, x.pos0 + r.t, x.len);
+    sl.lo -= 4 * hh;
+    sl.hi -= 4 * hh;
+    sl.sk -= 4 * hh;
+    const bool active = wave * 32 < x.left;
+
+    bf16x8 qf[4];
+    {
+        const uint16_t *q = p.q + (hk * p.group + r.g) * p.qs.head + (int64_t)(x.cu + r.t) * p.qs.token + hh * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + kk * 16);
+    }
+    const uint16_t *const kb = p.k + hk * p.ks.head, *const vb = p.v + hk * p.vs.head;
+    const int32_t *const table = p.tables + (int64_t)x.b * p.table_stride;
+    const bool eights = p.page % 8 == 0;
+    // This lane's share of a load of 8 rows: bytes from the first one on.
+    const unsigned int chunk = (unsigned int)(((lane & 7) ^ swz(wave * 8 + (lane >> 3))) << 4);
+    const unsigned int k_off = (unsigned int)(lane >> 3) * (unsigned int)(2 * p.ks.token) + chunk;
+    const unsigned int v_off = (unsigned int)(lane >> 3) * (unsigned int)(2 * p.vs.token) + chunk;
+
+    // The page of key `lane` of tile i, -1 where no row sees it.
+    auto page_of = [&](int i) __attribute__((always_inline)) {
+        if (i >= end) return -1;
+        const int key = tl.key(i) + lane;
+        return key < s_last.sk || (key >= s_first.lo && key < s_last.hi) ? table[p.pages(key)] : -1;
+    };
+    auto fetch = [&](int i, int page, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) -> uint64_t {
+        if (i >= end) return 0;
+        const int key = tl.key(i) + lane, row = key - p.pages(key) * p.page;
+        const bool good = (unsigned int)page < (unsigned int)p.n_pages;
+        const uint64_t keys = __ballot(good);
+        if (eights && keys == ~(uint64_t)0) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int pg = __builtin_amdgcn_readlane(page, wave * 8 + 32 * u);
+                const int rw = __builtin_amdgcn_readlane(row, wave * 8 + 32 * u);
+                const unsigned char *kr = (const unsigned char *)(kb + pg * p.ks.page + rw * p.ks.token);
+                const unsigned char *vr = (const unsigned char *)(vb + pg * p.vs.page + rw * p.vs.token);
+                __builtin_amdgcn_global_load_lds((global_void *)(kr + k_off), (lds_void *)(kd + (u * 4 + wave) * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_void *)(vr + v_off), (lds_void *)(vd + (u * 4 + wave) * 1024), 16, 0, 0);
+            }
+        } else {
+            page = good ? page : -1;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int from = wave * 8 + 32 * u + (lane >> 3), pg = __shfl(page, from), rw = __shfl(row, from);
+                const uint16_t *kr = pg < 0 ? zero_row : kb + pg * p.ks.page + rw * p.ks.token;
+                const uint16_t *vr = pg < 0 ? zero_row : vb + pg * p.vs.page + rw * p.vs.token;
+                __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)kr + chunk),
+                                                 (lds_void *)(kd + (u * 4 + wave) * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)vr + chunk),
+                                                 (lds_void *)(vd + (u * 4 + wave) * 1024), 16, 0, 0);
+            }
+        }
+        return keys;
+    };
+
+    const Reader rd(lane);
+    const References refs = p.refs;
+    float ref = 0.f, sum = 0.f;  // reference and the lane's half of the row's sum
+    bool has = false;            // the row has a reference
+    f32x16 acc[2];
+#pragma unroll
+    for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[dh][v] = 0.f;
+
+    // Scores of rows 32 u .. of a tile; `part`: of the keys that the lane's row sees, else -inf.
+    auto scores = [&](bool part, uint64_t keys, const unsigned char *kt, int u, int key0, f32x16 &s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) s = mfma(rd.rows(kt, u, kk), qf[kk], s);
+        if (part) {
+            hide(s, key0 + u * 32, sl.lo, (unsigned int)(sl.hi - sl.lo), key0 < sb.sk, sl.sk);
+            if (keys != ~(uint64_t)0) drop(s, (unsigned int)(keys >> (32 * u)) >> (4 * hh));
+        }
+    };
+    // The row's largest score in the tile, as a reference.
+    auto top = [&](bool part, uint64_t keys, const unsigned char *kt, int key0) __attribute__((always_inline)) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x16 s;
+            scores(part, keys, kt, u, key0, s);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) m = fmaxf(m, s[v]);
+        }
+        return refs.of(fmaxf(m, __shfl_xor(m, 32)));
+    };
+    // Probabilities against the row's reference, and the lane's part of their sum. (any_far: some rows'
+    // references may be far.)
+    auto probs = [&](bool any_far, bool part, uint64_t keys, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2])
+                     __attribute__((always_inline)) {
+        float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x16 s;
+            scores(part, keys, kt, u, key0, s);
+            if (any_far) {
+                const bool far = refs.far(ref);
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    s[v] = __builtin_amdgcn_exp2f(far ? fmaf(s[v], refs.unit, -ref) * refs.rest : fmaf(s[v], refs.scale, -ref));
+            } else {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], refs.scale, -ref));
+            }
+            pack(s, pb[u]);
+            if constexpr (LSE) {
+#pragma unroll
+                for (int v = 0; v < 16; v += 2) l0 += s[v], l1 += s[v + 1];
+                __builtin_amdgcn_sched_barrier(0);  // (else both halves' float32 values are held: spills)
+            } else {
+                l0 = add_up(pb[u], l0);
+            }
+        }
+        return l0 + l1;
+    };
+    auto tile = [&](bool part, uint64_t keys, const unsigned char *kt, const unsigned char *vt, int key0)
+                    __attribute__((always_inline)) {
+        bf16x8 pb[2][2];
+        float l;
+        // (Rare: a row's first tile, or logits far above those so far. Lanes l and l^32 share the
+        // row and decide together.)
+        bool look = __any(!has), over = false;
+#pragma nounroll
+        for (bool again = false;; again = true) {
+            if (look) {
+                const float m = top(part, keys, kt, key0);
+                if (has ? over : m > -INFINITY) {
+                    const float to = has ? fmaxf(ref, m) : m;
+                    const float a = has ? __builtin_amdgcn_exp2f(refs.difference(ref, to)) : 0.f;
+                    sum *= a;
+#pragma unroll
+                    for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) acc[dh][v] *= a;
+                    ref = to;
+                    has = true;
+                }
+            }
+            l = probs(false, part, keys, kt, key0, pb);
+            over = !(l <= kSumLimit);
+            const bool far = refs.far(ref);
+            if (!__any(over || far)) break;
+            if (__any(far)) {
+                asm volatile("" ::: "memory");  // (code of its own: the ordinary form stays in one piece)
+                l = probs(true, part, keys, kt, key0, pb);
+                over = !(l <= kSumLimit);
+            }
+            look = __any(over);
+            if (!look || again) break;
+            over = ((int)over | __shfl_xor((int)over, 32)) != 0;
+        }
+        sum += l;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dh = 0; dh < 2; ++dh) acc[dh] = mfma(rd.cols(vt, u, e, dh), pb[u][e], acc[dh]);
+    };
+    int i = begin, page = -1;
+    uint64_t keys = 0;  // of tile i
+    // Tile i from (kt, vt), tile i + 1 on its way into the other slots, the pages of tile i + 2 too.
+    auto step = [&](const unsigned char *kt, const unsigned char *vt, unsigned char *kd, unsigned char *vd)
+                    __attribute__((always_inline)) -> bool {
+        const uint64_t next = fetch(i + 1, page, kd, vd);
+        page = page_of(i + 2);
+        const int key0 = tl.key(i);
+        if (active && (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi)) && keys != 0)
+            tile(!(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi)) || keys != ~(uint64_t)0, keys, kt, vt, key0);
+        wait_vm_all();
+        __syncthreads();
+        keys = next;
+        return ++i < end;
+    };
+    if (i < end) {
+        keys = fetch(i, page_of(i), k_0, v_0);
+        page = page_of(i + 1);
+        wait_vm_all();
+        __syncthreads();
+        while (step(k_0, v_0, k_1, v_1) && step(k_1, v_1, k_0, v_0)) {
+        }
+    }
+
+    sum += __shfl_xor(sum, 32);
+    if (wave * 32 + ql >= x.left) return;
+    const int h = hk * p.group + r.g;
+    const int64_t row = (int64_t)h * p.N + x.cu + r.t;
+    if (p.splits > 1 && split == 0 && hh == 0) p.cuts[row] = cuts;
+    if (cuts > 1) {
+        const int64_t to = (int64_t)split * p.H * p.N + row;
+#pragma unroll
+        for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4 *>(p.part + to * 64 + dh * 32 + g * 8 + hh * 4) =
+                    f32x4{acc[dh][g * 4], acc[dh][g * 4 + 1], acc[dh][g * 4 + 2], acc[dh][g * 4 + 3]};
+        if (hh == 0) p.part_row[to] = make_float2(ref, sum);
+        return;
+    }
+    store_row(p.o + h * p.os.head + (int64_t)(x.cu + r.t) * p.os.token, acc, inverse(sum), hh);
+    if (LSE && hh == 0) p.lse[row] = sum == 0.f ? -INFINITY : refs.base2(ref) * kLn2 + logf(sum);
+}
+
+}  // namespace
+
+hipError_t launch_paged_wide(const PagedParams &p, hipStream_t s)
+{
+    // (A grid's threads in one dimension stay below 2^32.)
+    const int64_t ids = ((int64_t)p.H_kv * p.blocks + 7) / 8 * 8;
+    const unsigned wide = ids < (1 << 20) ? (unsigned)ids : 1u << 20;
+    const dim3 grid(wide, (unsigned)((ids + wide - 1) / wide), (unsigned)p.splits), block(256);
+    if (p.lse)
+        hipLaunchKernelGGL((wide_kernel<true>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((wide_kernel<false>), grid, block, 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace ress

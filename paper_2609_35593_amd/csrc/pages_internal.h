@@ -97,5 +97,6 @@ hipError_t launch_head_norm_bwd(const HeadNormBwdParams &p, hipStream_t s);
 hipError_t launch_tables(const TableParams &p, hipStream_t s);
 hipError_t launch_release(const ReleaseParams &p, hipStream_t s);
 hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s);
+hipError_t launch_paged_wide(const PagedParams &p, hipStream_t s);
 
 }  // namespace ress

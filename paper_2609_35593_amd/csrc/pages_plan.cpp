@@ -22,13 +22,15 @@ PagedPlan paged_plan(const ress_paged_shape *s)
 {
     PagedPlan r = {32, 0, 1};
     if (s->B == 0 || s->N == 0 || s->H == 0) return r;
-    // A sequence leaves at most one block that is not full.
     const int64_t group = s->H / s->H_kv, rows = s->N * group, some = s->B < s->N ? s->B : s->N;
+    // Blocks of 128 rows where sequences have more than 32 on average.
+    if (rows > 32 * some) r.rows = 128;
+    // A sequence leaves at most one block that is not full.
     r.blocks = (int)((rows + some * (r.rows - 1)) / r.rows);
     const int64_t capacity = (int64_t)s->max_pages * s->page;
     int64_t keys = window_tokens(s->frame, s->window) + s->n_sink + r.rows / group;
     if (keys > capacity) keys = capacity;
-    const int64_t tiles = (keys + 63) / 64, most = tiles / 4, want = 1024 / ((int64_t)r.blocks * s->H_kv);
+    const int64_t tiles = (keys + 63) / 64, most = tiles / (r.rows == 32 ? 4 : 8), want = 1024 / ((int64_t)r.blocks * s->H_kv);
     const int64_t n = want < most ? want : most;
     r.splits = (int)(n < 1 ? 1 : n > kMaxPagedSplits ? kMaxPagedSplits : n);
     return r;
