@@ -3,10 +3,11 @@
 // A workgroup owns 128 rows (new token, query head of a K/V head) of a sequence, a wave 32 of them, and walks over
 // the 64-key tiles that any of them sees, as window.hip's does: score tiles S^T = K Q^T, probabilities
 // that are the next product's operand as they lie, one softmax reference a row that moves only when a
-// tile's sum passes 2^50. What differs is where keys come from. Lane l of every wave finds the page of key l of a
-// tile in the table, two tiles ahead; a wave's 8 rows of a load lie in one page where pages are multiples of 8
-// tokens, so that their address is scalar, read from that lane's registers, and costs the vector unit nothing.
-// Other pages, and tiles that are not seen whole, take an address a lane. Keys on a page
+// tile's sum passes 2^50. What differs is where keys come from. A wave keeps 64 entries of the table in a
+// register, one a lane; its 8 rows of a load lie in one page where pages are multiples of 8 tokens, so
+// that their address is scalar and costs the vector unit one read of a lane (found anew for every tile by each of
+// its keys, pages took a fifth more vector instructions). Other pages, and tiles that are not seen whole, take an
+// address a lane. Keys on a page
 // outside the cache, and keys that no row of the block sees, come from a row of zeros, their scores hidden.
 #include "paged_device.h"
 
@@ -23,6 +24,12 @@ constexpr int kLeast = 8;  // tiles of a workgroup at least where keys are split
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
 typedef const __attribute__((address_space(1))) void global_void;
+
+// Eight rows from one on: at most 7 token strides of 2^22 elements and a row.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const unsigned char *row)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(row), 0, 7 * (1 << 23) + 128, 0x00020000);
+}
 
 template <bool LSE>
 __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
@@ -66,47 +73,54 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     }
     const uint16_t *const kb = p.k + hk * p.ks.head, *const vb = p.v + hk * p.vs.head;
     const int32_t *const table = p.tables + (int64_t)x.b * p.table_stride;
-    const bool eights = p.page % 8 == 0;
     // This lane's share of a load of 8 rows: bytes from the first one on.
     const unsigned int chunk = (unsigned int)(((lane & 7) ^ swz(wave * 8 + (lane >> 3))) << 4);
     const unsigned int k_off = (unsigned int)(lane >> 3) * (unsigned int)(2 * p.ks.token) + chunk;
     const unsigned int v_off = (unsigned int)(lane >> 3) * (unsigned int)(2 * p.vs.token) + chunk;
 
-    // The page of key `lane` of tile i, -1 where no row sees it.
-    auto page_of = [&](int i) __attribute__((always_inline)) {
-        if (i >= end) return -1;
-        const int key = tl.key(i) + lane;
-        return key < s_last.sk || (key >= s_first.lo && key < s_last.hi) ? table[p.pages(key)] : -1;
-    };
-    auto fetch = [&](int i, int page, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) -> uint64_t {
+    // Entries base .. base + 63 of the table, one a lane, and which of them are pages of the cache.
+    int entries = -1, base = -64;
+    uint64_t there = 0;
+    // Starts the loads of tile i; the keys that are read.
+    auto fetch = [&](int i, unsigned char *kd, unsigned char *vd) __attribute__((always_inline)) -> uint64_t {
         if (i >= end) return 0;
-        const int key = tl.key(i) + lane, row = key - p.pages(key) * p.page;
-        const bool good = (unsigned int)page < (unsigned int)p.n_pages;
-        const uint64_t keys = __ballot(good);
-        if (eights && keys == ~(uint64_t)0) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int pg = __builtin_amdgcn_readlane(page, wave * 8 + 32 * u);
-                const int rw = __builtin_amdgcn_readlane(row, wave * 8 + 32 * u);
-                const unsigned char *kr = (const unsigned char *)(kb + pg * p.ks.page + rw * p.ks.token);
-                const unsigned char *vr = (const unsigned char *)(vb + pg * p.vs.page + rw * p.vs.token);
-                __builtin_amdgcn_global_load_lds((global_void *)(kr + k_off), (lds_void *)(kd + (u * 4 + wave) * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_void *)(vr + v_off), (lds_void *)(vd + (u * 4 + wave) * 1024), 16, 0, 0);
-            }
-        } else {
-            page = good ? page : -1;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int from = wave * 8 + 32 * u + (lane >> 3), pg = __shfl(page, from), rw = __shfl(row, from);
-                const uint16_t *kr = pg < 0 ? zero_row : kb + pg * p.ks.page + rw * p.ks.token;
-                const uint16_t *vr = pg < 0 ? zero_row : vb + pg * p.vs.page + rw * p.vs.token;
-                __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)kr + chunk),
-                                                 (lds_void *)(kd + (u * 4 + wave) * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)vr + chunk),
-                                                 (lds_void *)(vd + (u * 4 + wave) * 1024), 16, 0, 0);
-            }
+        const int key0 = tl.key(i), e0 = p.pages(key0), e1 = min(p.pages(key0 + kTile - 1), p.max_pages - 1);
+        if (e0 < base || e1 >= base + 64) {
+            base = e0;
+            entries = table[min(base + lane, p.max_pages - 1)];
+            there = __ballot((unsigned int)entries < (unsigned int)p.n_pages);
         }
-        return keys;
+        const uint64_t need = ~(uint64_t)0 >> (63 - (e1 - e0));
+        const bool whole = key0 + kTile <= s_last.sk || (key0 >= s_first.lo && key0 + kTile <= s_last.hi);
+        if (p.eights && whole && (there >> (e0 - base) & need) == need) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int key = key0 + wave * 8 + 32 * u, e = p.pages(key), rw = key - e * p.page;
+                const int pg = __builtin_amdgcn_readlane(entries, e - base);
+                const uint64_t ko = ((uint64_t)(uint32_t)pg * p.k_page16 + (uint32_t)rw * p.k_token16) << 4;
+                const uint64_t vo = p.alike ? ko : ((uint64_t)(uint32_t)pg * p.v_page16 + (uint32_t)rw * p.v_token16) << 4;
+                const __amdgpu_buffer_rsrc_t kr = rows_at((const unsigned char *)kb + ko), vr = rows_at((const unsigned char *)vb + vo);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(kd + (u * 4 + wave) * 1024), 16, k_off, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void *)(vd + (u * 4 + wave) * 1024), 16, v_off, 0, 0, 0);
+            }
+            return ~(uint64_t)0;
+        }
+        const int key = key0 + lane, e = p.pages(key), row = key - e * p.page;
+        int page = __shfl(entries, e - base);
+        const bool seen = key < s_last.sk || (key >= s_first.lo && key < s_last.hi);
+        const bool good = seen && (unsigned int)page < (unsigned int)p.n_pages;
+        page = good ? page : -1;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int from = wave * 8 + 32 * u + (lane >> 3), pg = __shfl(page, from), rw = __shfl(row, from);
+            const uint16_t *kr = pg < 0 ? zero_row : kb + pg * p.ks.page + rw * p.ks.token;
+            const uint16_t *vr = pg < 0 ? zero_row : vb + pg * p.vs.page + rw * p.vs.token;
+            __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)kr + chunk),
+                                             (lds_void *)(kd + (u * 4 + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_void *)((const unsigned char *)vr + chunk),
+                                             (lds_void *)(vd + (u * 4 + wave) * 1024), 16, 0, 0);
+        }
+        return __ballot(good);
     };
 
     const Reader rd(lane);
@@ -215,13 +229,12 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
 #pragma unroll
                 for (int dh = 0; dh < 2; ++dh) acc[dh] = mfma(rd.cols(vt, u, e, dh), pb[u][e], acc[dh]);
     };
-    int i = begin, page = -1;
+    int i = begin;
     uint64_t keys = 0;  // of tile i
-    // Tile i from (kt, vt), tile i + 1 on its way into the other slots, the pages of tile i + 2 too.
+    // Tile i from (kt, vt), tile i + 1 on its way into the other slots.
     auto step = [&](const unsigned char *kt, const unsigned char *vt, unsigned char *kd, unsigned char *vd)
                     __attribute__((always_inline)) -> bool {
-        const uint64_t next = fetch(i + 1, page, kd, vd);
-        page = page_of(i + 2);
+        const uint64_t next = fetch(i + 1, kd, vd);
         const int key0 = tl.key(i);
         if (active && (key0 < sb.sk || (key0 + kTile > sa.lo && key0 < sb.hi)) && keys != 0)
             tile(!(key0 + kTile <= sa.sk || (key0 >= sb.lo && key0 + kTile <= sa.hi)) || keys != ~(uint64_t)0, keys, kt, vt, key0);
@@ -231,8 +244,7 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
         return ++i < end;
     };
     if (i < end) {
-        keys = fetch(i, page_of(i), k_0, v_0);
-        page = page_of(i + 1);
+        keys = fetch(i, k_0, v_0);
         wait_vm_all();
         __syncthreads();
         while (step(k_0, v_0, k_1, v_1) && step(k_1, v_1, k_0, v_0)) {

@@ -480,6 +480,13 @@ int ress_paged_attn(const ress_paged_shape *shape, const void *q, const void *k,
     p.os = s.o;
     p.ks = s.k;
     p.vs = s.v;
+    auto narrow = [&](const ress_page_strides &t) { return t.page / 8 <= 0xffffffff && t.token / 8 * s.page <= 0xffffffff; };
+    p.eights = s.page % 8 == 0 && narrow(s.k) && narrow(s.v);
+    p.alike = s.k.page == s.v.page && s.k.token == s.v.token;
+    p.k_page16 = (uint32_t)(s.k.page / 8);
+    p.k_token16 = (uint32_t)(s.k.token / 8);
+    p.v_page16 = (uint32_t)(s.v.page / 8);
+    p.v_token16 = (uint32_t)(s.v.token / 8);
     p.q = static_cast<const uint16_t *>(q);
     p.k = static_cast<const uint16_t *>(k);
     p.v = static_cast<const uint16_t *>(v);

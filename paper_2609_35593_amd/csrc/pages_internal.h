@@ -76,6 +76,10 @@ struct PagedParams {
     float scale, scale_log2;
     ress_strides qs, os;
     ress_page_strides ks, vs;
+    // Pages of multiples of 8 tokens whose strides, and whose rows' offsets in a page, fit 32 bits in steps of 16 bytes:
+    // those steps, and whether K's and V's are the same.
+    bool eights, alike;
+    uint32_t k_page16, k_token16, v_page16, v_token16;
     const uint16_t *q, *k, *v;
     const int32_t *cu_q, *lens, *tables;
     uint16_t *o;
