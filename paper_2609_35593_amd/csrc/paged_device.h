@@ -28,56 +28,109 @@ __device__ __forceinline__ Row row_of(const PagedParams &p, const Block &x, int 
     return {x.t0 + n, x.g0 + j - n * p.group};
 }
 
+// A sequence's rows of q, clamped (so a block's rows lie in [0, N) whatever the offsets hold), and its blocks.
+struct Rows {
+    int cu, end;
+    template <int ROWS>
+    __device__ __forceinline__ int blocks(const PagedParams &p) const
+    {
+        return (int)(((int64_t)(end - cu) * p.group + ROWS - 1) / ROWS);
+    }
+};
+__device__ __forceinline__ Rows rows_of(const PagedParams &p, int from, int to)
+{
+    const int cu = min(max(from, 0), p.N);
+    return {cu, min(max(to, cu), p.N)};
+}
+
+template <int ROWS>
+__device__ __forceinline__ void block_of(const PagedParams &p, Block &x, int b, int index, const Rows &r, int len)
+{
+    const int n = r.end - r.cu;
+    x.b = b;
+    x.cu = r.cu;
+    x.len = min(max(len, 0), p.capacity);
+    x.pos0 = x.len - n;
+    const int64_t first = (int64_t)index * ROWS, rows = (int64_t)n * p.group;
+    x.t0 = (int)((uint32_t)first / (uint32_t)p.group);  // (2^24 tokens of 256 heads at most)
+    x.g0 = (int)(first - (int64_t)x.t0 * p.group);
+    x.left = (int)(rows - first < ROWS ? rows - first : ROWS);
+}
+
+constexpr int kMostBlocks = 1 << 29;  // sums of blocks stop here
+
 // Block `index` of all sequences' blocks of ROWS rows; false behind the last. Every thread of a
-// workgroup of 256 calls it. (Offsets are clamped, so a block's rows lie in [0, N) whatever they hold.)
+// workgroup of 256 calls it. Up to 256 sequences each wave looks at all of them by itself, their offsets and
+// lengths in one round trip.
 template <int ROWS>
 __device__ __forceinline__ bool find_block(const PagedParams &p, int index, Block &x)
 {
-    __shared__ int found[3], ends[4];
-    constexpr int kMost = 1 << 29;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    if (p.B <= 256) {
+        int from[4], to[4], len[4], before = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c * 64 < p.B) {
+                const int b = min(c * 64 + lane, p.B - 1);
+                from[c] = p.cu_q[b];
+                to[c] = p.cu_q[b + 1];
+                len[c] = p.lens[b];
+            }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (c * 64 >= p.B) break;
+            const Rows r = rows_of(p, from[c], to[c]);
+            const int blocks = c * 64 + lane < p.B ? r.blocks<ROWS>(p) : 0;
+            int sum = blocks;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(sum, o);
+                if (lane >= o) sum = min(sum + y, kMostBlocks);
+            }
+            sum = min(sum + before, kMostBlocks);
+            const uint64_t here = __ballot(blocks > 0 && index < sum && index >= sum - blocks);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                block_of<ROWS>(p, x, c * 64 + l, index - __builtin_amdgcn_readlane(sum - blocks, l),
+                               {__builtin_amdgcn_readlane(r.cu, l), __builtin_amdgcn_readlane(r.end, l)},
+                               __builtin_amdgcn_readlane(len[c], l));
+                return true;
+            }
+            before = __builtin_amdgcn_readlane(sum, 63);
+        }
+        return false;
+    }
+    __shared__ int found[2], ends[4];
+    const int wave = threadIdx.x >> 6;
     int before = 0;
     if (threadIdx.x == 0) found[0] = -1;
     for (int b0 = 0; b0 < p.B; b0 += 256) {
         const int b = b0 + threadIdx.x;
-        int cu = 0, blocks = 0;
-        if (b < p.B) {
-            cu = min(max(p.cu_q[b], 0), p.N);
-            const int end = min(max(p.cu_q[b + 1], cu), p.N);
-            blocks = (int)(((int64_t)(end - cu) * p.group + ROWS - 1) / ROWS);
-        }
+        const int blocks = b < p.B ? rows_of(p, p.cu_q[b], p.cu_q[b + 1]).blocks<ROWS>(p) : 0;
         int sum = blocks;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int y = __shfl_up(sum, o);
-            if (lane >= o) sum = min(sum + y, kMost);
+            if (lane >= o) sum = min(sum + y, kMostBlocks);
         }
         if (lane == 63) ends[wave] = sum;
         __syncthreads();
         int head = before;
         for (int w = 0; w < 4; ++w) {
-            if (w < wave) head = min(head + ends[w], kMost);
-            before = min(before + ends[w], kMost);
+            if (w < wave) head = min(head + ends[w], kMostBlocks);
+            before = min(before + ends[w], kMostBlocks);
         }
-        sum = min(sum + head, kMost);
+        sum = min(sum + head, kMostBlocks);
         if (blocks > 0 && index < sum && index >= sum - blocks) {
             found[0] = b;
             found[1] = index - (sum - blocks);
-            found[2] = cu;
         }
         __syncthreads();
         if (before > index) break;
     }
-    if (p.B > 0) x.b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (p.B == 0 || x.b < 0) return false;
-    x.cu = __builtin_amdgcn_readfirstlane(found[2]);
-    const int end = min(max(p.cu_q[x.b + 1], x.cu), p.N), n = end - x.cu;
-    x.len = min(max(p.lens[x.b], 0), p.capacity);
-    x.pos0 = x.len - n;
-    const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane(found[1]) * ROWS, rows = (int64_t)n * p.group;
-    x.t0 = (int)((uint32_t)first / (uint32_t)p.group);  // (2^24 tokens of 256 heads at most)
-    x.g0 = (int)(first - (int64_t)x.t0 * p.group);
-    x.left = (int)(rows - first < ROWS ? rows - first : ROWS);
+    const int b = __builtin_amdgcn_readfirstlane(found[0]);
+    if (b < 0) return false;
+    block_of<ROWS>(p, x, b, __builtin_amdgcn_readfirstlane(found[1]), rows_of(p, p.cu_q[b], p.cu_q[b + 1]), p.lens[b]);
     return true;
 }
 

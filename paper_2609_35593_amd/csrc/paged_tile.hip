@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams 
 
     const Seen sa = seen_at(p, x.pos0 + x.t0, x.len), sb = seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len);
     const Tiles tl = tiles_of(sa, sb);
-    const int cuts = cuts_of(p, tl.n, kWaves);
+    const int cuts = cuts_of(p, tl.n, kTileLeast);
     if (split >= cuts) return;
     const int begin = (int)((int64_t)tl.n * split / cuts), end = (int)((int64_t)tl.n * (split + 1) / cuts);
     const int each = (end - begin + kWaves - 1) / kWaves;
@@ -208,37 +208,72 @@ __device__ __forceinline__ float share(const PagedParams &p, float ref, float to
     return __builtin_amdgcn_exp2f(WIDE ? p.refs.difference(ref, top) : (ref - top) * p.scale_log2);
 }
 
-// A wave a row, a channel a lane: its parts in order, their weights one a lane first. Rows outside every
-// sequence, and those that one workgroup finished, are left as they are.
-template <bool WIDE>
+// A row by W waves, a channel a lane, 16 parts a wave: all of a wave's parts are on their way at once, their weights one
+// a lane first; the waves' sums are added in order. Rows outside every sequence, and those that one workgroup
+// finished, are left as they are. (What a row does not have of p.splits parts may hold anything.)
+constexpr int kParts = 16;
+template <bool WIDE, int W>
 __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
 {
-    const int64_t rows = (int64_t)p.H * p.N, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    __shared__ float tops[4], sums[4], outs[4][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = W > 1 ? wave * kParts : 0;
+    const int64_t rows = (int64_t)p.H * p.N, row = W > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     if (row >= rows) return;
     const int64_t h = row / p.N, t = row - h * p.N;
-    if (t < p.cu_q[0] || t >= p.cu_q[p.B]) return;
-    const int n = min(p.cuts[row], p.splits);
-    if (n <= 1) return;
-    const int lane = threadIdx.x & 63;
-    const float2 r = lane < n ? p.part_row[lane * rows + row] : make_float2(kNone, 0.f);
+    const int from = p.cu_q[0], to = p.cu_q[p.B], cuts = p.cuts[row];
+    float y[kParts];
+    float2 r = make_float2(kNone, 0.f);
+    const int most = p.splits - first;  // parts that there may be
+    if (lane < kParts && lane < most) r = p.part_row[(first + lane) * rows + row];
+#pragma unroll
+    for (int s0 = 0; s0 < kParts; s0 += 4)
+        if (s0 < most)
+#pragma unroll
+            for (int s = s0; s < s0 + 4; ++s) y[s] = p.part[(first + min(s, most - 1)) * rows * 64 + row * 64 + lane];
+    if (t < from || t >= to || cuts <= 1) return;
+    const int n = min(cuts, p.splits) - first;
+    if (lane >= n) r = make_float2(kNone, 0.f);
     float top = r.y == 0.f ? kNone : r.x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if constexpr (W > 1) {
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w]);
+    }
     const float w = r.y == 0.f ? 0.f : share<WIDE>(p, r.x, top);
     float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
-    for (int s0 = 0; s0 < n; s0 += 8) {
-        float y[8];
 #pragma unroll
-        for (int s = 0; s < 8; ++s) y[s] = p.part[(min(s0 + s, n - 1) * rows + row) * 64 + lane];
+    for (int s = 0; s < kParts; ++s)
+        if (s < n)
+            o = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s)), y[s], o);
+    if constexpr (W > 1) {
+        outs[wave][lane] = o;
+        if (lane == 0) sums[wave] = sum;
+        __syncthreads();
+        if (wave > 0) return;
+        sum = o = 0.f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s)
-            if (s0 + s < n) o = fmaf(__shfl(w, s0 + s), y[s], o);
+        for (int i = 0; i < W; ++i) sum += sums[i], o += outs[i][lane];
     }
     p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(sum == 0.f ? 0.f : o / sum);
     if (p.lse && lane == 0)
         p.lse[row] = sum == 0.f ? -INFINITY : (WIDE ? p.refs.base2(top) * 0.6931471805599453f : top * p.scale) + logf(sum);
+}
+
+template <bool WIDE>
+hipError_t launch_join(const PagedParams &p, hipStream_t s)
+{
+    static_assert(kMaxPagedSplits <= 4 * kParts, "four waves hold a row's parts");
+    const int64_t rows = (int64_t)p.H * p.N;
+    if (p.splits <= kParts)
+        hipLaunchKernelGGL((join_kernel<WIDE, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+    else
+        hipLaunchKernelGGL((join_kernel<WIDE, 4>), dim3((unsigned)rows), dim3(256), 0, s, p);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -252,12 +287,7 @@ hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (p.splits == 1) return hipSuccess;
-    const dim3 grid((unsigned)(((int64_t)p.H * p.N + 3) / 4));
-    if (rows == 128)
-        hipLaunchKernelGGL((join_kernel<true>), grid, dim3(256), 0, s, p);
-    else
-        hipLaunchKernelGGL((join_kernel<false>), grid, dim3(256), 0, s, p);
-    return hipGetLastError();
+    return rows == 128 ? launch_join<true>(p, s) : launch_join<false>(p, s);
 }
 
 }  // namespace ress

@@ -19,7 +19,6 @@ using namespace paged;
 constexpr int kRows = 128;
 constexpr float kSumLimit = 0x1p50f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kLeast = 8;  // tiles of a workgroup at least where keys are split
 
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
@@ -49,7 +48,7 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
 
     const Seen s_first = seen_at(p, x.pos0 + x.t0, x.len), s_last = seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len);
     const Tiles tl = tiles_of(s_first, s_last);
-    const int cuts = cuts_of(p, tl.n, kLeast);
+    const int cuts = cuts_of(p, tl.n, kWideLeast);
     if (split >= cuts) return;
     const int begin = (int)((int64_t)tl.n * split / cuts), end = (int)((int64_t)tl.n * (split + 1) / cuts);
 

@@ -95,6 +95,7 @@ struct PagedPlan {
 };
 PagedPlan paged_plan(const ress_paged_shape *s);
 constexpr int kMaxPagedSplits = 64;
+constexpr int kTileLeast = 4, kWideLeast = 10;  // tiles of a workgroup at least where keys are cut (a wave one; see paged_plan)
 
 hipError_t launch_head_norm(const HeadNormParams &p, hipStream_t s);
 hipError_t launch_head_norm_bwd(const HeadNormBwdParams &p, hipStream_t s);

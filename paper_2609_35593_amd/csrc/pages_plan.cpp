@@ -30,8 +30,13 @@ PagedPlan paged_plan(const ress_paged_shape *s)
     const int64_t capacity = (int64_t)s->max_pages * s->page;
     int64_t keys = window_tokens(s->frame, s->window) + s->n_sink + r.rows / group;
     if (keys > capacity) keys = capacity;
-    const int64_t tiles = (keys + 63) / 64, most = tiles / (r.rows == 32 ? 4 : 8), want = 1024 / ((int64_t)r.blocks * s->H_kv);
-    const int64_t n = want < most ? want : most;
+    // Keys are cut over workgroups, of kTileLeast or kWideLeast tiles at least, while there are few blocks. (us by workgroups that share
+    // a block. 128 rows: 176 blocks of 687 tiles 1 / 5 / 8 / 16 793 / 342 / 333 / 313; 512 of up to 64, 1 / 4 / 16 104 / 90 / 93;
+    // 128 of 31, 1 / 3 43 / 38; but 176 of 21, 1 / 2 32 / 41. 32 rows: 192 blocks of 47 tiles 1 / 2 / 4 31.7 / 34.9 / 38.0, 384 55 /
+    // 58 / 62, 4 of 688, 16 / 32 / 64 33 / 25 / 24.)
+    const int64_t tiles = (keys + 63) / 64, blocks = (int64_t)r.blocks * s->H_kv;
+    const int64_t most = r.rows == 32 ? tiles / kTileLeast : tiles < 24 ? 1 : tiles / kWideLeast;
+    const int64_t want = (r.rows == 32 ? 256 : 2816) / blocks, n = want < most ? want : most;
     r.splits = (int)(n < 1 ? 1 : n > kMaxPagedSplits ? kMaxPagedSplits : n);
     return r;
 }
