@@ -93,6 +93,26 @@ bool weights_ok(const float *const *w, int n, const void *const *outs, int n_out
     return true;
 }
 
+ChunkRuns chunk_runs(const ress_rope_shape &s, int turned, int per)
+{
+    ChunkRuns r;
+    memset(&r, 0, sizeof r);
+    if (per == 0) return r;
+    if (s.layout != RESS_ROPE_SPLIT) {
+        r.n = 1;
+        r.half[0] = s.layout == RESS_ROPE_SECTIONS ? turned / 2 / per : 0;
+        r.count[0] = turned / per;
+        return r;
+    }
+    for (int a = 0, at = 0; a < s.n_axes; at += s.dims[a++]) {
+        r.first[r.n] = at / per;
+        r.half[r.n] = s.dims[a] / 2 / per;
+        r.count[r.n] = s.dims[a] / per;
+        r.pair[r.n++] = at / 2;
+    }
+    return r;
+}
+
 // The forward pass, into pages where `cache` is given.
 int head_norm(const ress_head_norm_shape *shape, const ress_page_cache *cache, const int32_t *pos, const int32_t *slots,
               const void *q_in, const void *k_in, const void *v_in, const float *const (&weights)[4], void *q_out, void *k_out,
@@ -146,6 +166,7 @@ int head_norm(const ress_head_norm_shape *shape, const ress_page_cache *cache, c
         p.r.chunk = per;
     }
     rope_tables(s, turned, p.r);
+    p.runs = chunk_runs(s, turned, p.r.chunk);
     p.r.pos = pos;
     p.r.q_in = q_in;
     p.r.k_in = k_in;
@@ -177,8 +198,7 @@ int head_norm(const ress_head_norm_shape *shape, const ress_page_cache *cache, c
 
 size_t head_bwd_workspace(const ress_rope_shape &s)
 {
-    const int parts = head_bwd_plan(s.H + s.H_kv, s.N, s.D).parts;
-    return align256((size_t)(parts > 0 ? parts : 1) * 4 * s.D * sizeof(float));
+    return align256((size_t)head_bwd_parts(s.H + s.H_kv, s.N) * 4 * s.D * sizeof(float));
 }
 
 // ------------------------------------------------------------------- pages
@@ -323,6 +343,7 @@ int ress_qk_norm_rope_bwd(const ress_head_norm_shape *shape, const ress_head_nor
     for (int per = (int)(16 / size); per >= (int)(8 / size) && !p.r.chunk; per /= 2)
         if (rope_chunks(s, per, turned) && tensors_in_chunks(s, per, t, 6)) p.r.chunk = per;
     rope_tables(s, turned, p.r);
+    p.runs = chunk_runs(s, turned, p.r.chunk);
     p.r.pos = pos;
     p.r.q_in = dq_out;
     p.r.k_in = dk_out;
@@ -341,7 +362,6 @@ int ress_qk_norm_rope_bwd(const ress_head_norm_shape *shape, const ress_head_nor
     p.xs[0] = s.q;
     p.xs[1] = s.k;
     p.part = wanted ? static_cast<float *>(workspace) : nullptr;
-    p.parts = head_bwd_plan(s.H + s.H_kv, s.N, s.D).parts;
     for (int i = 0; i < 4; ++i) p.sums[i] = sums[i];
     return launch_head_norm_bwd(p, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }

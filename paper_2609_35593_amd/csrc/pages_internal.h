@@ -6,10 +6,18 @@
 
 namespace ress {
 
+// Runs of chunks whose first `half` ones hold the pairs' first sides, the next `half` the second sides, and from
+// `pair` on the pairs (half = 0, interleaved: chunks that hold whole pairs, `count` of them).
+struct ChunkRuns {
+    int n;
+    int first[RESS_MAX_ROPE_AXES], half[RESS_MAX_ROPE_AXES], count[RESS_MAX_ROPE_AXES], pair[RESS_MAX_ROPE_AXES];
+};
+
 // The norm of heads with the rotation. r: tables, sizes, pos and strides as in rope.hip (q_in, k_in,
 // q_out, k_out are this pass's inputs and outputs; r.chunk: 0 for pairs).
 struct HeadNormParams {
     RopeParams r;
+    ChunkRuns runs;
     bool layer;  // subtract the mean
     float eps;
     const float *gamma[2], *beta[2];  // of Q and K; null: 1, 0
@@ -25,6 +33,7 @@ struct HeadNormParams {
 };
 
 struct HeadNormBwdParams {
+    ChunkRuns runs;
     RopeParams r;  // q_in, k_in: the gradients of the outputs; q_out, k_out: those of the inputs
     bool layer;
     float eps;
@@ -32,18 +41,18 @@ struct HeadNormBwdParams {
     const void *x[2];  // the forward pass's inputs
     ress_strides xs[2];
     float *part;    // [parts][4][D]: gamma and beta of Q, of K; null: not wanted
-    int parts;
     float *sums[4]; // outputs, each may be null
 };
 
-// Workgroups of the backward pass: over tokens, over heads. A function of the shape alone, whatever
-// the alignment: both kinds of its kernels take 256 / lanes tokens a workgroup in turn.
-constexpr int kHeadParts = 1024;
+// Workgroups of the backward pass, which take `tokens_each` tokens at a time: over tokens, over heads.
+constexpr int kHeadParts = 1024;  // at most, each with a row of partial sums
 struct HeadBwdPlan {
     int tokens, heads;  // workgroups over tokens; heads a workgroup
     int parts;
 };
-HeadBwdPlan head_bwd_plan(int H_all, int N, int D);
+HeadBwdPlan head_bwd_plan(int H_all, int N, int tokens_each);
+// Rows of partial sums that any of its plans needs at most.
+int head_bwd_parts(int H_all, int N);
 
 struct TableParams {
     int B, N, page, n_pages, max_pages;

@@ -4,18 +4,24 @@
 
 namespace ress {
 
-HeadBwdPlan head_bwd_plan(int H_all, int N, int D)
+HeadBwdPlan head_bwd_plan(int H_all, int N, int tokens_each)
 {
     HeadBwdPlan r = {0, 0, 0};
     if (H_all == 0 || N == 0) return r;
-    // Workgroups over tokens, of 2,048 channels of a head at least, and over heads while there are few.
-    const int64_t tokens = ((int64_t)N * D + 2047) / 2048;
+    // Workgroups over tokens, and over heads while there are few.
+    const int64_t tokens = ((int64_t)N + tokens_each - 1) / tokens_each;
     r.tokens = (int)(tokens < kHeadParts ? tokens : kHeadParts);
     int cuts = kHeadParts / r.tokens;
     if (cuts > H_all) cuts = H_all;
     r.heads = (H_all + cuts - 1) / cuts;
     r.parts = r.tokens * ((H_all + r.heads - 1) / r.heads);
     return r;
+}
+
+int head_bwd_parts(int H_all, int N)
+{
+    const int64_t rows = (int64_t)H_all * N;
+    return (int)(rows < 1 ? 1 : rows < kHeadParts ? rows : kHeadParts);
 }
 
 PagedPlan paged_plan(const ress_paged_shape *s)
