@@ -201,18 +201,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams 
     }
 }
 
-// References of parts: scores (WIDE = false), or in wide_kernel's form.
-template <bool WIDE>
-__device__ __forceinline__ float share(const PagedParams &p, float ref, float top)
-{
-    return __builtin_amdgcn_exp2f(WIDE ? p.refs.difference(ref, top) : (ref - top) * p.scale_log2);
-}
-
 // A row by W waves, a channel a lane, 16 parts a wave: all of a wave's parts are on their way at once, their weights one
 // a lane first; the waves' sums are added in order. Rows outside every sequence, and those that one workgroup
 // finished, are left as they are. (What a row does not have of p.splits parts may hold anything.)
 constexpr int kParts = 16;
-template <bool WIDE, int W>
+template <int W>
 __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
 {
     __shared__ float tops[4], sums[4], outs[4][64];
@@ -221,15 +214,17 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
     if (row >= rows) return;
     const int64_t h = row / p.N, t = row - h * p.N;
     const int from = p.cu_q[0], to = p.cu_q[p.B], cuts = p.cuts[row];
+    // (Few rows: their parts are on their way before it is known how many there are. Many: no more are read than there are.)
+    if (W == 1 && (t < from || t >= to || cuts <= 1)) return;
     float y[kParts];
     float2 r = make_float2(kNone, 0.f);
-    const int most = p.splits - first;  // parts that there may be
+    const int most = (W == 1 ? min(cuts, p.splits) : p.splits) - first;
     if (lane < kParts && lane < most) r = p.part_row[(first + lane) * rows + row];
 #pragma unroll
-    for (int s0 = 0; s0 < kParts; s0 += 4)
+    for (int s0 = 0; s0 < kParts; s0 += 2)
         if (s0 < most)
 #pragma unroll
-            for (int s = s0; s < s0 + 4; ++s) y[s] = p.part[(first + min(s, most - 1)) * rows * 64 + row * 64 + lane];
+            for (int s = s0; s < s0 + 2; ++s) y[s] = p.part[(first + min(s, most - 1)) * rows * 64 + row * 64 + lane];
     if (t < from || t >= to || cuts <= 1) return;
     const int n = min(cuts, p.splits) - first;
     if (lane >= n) r = make_float2(kNone, 0.f);
@@ -242,7 +237,7 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
 #pragma unroll
         for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w]);
     }
-    const float w = r.y == 0.f ? 0.f : share<WIDE>(p, r.x, top);
+    const float w = r.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((r.x - top) * p.scale_log2);
     float sum = w == 0.f ? 0.f : r.y * w, o = 0.f;
 #pragma unroll
     for (int e = 1; e < 64; e <<= 1) sum += __shfl_xor(sum, e);
@@ -261,33 +256,24 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
     }
     p.o[h * p.os.head + t * p.os.token + lane] = (uint16_t)bf16_bits(sum == 0.f ? 0.f : o / sum);
     if (p.lse && lane == 0)
-        p.lse[row] = sum == 0.f ? -INFINITY : (WIDE ? p.refs.base2(top) * 0.6931471805599453f : top * p.scale) + logf(sum);
-}
-
-template <bool WIDE>
-hipError_t launch_join(const PagedParams &p, hipStream_t s)
-{
-    static_assert(kMaxPagedSplits <= 4 * kParts, "four waves hold a row's parts");
-    const int64_t rows = (int64_t)p.H * p.N;
-    if (p.splits <= kParts)
-        hipLaunchKernelGGL((join_kernel<WIDE, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
-    else
-        hipLaunchKernelGGL((join_kernel<WIDE, 4>), dim3((unsigned)rows), dim3(256), 0, s, p);
-    return hipGetLastError();
+        p.lse[row] = sum == 0.f ? -INFINITY : top * p.scale + logf(sum);
 }
 
 }  // namespace
 
 hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
 {
-    if (rows == 128) {
-        if (hipError_t e = launch_paged_wide(p, s)) return e;
-    } else {
-        hipLaunchKernelGGL(tile_kernel, dim3((unsigned)p.blocks, (unsigned)p.H_kv, (unsigned)p.splits), dim3(64 * kWaves), 0, s, p);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
+    static_assert(kMaxPagedSplits <= 4 * kParts, "four waves hold a row's parts");
+    if (rows == 128) return launch_paged_wide(p, s);
+    hipLaunchKernelGGL(tile_kernel, dim3((unsigned)p.blocks, (unsigned)p.H_kv, (unsigned)p.splits), dim3(64 * kWaves), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
     if (p.splits == 1) return hipSuccess;
-    return rows == 128 ? launch_join<true>(p, s) : launch_join<false>(p, s);
+    const int64_t all = (int64_t)p.H * p.N;
+    if (p.splits <= kParts)
+        hipLaunchKernelGGL((join_kernel<1>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, p);
+    else
+        hipLaunchKernelGGL((join_kernel<4>), dim3((unsigned)all), dim3(256), 0, s, p);
+    return hipGetLastError();
 }
 
 }  // namespace ress

@@ -24,6 +24,12 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 
 typedef const __attribute__((address_space(1))) void global_void;
 
+// Where a split's part of a block lies, in parts.
+__device__ __forceinline__ int64_t part_at(const PagedParams &p, int split, int hk, int block)
+{
+    return ((int64_t)split * p.H_kv + hk) * p.blocks + block;
+}
+
 // Eight rows from one on: at most 7 token strides of 2^22 elements and a row.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const unsigned char *row)
 {
@@ -41,8 +47,9 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     const int id = blockIdx.x + gridDim.x * blockIdx.y, at = (id & 7) * per + (id >> 3);
     if ((id >> 3) >= per || at >= items) return;
     const int hk = at / p.blocks, split = blockIdx.z;
+    const int block = p.blocks - 1 - (at - hk * p.blocks);
     Block x;
-    if (!find_block<kRows>(p, p.blocks - 1 - (at - hk * p.blocks), x)) return;
+    if (!find_block<kRows>(p, block, x)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hh = lane >> 5, ql = lane & 31;
 
@@ -251,23 +258,89 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     }
 
     sum += __shfl_xor(sum, 32);
-    if (wave * 32 + ql >= x.left) return;
-    const int h = hk * p.group + r.g;
-    const int64_t row = (int64_t)h * p.N + x.cu + r.t;
-    if (p.splits > 1 && split == 0 && hh == 0) p.cuts[row] = cuts;
     if (cuts > 1) {
-        const int64_t to = (int64_t)split * p.H * p.N + row;
+        // A part as the lanes hold it: whole lines, read back by wide_join_kernel the same way. (By rows they were written and read
+        // in pieces of 32 bytes: 512 blocks cut in three 86 us, so 77.)
+        const int64_t part = part_at(p, split, hk, block);
 #pragma unroll
-        for (int dh = 0; dh < 2; ++dh)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<f32x4 *>(p.part + to * 64 + dh * 32 + g * 8 + hh * 4) =
-                    f32x4{acc[dh][g * 4], acc[dh][g * 4 + 1], acc[dh][g * 4 + 2], acc[dh][g * 4 + 3]};
-        if (hh == 0) p.part_row[to] = make_float2(ref, sum);
+        for (int v = 0; v < 8; ++v)
+            *reinterpret_cast<f32x4 *>(p.part + (part * 4 + wave) * 2048 + v * 256 + lane * 4) =
+                f32x4{acc[v >> 2][(v & 3) * 4], acc[v >> 2][(v & 3) * 4 + 1], acc[v >> 2][(v & 3) * 4 + 2], acc[v >> 2][(v & 3) * 4 + 3]};
+        if (hh == 0) p.part_row[part * kRows + wave * 32 + ql] = make_float2(ref, sum);
         return;
     }
+    if (wave * 32 + ql >= x.left) return;
+    const int h = hk * p.group + r.g;
     store_row(p.o + h * p.os.head + (int64_t)(x.cu + r.t) * p.os.token, acc, inverse(sum), hh);
-    if (LSE && hh == 0) p.lse[row] = sum == 0.f ? -INFINITY : refs.base2(ref) * kLn2 + logf(sum);
+    if (LSE && hh == 0) p.lse[(int64_t)h * p.N + x.cu + r.t] = sum == 0.f ? -INFINITY : refs.base2(ref) * kLn2 + logf(sum);
+}
+
+// A quarter of the channels of a block whose keys were split, laid out as wide_kernel's: its parts in order, 8 of them on their
+// way at once.
+__global__ void __launch_bounds__(256) wide_join_kernel(const PagedParams p)
+{
+    const int id = blockIdx.x + gridDim.x * blockIdx.y;
+    if (id >= p.H_kv * p.blocks) return;
+    const int hk = id / p.blocks, block = id - hk * p.blocks, quad0 = blockIdx.z * 2;
+    Block x;
+    if (!find_block<kRows>(p, block, x)) return;
+    const int n = cuts_of(p, tiles_of(seen_at(p, x.pos0 + x.t0, x.len), seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len)).n,
+                          kWideLeast);
+    if (n == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5, ql = lane & 31;
+    const References refs = p.refs;
+    const int64_t step = (int64_t)p.H_kv * p.blocks;  // parts between splits
+    const float2 *rows = p.part_row + part_at(p, 0, hk, block) * kRows + wave * 32 + ql;
+    const float *from = p.part + (part_at(p, 0, hk, block) * 4 + wave) * 2048 + quad0 * 256 + lane * 4;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int s0 = 0; s0 < n; s0 += 8) {
+        float2 r[8];
+        f32x4 y[8][2];
+#pragma unroll
+        for (int s = 0; s < 8; s += 2)
+            if (s0 + s < n)
+#pragma unroll
+                for (int e = s; e < s + 2; ++e) {
+                    const int64_t at = min(s0 + e, n - 1) * step;
+                    r[e] = rows[at * kRows];
+                    if (s0 + e >= n) r[e].y = 0.f;
+                    y[e][0] = *reinterpret_cast<const f32x4 *>(from + at * 8192);
+                    y[e][1] = *reinterpret_cast<const f32x4 *>(from + at * 8192 + 256);
+                }
+        // (Parts without mass have none of the row's references.)
+        float to = top;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            if (s0 + (s & ~1) < n && r[s].y != 0.f) to = fmaxf(to, r[s].x);
+        const float a = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(refs.difference(top, to));
+        sum *= a;
+        o[0] *= a;
+        o[1] *= a;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            if (s0 + (s & ~1) < n) {
+                const float w = r[s].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(refs.difference(r[s].x, to));
+                sum = fmaf(r[s].y, w, sum);
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[q][e] = fmaf(y[s][q][e], w, o[q][e]);
+            }
+        top = to;
+    }
+    if (wave * 32 + ql >= x.left) return;
+    const Row r = row_of(p, x, wave * 32 + ql);
+    const int h = hk * p.group + r.g;
+    const float f = inverse(sum);
+    uint16_t *row = p.o + h * p.os.head + (int64_t)(x.cu + r.t) * p.os.token + hh * 4;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const unsigned int lo = bf16_bits(o[q][0] * f) | bf16_bits(o[q][1] * f) << 16, hi = bf16_bits(o[q][2] * f) | bf16_bits(o[q][3] * f) << 16;
+        *reinterpret_cast<uint2 *>(row + (quad0 + q) * 8) = make_uint2(lo, hi);
+    }
+    if (p.lse && quad0 == 0 && hh == 0)
+        p.lse[(int64_t)h * p.N + x.cu + r.t] = sum == 0.f ? -INFINITY : refs.base2(top) * kLn2 + logf(sum);
 }
 
 }  // namespace
@@ -282,6 +355,9 @@ hipError_t launch_paged_wide(const PagedParams &p, hipStream_t s)
         hipLaunchKernelGGL((wide_kernel<true>), grid, block, 0, s, p);
     else
         hipLaunchKernelGGL((wide_kernel<false>), grid, block, 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits == 1) return hipSuccess;
+    hipLaunchKernelGGL(wide_join_kernel, dim3(grid.x, grid.y, 4), block, 0, s, p);
     return hipGetLastError();
 }
 

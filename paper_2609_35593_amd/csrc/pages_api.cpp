@@ -247,18 +247,18 @@ int check_paged(const ress_paged_shape *s, bool strides)
     return RESS_OK;
 }
 
-// Where a workspace's parts begin: outputs, references and sums, cuts; its size.
+// Where a workspace's parts begin: outputs, references and sums, who shares a row; its size.
 struct PagedSpace {
     size_t rows, cuts, bytes;
 };
 PagedSpace paged_space(const ress_paged_shape *s, const PagedPlan &plan)
 {
     if (plan.splits == 1) return {0, 0, 0};
-    const size_t rows = (size_t)s->H * s->N;
+    const size_t rows = plan.rows == 32 ? (size_t)s->H * s->N : (size_t)s->H_kv * plan.blocks * 128;
     PagedSpace w;
     w.rows = plan.splits * rows * 64 * sizeof(float);
     w.cuts = w.rows + plan.splits * rows * sizeof(float2);
-    w.bytes = align256(w.cuts + rows * sizeof(int32_t));
+    w.bytes = align256(w.cuts + (plan.rows == 32 ? rows * sizeof(int32_t) : 0));
     return w;
 }
 

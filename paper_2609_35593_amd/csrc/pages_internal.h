@@ -93,9 +93,11 @@ struct PagedParams {
     const int32_t *cu_q, *lens, *tables;
     uint16_t *o;
     float *lse;
-    float *part;      // splits > 1: [splits][H][N][64], unnormalised outputs,
-    float2 *part_row; // [splits][H][N], references and sums,
-    int32_t *cuts;    // and [H][N], the workgroups that share a row's keys
+    // splits > 1: unnormalised outputs, and references and sums. 32 rows: [splits][H][N] of 64 floats, and [H][N], the
+    // workgroups that share a row's keys. 128 rows: [splits][H_kv][blocks] of 128 x 64, as the lanes hold them.
+    float *part;
+    float2 *part_row;
+    int32_t *cuts;
 };
 
 struct PagedPlan {

@@ -36,14 +36,30 @@ PagedPlan paged_plan(const ress_paged_shape *s)
     const int64_t capacity = (int64_t)s->max_pages * s->page;
     int64_t keys = window_tokens(s->frame, s->window) + s->n_sink + r.rows / group;
     if (keys > capacity) keys = capacity;
-    // Keys are cut over workgroups, of kTileLeast or kWideLeast tiles at least, while there are few blocks. (us by workgroups that share
-    // a block. 128 rows: 176 blocks of 687 tiles 1 / 5 / 8 / 16 793 / 342 / 333 / 313; 512 of up to 64, 1 / 4 / 16 104 / 90 / 93;
-    // 128 of 31, 1 / 3 43 / 38; but 176 of 21, 1 / 2 32 / 41. 32 rows: 192 blocks of 47 tiles 1 / 2 / 4 31.7 / 34.9 / 38.0, 384 55 /
-    // 58 / 62, 4 of 688, 16 / 32 / 64 33 / 25 / 24.)
-    const int64_t tiles = (keys + 63) / 64, blocks = (int64_t)r.blocks * s->H_kv;
-    const int64_t most = r.rows == 32 ? tiles / kTileLeast : tiles < 24 ? 1 : tiles / kWideLeast;
-    const int64_t want = (r.rows == 32 ? 256 : 2816) / blocks, n = want < most ? want : most;
-    r.splits = (int)(n < 1 ? 1 : n > kMaxPagedSplits ? kMaxPagedSplits : n);
+    const int64_t tiles = (keys + 63) / 64, n = (int64_t)r.blocks * s->H_kv;
+    int64_t want, most;
+    if (r.rows == 32) {
+        // Keys are cut over workgroups while there are few blocks. (us by workgroups that share a block, 1 / 2 / 4: 192 blocks of 47
+        // tiles 31.7 / 34.9 / 38.0, 384 55 / 58 / 62; 4 of 688, 16 / 32 / 64 33 / 25 / 24.)
+        want = 256 / n;
+        most = tiles / kTileLeast;
+    } else if (n >= 1000 || tiles < 24) {
+        // 1 / 3: 1,024 blocks of up to 64 tiles, 4 heads a K/V head, 96 / 119 (one head 150 / 128), 2,048 181 / 219, 1,250 of 18
+        // 78 / 84; 176 of 21 32.0 / 33.4.
+        return r;
+    } else {
+        // As many as fill the chip's 1,024 places once, by 80% at least and not to the last one, else nearly half as many
+        // again; long lists are cut further, into parts of 40 tiles. 1 / 2 / 3 / 4 / 6 / 8 / 16: 440 blocks of up to 66 tiles 107 / 94 /
+        // 92 / 92 / 92 / 94 / 92; 880 139 / 160 / 156; 512 of up to 64 102 / 90 / 77 / 77 / 78 / 78; 220 of 66 85 / 65 / 59 / 57 / 62; 176 of 86
+        // 106 / 81 / 72 / 61 / 68 / 64 / 64; 176 of 687 782 / 523 / 434 / 341 / 370 / 330 / 310; 128 of 64 78 / 48 / 45 / 38 / 37.
+        want = 1024 / n;
+        if (want * n < 820 || want * n > 1000) want = (1400 + n - 1) / n;
+        const int64_t parts = 2816 / n < tiles / 40 ? 2816 / n : tiles / 40;
+        if (parts > want) want = parts;
+        most = tiles / kWideLeast;
+    }
+    const int64_t splits = want < most ? want : most;
+    r.splits = (int)(splits < 1 ? 1 : splits > kMaxPagedSplits ? kMaxPagedSplits : splits);
     return r;
 }
 
