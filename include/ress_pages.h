@@ -168,7 +168,7 @@ typedef struct {
 } ress_paged_shape;
 
 /* Bytes of device workspace ress_paged_attn needs: partial results of keys that are split over
- * workgroups (at most 100 MB; strides do not matter). */
+ * workgroups (at most 100 MB), and a list of more than 512 sequences; strides do not matter. */
 int ress_paged_attn_workspace_size(const ress_paged_shape *shape, size_t *bytes);
 
 /* The new tokens of sequence b are rows cu_q[b] .. cu_q[b + 1] - 1 of q and the last ones of its lens[b] tokens,

@@ -59,28 +59,44 @@ __device__ __forceinline__ void block_of(const PagedParams &p, Block &x, int b, 
 
 constexpr int kMostBlocks = 1 << 29;  // sums of blocks stop here
 
-// Block `index` of all sequences' blocks of ROWS rows; false behind the last. Every thread of a
-// workgroup of 256 calls it. Up to 256 sequences each wave looks at all of them by itself, their offsets and
-// lengths in one round trip.
+// Block `index` of all sequences' blocks of ROWS rows; false behind the last. Each wave looks for itself: at all sequences, 256 of
+// them in one round trip, or, where there are more than kMostScanned, in the list of where each one's blocks begin, 64 ways at a
+// time. (One token of each of 512 / 768 / 1,024 / 4,096 / 16,384 sequences over 1,000 keys, us: 28.2 / 44.2 / 56.7 / 377 /
+// 3,927 by scans; 31.3 / 42.0 / 52 / 203 / 778 with the list and its launch.)
 template <int ROWS>
 __device__ __forceinline__ bool find_block(const PagedParams &p, int index, Block &x)
 {
     const int lane = threadIdx.x & 63;
-    if (p.B <= 256) {
-        int from[4], to[4], len[4], before = 0;
+    if (p.starts) {
+        if (index >= p.starts[p.B]) return false;
+        int b = 0;
+        for (int n = p.B; n > 1;) {
+            const int step = (n + 63) / 64, at = lane * step;
+            const int l = __popcll(__ballot(at < n && p.starts[b + min(at, n - 1)] <= index)) - 1;
+            b += l * step;
+            n = min(step, n - l * step);
+        }
+        b = __builtin_amdgcn_readfirstlane(b);
+        block_of<ROWS>(p, x, b, index - p.starts[b], rows_of(p, p.cu_q[b], p.cu_q[b + 1]), p.lens[b]);
+        return true;
+    }
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 256) {
+        int from[4], to[4], len[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (c * 64 < p.B) {
-                const int b = min(c * 64 + lane, p.B - 1);
+            if (b0 + c * 64 < p.B) {
+                const int b = min(b0 + c * 64 + lane, p.B - 1);
                 from[c] = p.cu_q[b];
                 to[c] = p.cu_q[b + 1];
                 len[c] = p.lens[b];
             }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            if (c * 64 >= p.B) break;
+            const int first = b0 + c * 64;
+            if (first >= p.B) break;
             const Rows r = rows_of(p, from[c], to[c]);
-            const int blocks = c * 64 + lane < p.B ? r.blocks<ROWS>(p) : 0;
+            const int blocks = first + lane < p.B ? r.blocks<ROWS>(p) : 0;
             int sum = blocks;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -91,47 +107,15 @@ __device__ __forceinline__ bool find_block(const PagedParams &p, int index, Bloc
             const uint64_t here = __ballot(blocks > 0 && index < sum && index >= sum - blocks);
             if (here) {
                 const int l = __builtin_ctzll(here);
-                block_of<ROWS>(p, x, c * 64 + l, index - __builtin_amdgcn_readlane(sum - blocks, l),
+                block_of<ROWS>(p, x, first + l, index - __builtin_amdgcn_readlane(sum - blocks, l),
                                {__builtin_amdgcn_readlane(r.cu, l), __builtin_amdgcn_readlane(r.end, l)},
                                __builtin_amdgcn_readlane(len[c], l));
                 return true;
             }
             before = __builtin_amdgcn_readlane(sum, 63);
         }
-        return false;
     }
-    __shared__ int found[2], ends[4];
-    const int wave = threadIdx.x >> 6;
-    int before = 0;
-    if (threadIdx.x == 0) found[0] = -1;
-    for (int b0 = 0; b0 < p.B; b0 += 256) {
-        const int b = b0 + threadIdx.x;
-        const int blocks = b < p.B ? rows_of(p, p.cu_q[b], p.cu_q[b + 1]).blocks<ROWS>(p) : 0;
-        int sum = blocks;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(sum, o);
-            if (lane >= o) sum = min(sum + y, kMostBlocks);
-        }
-        if (lane == 63) ends[wave] = sum;
-        __syncthreads();
-        int head = before;
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) head = min(head + ends[w], kMostBlocks);
-            before = min(before + ends[w], kMostBlocks);
-        }
-        sum = min(sum + head, kMostBlocks);
-        if (blocks > 0 && index < sum && index >= sum - blocks) {
-            found[0] = b;
-            found[1] = index - (sum - blocks);
-        }
-        __syncthreads();
-        if (before > index) break;
-    }
-    const int b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (b < 0) return false;
-    block_of<ROWS>(p, x, b, __builtin_amdgcn_readfirstlane(found[1]), rows_of(p, p.cu_q[b], p.cu_q[b + 1]), p.lens[b]);
-    return true;
+    return false;
 }
 
 // The keys that position pos of a sequence of len tokens sees: [lo, hi) and [0, sk). (Before its first: none.)

@@ -201,6 +201,36 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams 
     }
 }
 
+// Where every sequence's blocks of `rows` rows begin, and how many blocks there are: one workgroup.
+constexpr int kStartThreads = 1024;
+__global__ void __launch_bounds__(kStartThreads) starts_kernel(const PagedParams p, int rows)
+{
+    __shared__ int ends[kStartThreads / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kStartThreads) {
+        const int b = b0 + threadIdx.x;
+        const Rows r = b < p.B ? rows_of(p, p.cu_q[b], p.cu_q[b + 1]) : Rows{0, 0};
+        const int own = rows == kRows ? r.blocks<kRows>(p) : r.blocks<128>(p);
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(sum, o);
+            if (lane >= o) sum = min(sum + y, kMostBlocks);
+        }
+        if (lane == 63) ends[wave] = sum;
+        __syncthreads();
+        int start = min(before + (sum - own), kMostBlocks);
+        for (int w = 0; w < kStartThreads / 64; ++w) {
+            if (w < wave) start = min(start + ends[w], kMostBlocks);
+            before = min(before + ends[w], kMostBlocks);
+        }
+        if (b < p.B) p.starts[b] = start;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) p.starts[p.B] = before;
+}
+
 // A row by W waves, a channel a lane, 16 parts a wave: all of a wave's parts are on their way at once, their weights one
 // a lane first; the waves' sums are added in order. Rows outside every sequence, and those that one workgroup
 // finished, are left as they are. (What a row does not have of p.splits parts may hold anything.)
@@ -264,6 +294,10 @@ __global__ void __launch_bounds__(256) join_kernel(const PagedParams p)
 hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
 {
     static_assert(kMaxPagedSplits <= 4 * kParts, "four waves hold a row's parts");
+    if (p.starts) {
+        hipLaunchKernelGGL(starts_kernel, dim3(1), dim3(kStartThreads), 0, s, p, rows);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
     if (rows == 128) return launch_paged_wide(p, s);
     hipLaunchKernelGGL(tile_kernel, dim3((unsigned)p.blocks, (unsigned)p.H_kv, (unsigned)p.splits), dim3(64 * kWaves), 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;

@@ -247,18 +247,20 @@ int check_paged(const ress_paged_shape *s, bool strides)
     return RESS_OK;
 }
 
-// Where a workspace's parts begin: outputs, references and sums, who shares a row; its size.
+// Where a workspace's parts begin: outputs, references and sums, who shares a row, where sequences' blocks begin; its size.
 struct PagedSpace {
-    size_t rows, cuts, bytes;
+    size_t rows, cuts, starts, bytes;
 };
 PagedSpace paged_space(const ress_paged_shape *s, const PagedPlan &plan)
 {
-    if (plan.splits == 1) return {0, 0, 0};
-    const size_t rows = plan.rows == 32 ? (size_t)s->H * s->N : (size_t)s->H_kv * plan.blocks * 128;
-    PagedSpace w;
-    w.rows = plan.splits * rows * 64 * sizeof(float);
-    w.cuts = w.rows + plan.splits * rows * sizeof(float2);
-    w.bytes = align256(w.cuts + (plan.rows == 32 ? rows * sizeof(int32_t) : 0));
+    PagedSpace w = {0, 0, 0, 0};
+    if (plan.splits > 1) {
+        const size_t rows = plan.rows == 32 ? (size_t)s->H * s->N : (size_t)s->H_kv * plan.blocks * 128;
+        w.rows = plan.splits * rows * 64 * sizeof(float);
+        w.cuts = w.rows + plan.splits * rows * sizeof(float2);
+        w.starts = w.cuts + (plan.rows == 32 ? rows * sizeof(int32_t) : 0);
+    }
+    w.bytes = align256(w.starts + (plan.blocks > 0 && s->B > kMostScanned ? ((size_t)s->B + 1) * sizeof(int32_t) : 0));
     return w;
 }
 
@@ -515,8 +517,9 @@ int ress_paged_attn(const ress_paged_shape *shape, const void *q, const void *k,
     p.tables = tables;
     p.o = static_cast<uint16_t *>(o);
     p.lse = lse;
+    char *const w = static_cast<char *>(workspace);
+    if (s.B > kMostScanned) p.starts = reinterpret_cast<int32_t *>(w + space.starts);
     if (plan.splits > 1) {
-        char *const w = static_cast<char *>(workspace);
         p.part = reinterpret_cast<float *>(w);
         p.part_row = reinterpret_cast<float2 *>(w + space.rows);
         p.cuts = reinterpret_cast<int32_t *>(w + space.cuts);

@@ -98,8 +98,10 @@ struct PagedParams {
     float *part;
     float2 *part_row;
     int32_t *cuts;
+    int32_t *starts;  // [B + 1], of more than kMostScanned sequences: blocks before each one's, and all
 };
 
+constexpr int kMostScanned = 512;  // (see find_block)
 struct PagedPlan {
     int rows;    // of a block
     int blocks, splits;

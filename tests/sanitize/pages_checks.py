@@ -120,7 +120,8 @@ def paged(B, N, H, H_kv, page, n_pages, max_pages, frame, window, sink, k=(1 << 
         seen["rows"].add(rows)
         seen["splits"].add((rows, splits))
         share = H * N if rows == 32 else H_kv * blocks * 128
-        assert n == (0 if splits == 1 else (splits * share * 264 + (4 * share if rows == 32 else 0) + 255) // 256 * 256), what
+        parts = 0 if splits == 1 else splits * share * 264 + (4 * share if rows == 32 else 0)
+        assert n == (parts + (4 * (B + 1) if B > 512 else 0) + 255) // 256 * 256, what
     st = legal(lib.ress_paged_attn(C.byref(s), *P[:6], 0.125, P[6], P[7], P[8], n, None))
     assert st == (E_HIP if B and N and H else 0), (what, st)
     if n:
@@ -129,7 +130,7 @@ def paged(B, N, H, H_kv, page, n_pages, max_pages, frame, window, sink, k=(1 << 
 
 
 HEADS = [(1, 1), (8, 2), (16, 16), (256, 1), (256, 256), (12, 4)]
-for (H, H_kv), B, N, (page, max_pages) in itertools.product(HEADS, (0, 1, 24, 65535), (0, 1, 127, 1374, TOKENS),
+for (H, H_kv), B, N, (page, max_pages) in itertools.product(HEADS, (0, 1, 24, 512, 513, 65535), (0, 1, 127, 1374, TOKENS),
                                                             ((1, TOKENS), (16, 1 << 20), (64, 700), (TOKENS, 1), (24, 0), (7, 1))):
     for frame, window, sink in ((1, 1, 0), (TOP, TOP, TOP), (1, TOP, 0), (1374, 4, 1374)):
         assert paged(B, N, H, H_kv, page, min(TOP // page, 1000), max_pages, frame, window, sink)

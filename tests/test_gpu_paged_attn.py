@@ -233,6 +233,18 @@ def test_many_sequences(ress):
         _check(ress, q, k, v, cu, lens, tables, 1, 50, 3)
 
 
+@pytest.mark.parametrize("B", [512, 513, 4097])
+@pytest.mark.parametrize("many", [0, 130])
+def test_thousands_of_sequences(ress, B, many):
+    """Around the number from which a list tells where sequences' blocks begin, and beyond; blocks of 32 rows and of 128, empty
+    sequences first, last and between, and rows behind the last."""
+    g = torch.Generator().manual_seed(B + many)
+    lens = torch.randint(many, 60 + many, (B,), generator=g).tolist()
+    new = [0 if i % 5 == 0 or i == B - 1 else min(n, many or 1 + i % 3) for i, n in enumerate(lens)]
+    q, k, v, cu, tables = _state(B, 1, 1, 32, lens, new, padding=5)
+    _check(ress, q, k, v, cu, lens, tables, 1, 40, 2)
+
+
 def test_captured_call_follows_its_lengths(ress):
     """One graph over steps whose lengths, offsets and tables change, beside eager work; a second one with a workspace of its own."""
     H, H_kv, page, B, N = 8, 2, 16, 3, 60

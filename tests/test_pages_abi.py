@@ -294,6 +294,12 @@ def test_paged_attn_refusals(ress):
     n = C.c_size_t(0)
     assert size(C.byref(long), C.byref(n)) == OK and n.value > 0 and size(C.byref(long), None) == INVALID
     assert call(long, ws=None) == WORKSPACE and call(long, nb=n.value - 1) == WORKSPACE and call(long, ws=off(P[10], 64)) == WORKSPACE
+    # A list of more than 512 sequences, whatever their keys.
+    for B, need in ((512, 0), (513, 514 * 4), (65535, 65536 * 4)):
+        sh = _paged(B=B, N=B, page=16, max_pages=2, n_pages=2 * B, table_stride=2, q=(64 << 16, 64), o=(64 << 16, 64))
+        assert size(C.byref(sh), C.byref(n)) == OK and n.value == -(-need // 256) * 256, B
+        if need:
+            assert call(sh, ws=None) == WORKSPACE and call(sh, nb=n.value - 1) == WORKSPACE
 
 
 def test_binding_refuses_host_tensors_and_shapes(ress):
