@@ -10,7 +10,7 @@ namespace ress {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kMost = 1 << 28;  // sums of tokens and pages stop here (more than any N or n_pages takes, less than 2^31 with one more)
+constexpr int kMost = 1 << 28;  // sums of tokens, and of pages for them, stop here (more than any N takes, less than 2^31 with one more)
 
 // Tokens and pages, whose sums stop at kMost. (The least of a sum and a bound: associative, so the order of a scan is free.)
 struct Need {
@@ -169,6 +169,9 @@ __global__ void __launch_bounds__(kListThreads) lists_kernel(const TableParams p
 
 constexpr int kScan = 1024;  // sequences up to which every workgroup adds up the counts before its own
 
+// Heights of the stack, which stop at 2^31 - 1 (no n_pages is more).
+__device__ __forceinline__ uint32_t higher(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
+
 __device__ __forceinline__ bool valid(const ReleaseParams &p, int page) { return (unsigned int)page < (unsigned int)p.n_pages; }
 
 // A workgroup a sequence: how many of its entries go back. (The stack's height is kept beside the
@@ -189,25 +192,30 @@ __global__ void __launch_bounds__(256) count_kernel(const ReleaseParams p)
     if (b == 0 && threadIdx.x == 0) p.counts[p.B] = min(max(p.n_free[0], 0), p.n_pages);
 }
 
-// Many sequences: counts become the sums before them (at most kMost), by one workgroup.
+// Many sequences: counts become the sums before them, by one workgroup.
 __global__ void __launch_bounds__(kThreads) sums_kernel(const ReleaseParams p)
 {
-    __shared__ Need waves[kWaves];
+    __shared__ uint32_t waves[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Need before = {0, 0};
+    uint32_t before = 0;
     for (int b0 = 0; b0 < p.B; b0 += kThreads) {
         const int b = b0 + threadIdx.x;
-        const Need own = {b < p.B ? p.counts[b] : 0, 0};
-        Need sum = scan_wave(own, lane);
-        if (lane == 63) waves[wave] = sum;
-        __syncthreads();
-        Need head = before;
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) head = head + waves[w];
-            before = before + waves[w];
+        const uint32_t own = b < p.B ? p.counts[b] : 0;
+        uint32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t y = __shfl_up(sum, o);
+            if (lane >= o) sum = higher(sum, y);
         }
-        sum = head + sum;
-        if (b < p.B) p.counts[b] = sum.tokens - own.tokens;
+        if (lane == 63) waves[wave] = sum;
+        const uint32_t up = __shfl_up(sum, 1);  // (of the lanes before: a sum that stopped tells nothing of what it is without one's own)
+        uint32_t head = higher(before, lane ? up : 0);
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) head = higher(head, waves[w]);
+            before = higher(before, waves[w]);
+        }
+        if (b < p.B) p.counts[b] = (int32_t)head;
         __syncthreads();
     }
 }
@@ -215,19 +223,19 @@ __global__ void __launch_bounds__(kThreads) sums_kernel(const ReleaseParams p)
 // A workgroup a sequence: its entries onto the stack, in order.
 __global__ void __launch_bounds__(256) push_kernel(const ReleaseParams p, bool summed)
 {
-    __shared__ int waves[4];
+    __shared__ uint32_t waves[4];
     const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int first = min(max(p.first[b], 0), p.max_pages), last = min(max(p.last[b], 0), p.max_pages);
     int32_t *row = p.tables + (int64_t)b * p.stride;
-    int at = summed && threadIdx.x == 0 ? p.counts[b] : 0;
+    uint32_t at = summed && threadIdx.x == 0 ? p.counts[b] : 0;
     if (!summed)
-        for (int i = threadIdx.x; i < b; i += 256) at = min(at + p.counts[i], kMost);
+        for (int i = threadIdx.x; i < b; i += 256) at = higher(at, p.counts[i]);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) at = min(at + __shfl_xor(at, o), kMost);
+    for (int o = 1; o < 64; o <<= 1) at = higher(at, __shfl_xor(at, o));
     if (lane == 0) waves[wave] = at;
     __syncthreads();
     at = p.counts[p.B];
-    for (int w = 0; w < 4; ++w) at = min(at + waves[w], kMost);
+    for (int w = 0; w < 4; ++w) at = higher(at, waves[w]);
     for (int i0 = first; i0 < last; i0 += 256) {
         const int i = i0 + (int)threadIdx.x;
         const int page = i < last ? row[i] : -1;
@@ -236,17 +244,17 @@ __global__ void __launch_bounds__(256) push_kernel(const ReleaseParams p, bool s
         __syncthreads();
         if (lane == 0) waves[wave] = __popcll(in_wave);
         __syncthreads();
-        int to = at + __popcll(in_wave & ((1ull << lane) - 1));
+        uint32_t to = at + __popcll(in_wave & ((1ull << lane) - 1));
         for (int w = 0; w < 4; ++w) {
             if (w < wave) to += waves[w];
-            at = min(at + waves[w], kMost);
+            at = higher(at, waves[w]);
         }
         if (back) {
-            if (to < p.n_pages) p.free_pages[to] = page;
+            if (to < (uint32_t)p.n_pages) p.free_pages[to] = page;
             if (p.clear) row[i] = -1;
         }
     }
-    if (b == p.B - 1 && threadIdx.x == 0) p.n_free_out[0] = min(at, p.n_pages);
+    if (b == p.B - 1 && threadIdx.x == 0) p.n_free_out[0] = (int32_t)min(at, (uint32_t)p.n_pages);
 }
 
 // No sequences: the stack stays as it is.

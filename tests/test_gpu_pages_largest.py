@@ -169,3 +169,29 @@ def test_the_last_slots(ress):
     slots = torch.tensor([(1 << 24) - 1, 1 << 24, 0], dtype=I32, device="cuda")
     ress.ress_qk_norm_rope_pages(None, k, k, pos, slots, big, out, dims=(64,))
     assert torch.equal(out[0, 0, -1], k[0, 0]) and torch.equal(out[0, 0, 0], k[0, 2]) and out.count_nonzero() == 128
+
+
+@pytest.mark.parametrize("B", [3, 1500])
+def test_a_stack_of_more_than_2_28_pages(ress, B):
+    """Pages given back to, and taken from, heights beyond 2^28, and a stack that is full before the last entry."""
+    say("[largest] stack", B)
+    n_pages = (1 << 28) + 5 * B
+    height = n_pages - 4 * B
+    free = torch.zeros(n_pages, dtype=I32, device="cuda")
+    want = torch.arange(5 * B, dtype=I32, device="cuda") * 7 + n_pages - 40 * B
+    tables = torch.full((B, 8), -1, dtype=I32, device="cuda")
+    tables[:, 1:6] = want.view(B, 5)
+    first, last = (torch.full((B,), i, dtype=I32, device="cuda") for i in (0, 8))
+    n_free = torch.full((1,), height, dtype=I32, device="cuda")
+    out = ress.ress_pages_release(first, last, tables, free, n_free)
+    assert out.tolist() == [n_pages]  # a fifth of the entries has no room
+    assert torch.equal(free[height:], want[:4 * B]) and not free[:1000].any() and free[height - 1000:height].count_nonzero() == 0
+    assert (tables == -1).all()
+    # Two tokens of each sequence, on pages of one: from the top of the stack down.
+    r = ress.ress_page_tables(torch.zeros_like(first), torch.full_like(first, 2), tables, free, out, page=1, tokens=2 * B)
+    assert r["n_free"].tolist() == [n_pages - 2 * B] and r["n_refused"].tolist() == [0]
+    taken = want[:4 * B].flip(0)[:2 * B]
+    assert torch.equal(tables[:, :2].reshape(-1), taken) and torch.equal(r["slots"], taken)
+    # The first of each goes back.
+    out = ress.ress_pages_release(torch.zeros_like(first), torch.full_like(first, 1), tables, free, r["n_free"])
+    assert out.tolist() == [n_pages - B] and torch.equal(free[n_pages - 2 * B:n_pages - B], taken.view(B, 2)[:, 0])
