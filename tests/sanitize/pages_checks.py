@@ -88,8 +88,8 @@ for _ in range(20000):
     if H == 0 or N == 0:
         assert parts == 0 and most == 1
         continue
-    assert 1 <= tokens <= -(-N // each) and 1 <= heads <= H and parts == tokens * -(-H // heads) and parts <= most <= 1024, (H, N, each)
-    assert tokens == min(-(-N // each), 1024)
+    assert 1 <= tokens <= -(-N // each) and 1 <= heads <= H and parts == tokens * -(-H // heads) and parts <= most <= 768, (H, N, each)
+    assert tokens == min(-(-N // each), 768)
 
 # -------------------------------------------------------------------- pages
 reached = 0

@@ -151,6 +151,19 @@ def test_offsets_that_descend_or_pass_the_rows(ress):
         assert (buf[:, :3] == 7.0).all() and (buf[:, 20:] == 7.0).all()
 
 
+def test_thousands_of_offsets_in_no_order(ress):
+    """The same with a list of where blocks begin."""
+    g = torch.Generator().manual_seed(3)
+    q, k, v, cu, tables = _state(2, 2, 1, 16, [40] * 700, [1] * 700)
+    k, v = k.nan_to_num(0.5), v.nan_to_num(0.5)
+    buf = torch.full((2, 720, 64), 7.0, dtype=BF, device="cuda")
+    for lo, hi in ((0, 700), (-10, 900), (-2 ** 31, 2 ** 31 - 1)):
+        bad = torch.randint(lo, hi, (701,), generator=g).tolist()
+        ress.ress_paged_attn(q, k, v, _t(bad), _t([40] * 700), tables, window=30, out=buf[:, 3:703])
+        torch.cuda.synchronize()
+        assert (buf[:, :3] == 7.0).all() and (buf[:, 703:] == 7.0).all()
+
+
 def test_offsets_that_begin_behind_the_first_row(ress):
     lens, new = [9000, 70], [1, 2]
     q, k, v, cu, tables = _state(3, 8, 2, 16, lens, new, padding=6)
