@@ -14,7 +14,7 @@ SOURCES = ["pool.hip", "select.hip", "attn.hip", "proj.hip", "drift.hip", "ress_
            "norm.hip", "rope.hip", "window.hip", "window_bwd.hip", "window_decode.hip", "layer_plan.cpp", "layer_api.cpp",
            "heads.hip", "pages.hip", "paged_tile.hip", "paged_wide.hip", "pages_plan.cpp", "pages_api.cpp"]
 HEADERS = [os.path.join(CSRC, h) for h in ("ress_internal.h", "layer_internal.h", "tiles.h", "checks.h", "pages_internal.h",
-                                            "paged_device.h")]
+                                            "scan.h", "paged_device.h")]
 HEADERS += [os.path.join(HERE, "..", "include", h) for h in ("ress.h", "ress_layer.h", "ress_pages.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-ffp-contract=fast",

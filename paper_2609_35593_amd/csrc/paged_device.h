@@ -3,6 +3,7 @@
 #pragma once
 
 #include "pages_internal.h"
+#include "scan.h"
 #include "tiles.h"
 
 namespace ress {
@@ -58,6 +59,7 @@ __device__ __forceinline__ void block_of(const PagedParams &p, Block &x, int b, 
 }
 
 constexpr int kMostBlocks = 1 << 29;  // sums of blocks stop here
+__device__ __forceinline__ int sum_of(int a, int b) { return min(a + b, kMostBlocks); }
 
 // Block `index` of all sequences' blocks of ROWS rows; false behind the last. Each wave looks for itself: at all sequences, 256 of
 // them in one round trip, or, where there are more than kMostScanned, in the list of where each one's blocks begin, 64 ways at a
@@ -97,13 +99,7 @@ __device__ __forceinline__ bool find_block(const PagedParams &p, int index, Bloc
             if (first >= p.B) break;
             const Rows r = rows_of(p, from[c], to[c]);
             const int blocks = first + lane < p.B ? r.blocks<ROWS>(p) : 0;
-            int sum = blocks;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(sum, o);
-                if (lane >= o) sum = min(sum + y, kMostBlocks);
-            }
-            sum = min(sum + before, kMostBlocks);
+            const int sum = sum_of(scan_wave(blocks, sum_of), before);
             const uint64_t here = __ballot(blocks > 0 && index < sum && index >= sum - blocks);
             if (here) {
                 const int l = __builtin_ctzll(here);

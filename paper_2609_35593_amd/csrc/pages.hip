@@ -9,6 +9,7 @@
 // tokens each 7.4 and 2.0 for their 65,538 slots and positions. Pages given back by 64 sequences: 2.7 us for the counts, 3.8 for
 // the stack (a launch between, because a stack's height depends on every sequence before).
 #include "pages_internal.h"
+#include "scan.h"
 
 namespace ress {
 namespace {
@@ -20,20 +21,9 @@ constexpr int kMost = 1 << 28;  // sums of tokens, and of pages for them, stop h
 struct Need {
     int tokens, pages;
 };
-__device__ __forceinline__ Need operator+(Need a, Need b)
-{
-    return {min(a.tokens + b.tokens, kMost), min(a.pages + b.pages, kMost)};
-}
-
-__device__ __forceinline__ Need scan_wave(Need x, int lane)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const Need y = {__shfl_up(x.tokens, o), __shfl_up(x.pages, o)};
-        if (lane >= o) x = x + y;
-    }
-    return x;
-}
+__device__ __forceinline__ int sum_of(int a, int b) { return min(a + b, kMost); }
+__device__ __forceinline__ Need operator+(Need a, Need b) { return {sum_of(a.tokens, b.tokens), sum_of(a.pages, b.pages)}; }
+__device__ __forceinline__ Need scan_needs(Need x) { return {scan_wave(x.tokens, sum_of), scan_wave(x.pages, sum_of)}; }
 
 // The last of [0, n) whose entry of the ascending list is at most x (list[0] <= x).
 __device__ __forceinline__ int last_at_most(const int *list, int n, int x)
@@ -73,7 +63,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const TableParams p, boo
         const bool fits = want <= capacity - len;
         Need own = {0, 0};
         if (fits) own = {want, pages_for(p, len + want) - pages_for(p, len)};
-        Need sum = scan_wave(own, lane);
+        Need sum = scan_needs(own);
         if (lane == 63) waves[wave] = sum;
         __syncthreads();
         Need head = before;
@@ -205,12 +195,7 @@ __global__ void __launch_bounds__(kThreads) sums_kernel(const ReleaseParams p)
     for (int b0 = 0; b0 < p.B; b0 += kThreads) {
         const int b = b0 + threadIdx.x;
         const uint32_t own = b < p.B ? p.counts[b] : 0;
-        uint32_t sum = own;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t y = __shfl_up(sum, o);
-            if (lane >= o) sum = higher(sum, y);
-        }
+        const uint32_t sum = scan_wave((int)own, [](int a, int b) { return (int)higher(a, b); });
         if (lane == 63) waves[wave] = sum;
         const uint32_t up = __shfl_up(sum, 1);  // (of the lanes before: a sum that stopped tells nothing of what it is without one's own)
         uint32_t head = higher(before, lane ? up : 0);

@@ -495,6 +495,9 @@ int ress_paged_attn(const ress_paged_shape *shape, const void *q, const void *k,
     p.table_stride = s.table_stride;
     p.blocks = plan.blocks;
     p.splits = plan.splits;
+    p.share = (float)s.H_kv / kTileParts;
+    const int64_t reach = window_tokens(s.frame, s.window) + s.n_sink;
+    p.most_keys = (int)(reach < p.capacity ? reach : p.capacity);
     p.scale = scale;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.refs = references(p.scale_log2);

@@ -84,6 +84,8 @@ struct PagedParams {
     int64_t table_stride;
     int blocks;  // of all sequences, at most
     int splits;  // workgroups that share a block's keys, at most
+    float share;    // 32 rows, splits > 1: of all sequences' keys of a K/V head, what a workgroup takes
+    int most_keys;  // that a token sees
     References refs;
     float scale, scale_log2;
     ress_strides qs, os;
@@ -111,6 +113,8 @@ struct PagedPlan {
 };
 PagedPlan paged_plan(const ress_paged_shape *s);
 constexpr int kMaxPagedSplits = 64;
+constexpr int kMostCut = 256;    // sequences up to which keys are cut
+constexpr int kTileParts = 256;  // workgroups that blocks of 32 rows are cut for
 constexpr int kTileLeast = 4, kWideLeast = 10;  // tiles of a workgroup at least where keys are cut (a wave one; see paged_plan)
 
 hipError_t launch_head_norm(const HeadNormParams &p, hipStream_t s);

@@ -39,9 +39,14 @@ PagedPlan paged_plan(const ress_paged_shape *s)
     const int64_t tiles = (keys + 63) / 64, n = (int64_t)r.blocks * s->H_kv;
     int64_t want, most;
     if (r.rows == 32) {
-        // Keys are cut over workgroups while there are few blocks. (us by workgroups that share a block, 1 / 2 / 4: 192 blocks of 47
-        // tiles 31.7 / 34.9 / 38.0, 384 55 / 58 / 62; 4 of 688, 16 / 32 / 64 33 / 25 / 24.)
-        want = 256 / n;
+        // Parts by keys (see find_part), as many as kTileParts workgroups need for one long sequence; of more rows 16, which a wave joins.
+        // (us where a block is one part / where parts go by keys: single tokens of 64 sequences of 1 to 30,000 keys on a log scale, 16
+        // heads for 4, 242 / 46; 250 of 1 to 6,000 evenly, one K/V head, 56 / 50, all of 3,000 36 / 38; 96 with 4 K/V heads 77 /
+        // 75, all of 3,000 55 / 57.)
+        if (s->B > kMostCut || n > 1024 || tiles < 2 * kTileLeast) return r;
+        want = kTileParts / s->H_kv;
+        if (want > 8192 / n) want = 8192 / n;
+        if (want > 16 && (int64_t)s->H * s->N > 512) want = 16;
         most = tiles / kTileLeast;
     } else if (n >= 1000 || tiles < 24) {
         // 1 / 3: 1,024 blocks of up to 64 tiles, 4 heads a K/V head, 96 / 119 (one head 150 / 128), 2,048 181 / 219, 1,250 of 18

@@ -246,6 +246,16 @@ def test_many_sequences(ress):
         _check(ress, q, k, v, cu, lens, tables, 1, 50, 3)
 
 
+@pytest.mark.parametrize("B,H,H_kv,top,new", [(60, 8, 4, 6000, 1), (60, 8, 4, 6000, 30), (130, 2, 1, 5000, 1), (130, 2, 1, 5000, 90),
+                                              (256, 2, 2, 700, 1), (257, 2, 2, 700, 1), (40, 16, 16, 900, 1)])
+def test_uneven_lengths(ress, B, H, H_kv, top, new):
+    """Keys cut by sequences' lengths, from one to `top` on a log scale: single tokens and chunks, some sequences without any."""
+    lens = [round(top ** (i / (B - 1))) for i in range(B)]
+    q, k, v, cu, tables = _state(B + new, H, H_kv, 16, lens, [0 if i % 9 == 4 else min(n, new) for i, n in enumerate(lens)])
+    _check(ress, q, k, v, cu, lens, tables)
+    _check(ress, q, k, v, cu, lens, tables, 5, 60, 30)
+
+
 @pytest.mark.parametrize("B", [512, 513, 4097])
 @pytest.mark.parametrize("many", [0, 130])
 def test_thousands_of_sequences(ress, B, many):
