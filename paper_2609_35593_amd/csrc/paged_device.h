@@ -114,6 +114,74 @@ __device__ __forceinline__ bool find_block(const PagedParams &p, int index, Bloc
     return false;
 }
 
+// A block's part: of `cuts`, the block's index among all sequences', and among all parts the first one's and how far apart they
+// are.
+struct Part {
+    Block x;
+    int split, cuts, block, first, step;
+};
+
+// The part that `pick` names by its index among all blocks' parts; false where there is none. pick is given how many parts there are,
+// with COUNT, and may answer -1. A block's parts go by its share of all keys, so that workgroups hold about as many each, whatever
+// the sequences' lengths (by as many parts for each block, single tokens of 24 sequences of 1 to 20,000 keys on a log scale, 16
+// heads for 4, 90 us, so 21; of 28 of up to 33,462 evenly, 8 heads for one, 51 and 33). Of a sequence the parts of one
+// range of keys lie side by side. Each wave looks by itself. The weights are the keys that a sequence's last token sees, their sums
+// float32 in a fixed order: the same in every workgroup.
+template <int ROWS, bool COUNT, class Pick>
+__device__ __forceinline__ bool find_part(const PagedParams &p, Pick pick, Part &part)
+{
+    const int lane = threadIdx.x & 63;
+    int from = 0, to = 0, len = 0, blocks = 0;
+    float keys = 0.f, all = 0.f;
+    auto look = [&](int b0) __attribute__((always_inline)) {
+        const int b = min(b0 + lane, p.B - 1);
+        from = p.cu_q[b];
+        to = p.cu_q[b + 1];
+        len = p.lens[b];
+        blocks = b0 + lane < p.B ? rows_of(p, from, to).blocks<ROWS>(p) : 0;
+        keys = (float)min(max(len, 0), p.most_keys);
+    };
+#pragma nounroll
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        look(b0);
+        all = fmaf((float)blocks, keys, all);
+    }
+    const float each = 1.f / fmaxf(sum_wave(all) * p.share, (float)((ROWS == 32 ? kTileLeast : kWideLeast) * kTile));
+    auto cuts_each = [&]() __attribute__((always_inline)) { return min(max((int)fmaf(keys, each, 0.5f), 1), p.splits); };
+    int total = 0;
+    if constexpr (COUNT)
+#pragma nounroll
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            if (p.B > 64) look(b0);
+            total = sum_of(total, __builtin_amdgcn_readlane(scan_wave(blocks * cuts_each(), sum_of), 63));
+        }
+    const int index = pick(total);
+    int before = 0, blocks_before = 0;
+#pragma nounroll
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (p.B > 64) look(b0);
+        const int cuts = cuts_each(), parts = blocks * cuts;
+        const int sum = sum_of(scan_wave(parts, sum_of), before), blocks_sum = COUNT ? sum_of(scan_wave(blocks, sum_of), blocks_before) : 0;
+        const uint64_t here = __ballot(parts > 0 && index < sum && index >= sum - parts);
+        if (here) {
+            const int l = __builtin_ctzll(here), first = __builtin_amdgcn_readlane(sum - parts, l), at = index - first;
+            const Rows r = rows_of(p, from, to);
+            part.cuts = __builtin_amdgcn_readlane(cuts, l);
+            part.step = __builtin_amdgcn_readlane(blocks, l);
+            part.split = __builtin_amdgcn_readfirstlane((int)((uint32_t)at / (uint32_t)part.step));
+            const int block = at - part.split * part.step;
+            part.first = first + block;
+            part.block = __builtin_amdgcn_readlane(blocks_sum - blocks, l) + block;
+            block_of<ROWS>(p, part.x, b0 + l, block, {__builtin_amdgcn_readlane(r.cu, l), __builtin_amdgcn_readlane(r.end, l)},
+                           __builtin_amdgcn_readlane(len, l));
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(sum, 63);
+        blocks_before = __builtin_amdgcn_readlane(blocks_sum, 63);
+    }
+    return false;
+}
+
 // The keys that position pos of a sequence of len tokens sees: [lo, hi) and [0, sk). (Before its first: none.)
 __device__ __forceinline__ Seen seen_at(const PagedParams &p, int pos, int len)
 {
@@ -155,12 +223,6 @@ __device__ __forceinline__ void drop(f32x16 &s, unsigned int bits)
         const float x = s[v];  // (the bit cast of a vector's element in place reads its first one)
         s[v] = __builtin_bit_cast(float, (__builtin_bit_cast(int, x) & there) | (~there & (int)0xff800000));
     }
-}
-
-// Workgroups that share a block of n tiles, each with `least` at least.
-__device__ __forceinline__ int cuts_of(const PagedParams &p, int n, int least)
-{
-    return max(1, min(p.splits, n / least));
 }
 
 }  // namespace paged

@@ -28,61 +28,16 @@ constexpr int kPart = 66;  // floats of a wave's part of a row: reference, sum, 
 // and finite: its sums are 0 whatever their weight.
 constexpr float kNone = -FLT_MAX;
 
-// Part `index` of all blocks' parts: its block, how many parts that has, and which one it is; false behind the last. A block's parts go
-// by its share of all keys, so that workgroups hold about as many each, whatever the sequences' lengths (by as many
-// parts for each block, single tokens of 24 sequences of 1 to 20,000 keys on a log scale, 16 heads for 4, 90 us, so 21; of 28
-// of up to 33,462 evenly, 8 heads for one, 51 and 33). Each wave looks by itself. The weights are the keys that a sequence's last
-// token sees, their sums float32 in a fixed order: the same in every workgroup.
-__device__ __forceinline__ bool find_part(const PagedParams &p, int index, Block &x, int &split, int &cuts)
-{
-    const int lane = threadIdx.x & 63;
-    int from = 0, to = 0, len = 0, blocks = 0;
-    float keys = 0.f, all = 0.f;
-    auto look = [&](int b0) __attribute__((always_inline)) {
-        const int b = min(b0 + lane, p.B - 1);
-        from = p.cu_q[b];
-        to = p.cu_q[b + 1];
-        len = p.lens[b];
-        blocks = b0 + lane < p.B ? rows_of(p, from, to).blocks<kRows>(p) : 0;
-        keys = (float)min(max(len, 0), p.most_keys);
-    };
-#pragma nounroll
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        look(b0);
-        all = fmaf((float)blocks, keys, all);
-    }
-    const float each = 1.f / fmaxf(sum_wave(all) * p.share, (float)(kTileLeast * kTile));
-    int before = 0;
-#pragma nounroll
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        if (p.B > 64) look(b0);
-        const int parts_each = min(max((int)fmaf(keys, each, 0.5f), 1), p.splits), parts = blocks * parts_each;
-        const int sum = sum_of(scan_wave(parts, sum_of), before);
-        const uint64_t here = __ballot(parts > 0 && index < sum && index >= sum - parts);
-        if (here) {
-            const int l = __builtin_ctzll(here), at = index - __builtin_amdgcn_readlane(sum - parts, l);
-            const Rows r = rows_of(p, from, to);
-            cuts = __builtin_amdgcn_readlane(parts_each, l);
-            const int block = __builtin_amdgcn_readfirstlane((int)((uint32_t)at / (uint32_t)cuts));
-            split = at - block * cuts;
-            block_of<kRows>(p, x, b0 + l, block, {__builtin_amdgcn_readlane(r.cu, l), __builtin_amdgcn_readlane(r.end, l)},
-                            __builtin_amdgcn_readlane(len, l));
-            return true;
-        }
-        before = __builtin_amdgcn_readlane(sum, 63);
-    }
-    return false;
-}
-
 __global__ void __launch_bounds__(64 * kWaves, 2) tile_kernel(const PagedParams p)
 {
     constexpr int kStep = 33;  // floats between a part's rows in LDS: no conflicts
     __shared__ __attribute__((aligned(1024))) unsigned char v_0[kWaves * kTileBytes], v_1[kWaves * kTileBytes];
     static_assert(2 * kPart * kStep * 4 <= (int)sizeof v_0, "two waves' parts fit a slot array");
-    Block x;
-    int split = 0, cuts = 1;
-    if (!(p.splits > 1 ? find_part(p, blockIdx.y, x, split, cuts) : find_block<kRows>(p, blockIdx.x, x))) return;
-    const int hk = p.splits > 1 ? blockIdx.x : blockIdx.y;
+    Part part;
+    if (!(p.splits > 1 ? find_part<kRows, false>(p, [](int) { return (int)blockIdx.y; }, part) : find_block<kRows>(p, blockIdx.x, part.x)))
+        return;
+    const Block &x = part.x;
+    const int hk = p.splits > 1 ? blockIdx.x : blockIdx.y, split = p.splits > 1 ? part.split : 0, cuts = p.splits > 1 ? part.cuts : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hh = lane >> 5, ql = lane & 31;
 
@@ -345,8 +300,8 @@ hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
     if (rows == 128) return launch_paged_wide(p, s);
     // Parts of all blocks: a block's share of kTileParts, rounded, and at least one. Heads first, so that workgroups without a part come
     // last: between the others each left a CU with two and one with none (one token over 43,961 keys 17.5 us, so 14).
-    const unsigned parts = (unsigned)(p.blocks + kTileParts / p.H_kv + 1), H_kv = (unsigned)p.H_kv;
-    hipLaunchKernelGGL(tile_kernel, p.splits > 1 ? dim3(H_kv, parts) : dim3((unsigned)p.blocks, H_kv), dim3(64 * kWaves), 0, s, p);
+    const unsigned H_kv = (unsigned)p.H_kv;
+    hipLaunchKernelGGL(tile_kernel, p.splits > 1 ? dim3(H_kv, (unsigned)p.parts) : dim3((unsigned)p.blocks, H_kv), dim3(64 * kWaves), 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.splits == 1) return hipSuccess;
     const int64_t all = (int64_t)p.H * p.N;

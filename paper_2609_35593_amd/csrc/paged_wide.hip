@@ -22,18 +22,13 @@ namespace {
 using namespace paged;
 
 constexpr int kRows = 128;
+constexpr int kRun = 8;
 constexpr float kSumLimit = 0x1p50f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
 typedef const __attribute__((address_space(1))) void global_void;
-
-// Where a split's part of a block lies, in parts.
-__device__ __forceinline__ int64_t part_at(const PagedParams &p, int split, int hk, int block)
-{
-    return ((int64_t)split * p.H_kv + hk) * p.blocks + block;
-}
 
 // Eight rows from one on: at most 7 token strides of 2^22 elements and a row.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const unsigned char *row)
@@ -47,21 +42,28 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     __shared__ __attribute__((aligned(1024))) unsigned char k_0[kTileBytes], k_1[kTileBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char v_0[kTileBytes], v_1[kTileBytes];
 
-    // Contiguous runs of (K/V head, block) per XCD, last blocks first.
-    const int items = p.H_kv * p.blocks, per = (items + 7) / 8;
-    const int id = blockIdx.x + gridDim.x * blockIdx.y, at = (id & 7) * per + (id >> 3);
-    if ((id >> 3) >= per || at >= items) return;
-    const int hk = at / p.blocks, split = blockIdx.z;
-    const int block = p.blocks - 1 - (at - hk * p.blocks);
-    Block x;
-    if (!find_block<kRows>(p, block, x)) return;
+    // Runs of kRun blocks or parts of a K/V head, which see about the same keys, to the XCDs in turn, heads first, the last blocks first;
+    // workgroups that have nothing come last. (An eighth of them all to each XCD, empty ones among them: 24 prompts of 30 to
+    // 6,000 tokens on a log scale, 8 heads for 2, 288 us, so 149; of equal ones 1,183 and 1,205. Runs of 4 / 8 / 16 / 32: 148 / 149
+    // / 152 / 163.)
+    const int id = blockIdx.x + gridDim.x * blockIdx.y, turn = id >> 3, run = turn / kRun * 8 + (id & 7);
+    const int hk = run % p.H_kv;
+    auto pick = [&](int n) __attribute__((always_inline)) { return n - 1 - (run / p.H_kv * kRun + turn % kRun); };
+    Part part;
+    part.split = 0, part.cuts = 1;
+    if (p.splits > 1) {
+        if (!find_part<kRows, true>(p, [&](int n) __attribute__((always_inline)) { return pick(min(n, p.parts)); }, part)) return;
+    } else {
+        const int block = pick(p.blocks);
+        if (block < 0 || !find_block<kRows>(p, block, part.x)) return;
+    }
+    const Block &x = part.x;
+    const int split = part.split, cuts = part.cuts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hh = lane >> 5, ql = lane & 31;
 
     const Seen s_first = seen_at(p, x.pos0 + x.t0, x.len), s_last = seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len);
     const Tiles tl = tiles_of(s_first, s_last);
-    const int cuts = cuts_of(p, tl.n, kWideLeast);
-    if (split >= cuts) return;
     const int begin = (int)((int64_t)tl.n * split / cuts), end = (int)((int64_t)tl.n * (split + 1) / cuts);
 
     // What the wave's rows and this lane's row see (rows behind the last repeat it), the lane's against its first key
@@ -263,15 +265,16 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     }
 
     sum += __shfl_xor(sum, 32);
+    if (p.splits > 1 && split == 0 && hk == 0 && threadIdx.x == 0 && part.block < p.blocks) p.cut[part.block] = make_int4(part.first, part.step, cuts, 0);
     if (cuts > 1) {
         // A part as the lanes hold it: whole lines, read back by wide_join_kernel the same way. (By rows they were written and read
         // in pieces of 32 bytes: 512 blocks cut in three 86 us, so 77.)
-        const int64_t part = part_at(p, split, hk, block);
+        const int64_t at = (int64_t)hk * p.parts + part.first + split * part.step;
 #pragma unroll
         for (int v = 0; v < 8; ++v)
-            *reinterpret_cast<f32x4 *>(p.part + (part * 4 + wave) * 2048 + v * 256 + lane * 4) =
+            *reinterpret_cast<f32x4 *>(p.part + (at * 4 + wave) * 2048 + v * 256 + lane * 4) =
                 f32x4{acc[v >> 2][(v & 3) * 4], acc[v >> 2][(v & 3) * 4 + 1], acc[v >> 2][(v & 3) * 4 + 2], acc[v >> 2][(v & 3) * 4 + 3]};
-        if (hh == 0) p.part_row[part * kRows + wave * 32 + ql] = make_float2(ref, sum);
+        if (hh == 0) p.part_row[at * kRows + wave * 32 + ql] = make_float2(ref, sum);
         return;
     }
     if (wave * 32 + ql >= x.left) return;
@@ -287,16 +290,17 @@ __global__ void __launch_bounds__(256) wide_join_kernel(const PagedParams p)
     const int id = blockIdx.x + gridDim.x * blockIdx.y;
     if (id >= p.H_kv * p.blocks) return;
     const int hk = id / p.blocks, block = id - hk * p.blocks, quad0 = blockIdx.z * 2;
+    const int4 cut = p.cut[block];
     Block x;
     if (!find_block<kRows>(p, block, x)) return;
-    const int n = cuts_of(p, tiles_of(seen_at(p, x.pos0 + x.t0, x.len), seen_at(p, x.pos0 + row_of(p, x, x.left - 1).t, x.len)).n,
-                          kWideLeast);
-    if (n == 1) return;
+    const int n = min(cut.z, p.splits);
+    if (n <= 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5, ql = lane & 31;
     const References refs = p.refs;
-    const int64_t step = (int64_t)p.H_kv * p.blocks;  // parts between splits
-    const float2 *rows = p.part_row + part_at(p, 0, hk, block) * kRows + wave * 32 + ql;
-    const float *from = p.part + (part_at(p, 0, hk, block) * 4 + wave) * 2048 + quad0 * 256 + lane * 4;
+    // (Clamped: where offsets descend, nothing wrote it.)
+    const int first = min(max(cut.x, 0), p.parts - 1), step = min(max(cut.y, 0), p.parts);
+    const float2 *rows = p.part_row + (int64_t)hk * p.parts * kRows + wave * 32 + ql;
+    const float *from = p.part + ((int64_t)hk * p.parts * 4 + wave) * 2048 + quad0 * 256 + lane * 4;
     float top = -INFINITY, sum = 0.f;
     f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     for (int s0 = 0; s0 < n; s0 += 8) {
@@ -307,7 +311,7 @@ __global__ void __launch_bounds__(256) wide_join_kernel(const PagedParams p)
             if (s0 + s < n)
 #pragma unroll
                 for (int e = s; e < s + 2; ++e) {
-                    const int64_t at = min(s0 + e, n - 1) * step;
+                    const int64_t at = min(first + min(s0 + e, n - 1) * step, p.parts - 1);
                     r[e] = rows[at * kRows];
                     if (s0 + e >= n) r[e].y = 0.f;
                     y[e][0] = *reinterpret_cast<const f32x4 *>(from + at * 8192);
@@ -353,16 +357,20 @@ __global__ void __launch_bounds__(256) wide_join_kernel(const PagedParams p)
 hipError_t launch_paged_wide(const PagedParams &p, hipStream_t s)
 {
     // (A grid's threads in one dimension stay below 2^32.)
-    const int64_t ids = ((int64_t)p.H_kv * p.blocks + 7) / 8 * 8;
-    const unsigned wide = ids < (1 << 20) ? (unsigned)ids : 1u << 20;
-    const dim3 grid(wide, (unsigned)((ids + wide - 1) / wide), (unsigned)p.splits), block(256);
+    auto grid_of = [](int64_t ids) {
+        const unsigned wide = ids < (1 << 20) ? (unsigned)ids : 1u << 20;
+        return dim3(wide, (unsigned)((ids + wide - 1) / wide));
+    };
+    const int64_t blocks = (int64_t)p.H_kv * p.blocks, runs = (int64_t)((p.splits > 1 ? p.parts : p.blocks) + kRun - 1) / kRun * p.H_kv;
+    const dim3 grid = grid_of((runs + 7) / 8 * 8 * kRun), block(256);
     if (p.lse)
         hipLaunchKernelGGL((wide_kernel<true>), grid, block, 0, s, p);
     else
         hipLaunchKernelGGL((wide_kernel<false>), grid, block, 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.splits == 1) return hipSuccess;
-    hipLaunchKernelGGL(wide_join_kernel, dim3(grid.x, grid.y, 4), block, 0, s, p);
+    const dim3 join = grid_of(blocks);
+    hipLaunchKernelGGL(wide_join_kernel, dim3(join.x, join.y, 4), block, 0, s, p);
     return hipGetLastError();
 }
 

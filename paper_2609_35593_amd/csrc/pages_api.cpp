@@ -255,10 +255,10 @@ PagedSpace paged_space(const ress_paged_shape *s, const PagedPlan &plan)
 {
     PagedSpace w = {0, 0, 0, 0};
     if (plan.splits > 1) {
-        const size_t rows = plan.rows == 32 ? (size_t)s->H * s->N : (size_t)s->H_kv * plan.blocks * 128;
-        w.rows = plan.splits * rows * 64 * sizeof(float);
-        w.cuts = w.rows + plan.splits * rows * sizeof(float2);
-        w.starts = w.cuts + (plan.rows == 32 ? rows * sizeof(int32_t) : 0);
+        const size_t rows = plan.rows == 32 ? (size_t)plan.splits * s->H * s->N : (size_t)s->H_kv * plan.parts * 128;
+        w.rows = rows * 64 * sizeof(float);
+        w.cuts = w.rows + rows * sizeof(float2);
+        w.starts = w.cuts + (plan.rows == 32 ? (size_t)s->H * s->N * sizeof(int32_t) : plan.blocks * sizeof(int4));
     }
     w.bytes = align256(w.starts + (plan.blocks > 0 && s->B > kMostScanned ? ((size_t)s->B + 1) * sizeof(int32_t) : 0));
     return w;
@@ -495,7 +495,8 @@ int ress_paged_attn(const ress_paged_shape *shape, const void *q, const void *k,
     p.table_stride = s.table_stride;
     p.blocks = plan.blocks;
     p.splits = plan.splits;
-    p.share = (float)s.H_kv / kTileParts;
+    p.parts = plan.parts;
+    if (plan.splits > 1) p.share = (float)s.H_kv / (float)plan.target;
     const int64_t reach = window_tokens(s.frame, s.window) + s.n_sink;
     p.most_keys = (int)(reach < p.capacity ? reach : p.capacity);
     p.scale = scale;
@@ -525,7 +526,10 @@ int ress_paged_attn(const ress_paged_shape *shape, const void *q, const void *k,
     if (plan.splits > 1) {
         p.part = reinterpret_cast<float *>(w);
         p.part_row = reinterpret_cast<float2 *>(w + space.rows);
-        p.cuts = reinterpret_cast<int32_t *>(w + space.cuts);
+        if (plan.rows == 32)
+            p.cuts = reinterpret_cast<int32_t *>(w + space.cuts);
+        else
+            p.cut = reinterpret_cast<int4 *>(w + space.cuts);
     }
     return launch_paged(p, plan.rows, stream) == hipSuccess ? RESS_OK : RESS_E_HIP;
 }

@@ -84,7 +84,8 @@ struct PagedParams {
     int64_t table_stride;
     int blocks;  // of all sequences, at most
     int splits;  // workgroups that share a block's keys, at most
-    float share;    // 32 rows, splits > 1: of all sequences' keys of a K/V head, what a workgroup takes
+    int parts;      // splits > 1: of all blocks of a K/V head, at most
+    float share;    // splits > 1: of all sequences' keys of a K/V head, what a workgroup takes
     int most_keys;  // that a token sees
     References refs;
     float scale, scale_log2;
@@ -99,10 +100,12 @@ struct PagedParams {
     uint16_t *o;
     float *lse;
     // splits > 1: unnormalised outputs, and references and sums. 32 rows: [splits][H][N] of 64 floats, and [H][N], the
-    // workgroups that share a row's keys. 128 rows: [splits][H_kv][blocks] of 128 x 64, as the lanes hold them.
+    // workgroups that share a row's keys. 128 rows: [H_kv][parts] of 128 x 64, as the lanes hold them, and [blocks], the first part, how
+    // far the next ones are, and how many.
     float *part;
     float2 *part_row;
     int32_t *cuts;
+    int4 *cut;
     int32_t *starts;  // [B + 1], of more than kMostScanned sequences: blocks before each one's, and all
 };
 
@@ -110,6 +113,7 @@ constexpr int kMostScanned = 512;  // (see find_block)
 struct PagedPlan {
     int rows;    // of a block
     int blocks, splits;
+    int target, parts;  // splits > 1: workgroups that keys are cut for, parts of a K/V head at most
 };
 PagedPlan paged_plan(const ress_paged_shape *s);
 constexpr int kMaxPagedSplits = 64;

@@ -26,7 +26,7 @@ int head_bwd_parts(int H_all, int N)
 
 PagedPlan paged_plan(const ress_paged_shape *s)
 {
-    PagedPlan r = {32, 0, 1};
+    PagedPlan r = {32, 0, 1, 0, 0};
     if (s->B == 0 || s->N == 0 || s->H == 0) return r;
     const int64_t group = s->H / s->H_kv, rows = s->N * group, some = s->B < s->N ? s->B : s->N;
     // Blocks of 128 rows where sequences have more than 32 on average.
@@ -44,6 +44,7 @@ PagedPlan paged_plan(const ress_paged_shape *s)
         // heads for 4, 242 / 46; 250 of 1 to 6,000 evenly, one K/V head, 56 / 50, all of 3,000 36 / 38; 96 with 4 K/V heads 77 /
         // 75, all of 3,000 55 / 57.)
         if (s->B > kMostCut || n > 1024 || tiles < 2 * kTileLeast) return r;
+        r.target = kTileParts;
         want = kTileParts / s->H_kv;
         if (want > 8192 / n) want = 8192 / n;
         if (want > 16 && (int64_t)s->H * s->N > 512) want = 16;
@@ -53,18 +54,27 @@ PagedPlan paged_plan(const ress_paged_shape *s)
         // 78 / 84; 176 of 21 32.0 / 33.4.
         return r;
     } else {
-        // As many as fill the chip's 1,024 places once, by 80% at least and not to the last one, else nearly half as many
-        // again; long lists are cut further, into parts of 40 tiles. 1 / 2 / 3 / 4 / 6 / 8 / 16: 440 blocks of up to 66 tiles 107 / 94 /
-        // 92 / 92 / 92 / 94 / 92; 880 139 / 160 / 156; 512 of up to 64 102 / 90 / 77 / 77 / 78 / 78; 220 of 66 85 / 65 / 59 / 57 / 62; 176 of 86
-        // 106 / 81 / 72 / 61 / 68 / 64 / 64; 176 of 687 782 / 523 / 434 / 341 / 370 / 330 / 310; 128 of 64 78 / 48 / 45 / 38 / 37.
+        // Parts by keys here too, for as many workgroups as fill the chip's 1,024 places once, by 80% at least and not to the last one, else
+        // nearly half as many again; long lists are cut further, into parts of 40 tiles. By parts of a block, 1 / 2 / 3 / 4 / 6 / 8 /
+        // 16: 440 blocks of up to 66 tiles 107 / 94 / 92 / 92 / 92 / 94 / 92; 880 139 / 160 / 156; 512 of up to 64 102 / 90 / 77 / 77 / 78
+        // / 78; 220 of 66 85 / 65 / 59 / 57 / 62; 176 of 86 106 / 81 / 72 / 61 / 68 / 64 / 64; 176 of 687 782 / 523 / 434 / 341 / 370 / 330 /
+        // 310; 128 of 64 78 / 48 / 45 / 38 / 37. (As many parts for every block / by keys: 200 tokens each of 16 sequences of 50 to 20,000 on a
+        // log scale, 16 heads for 4, 178 / 107; 512 each of 12 of 100 to 8,000, 8 heads, 75 / 62; of 4 of 16,384, 16 for 4, 208 / 194.)
+        if (s->B > kMostCut) return r;
         want = 1024 / n;
         if (want * n < 820 || want * n > 1000) want = (1400 + n - 1) / n;
         const int64_t parts = 2816 / n < tiles / 40 ? 2816 / n : tiles / 40;
         if (parts > want) want = parts;
+        // (The workspace stays below 100 MB.)
+        const int64_t room = 2700 - n - s->H_kv;
+        r.target = (int)(want * n < room ? want * n : room);
+        want = kMaxPagedSplits;
         most = tiles / kWideLeast;
     }
     const int64_t splits = want < most ? want : most;
     r.splits = (int)(splits < 1 ? 1 : splits > kMaxPagedSplits ? kMaxPagedSplits : splits);
+    // (A block's share of the target, rounded, and at least one.)
+    r.parts = r.blocks + r.target / s->H_kv + 1;
     return r;
 }
 

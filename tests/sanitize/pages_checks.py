@@ -80,11 +80,11 @@ for n_pages, page, st in itertools.product(edge, edge, ((0, 0, 0), (1 << 20, 64,
     pg = ress_page_strides(*st)
     s, c = ress_head_norm_shape(rope, 1, 1e-5), ress_page_cache(n_pages, page, pg, pg, x)
     legal(lib.ress_qk_norm_rope_pages(C.byref(s), C.byref(c), *P[:12], None))
-out = (C.c_int * 4)()
+out = (C.c_int * 5)()
 for _ in range(20000):
     H, N, each = rng.choice((0, 1, 2, 20, 511, 512)), rng.choice((0, 1, 2 ** rng.randrange(25), rng.randrange(1, TOKENS))), rng.choice((4, 8, 16, 32, 64, 128))
     lib.plan_head_bwd(H, N, each, out)
-    tokens, heads, parts, most = out
+    tokens, heads, parts, most = out[:4]
     if H == 0 or N == 0:
         assert parts == 0 and most == 1
         continue
@@ -114,13 +114,15 @@ def paged(B, N, H, H_kv, page, n_pages, max_pages, frame, window, sink, k=(1 << 
     if n is None:
         return False
     lib.plan_paged(C.byref(s), out)
-    rows, blocks, splits = out[:3]
+    rows, blocks, splits, most, target = out[:5]
     assert n <= 100e6, what
     if B and N and H:
         seen["rows"].add(rows)
         seen["splits"].add((rows, splits))
-        share = H * N if rows == 32 else H_kv * blocks * 128
-        parts = 0 if splits == 1 else splits * share * 264 + (4 * share if rows == 32 else 0)
+        parts = 0
+        if splits > 1:
+            parts = H * N * (splits * 264 + 4) if rows == 32 else H_kv * most * 128 * 264 + 16 * blocks
+            assert B <= 256 and 1 <= target and most == blocks + target // H_kv + 1, what
         assert n == (parts + (4 * (B + 1) if B > 512 else 0) + 255) // 256 * 256, what
     st = legal(lib.ress_paged_attn(C.byref(s), *P[:6], 0.125, P[6], P[7], P[8], n, None))
     assert st == (E_HIP if B and N and H else 0), (what, st)

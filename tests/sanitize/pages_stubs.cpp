@@ -77,7 +77,7 @@ extern "C" {
 void plan_paged(const ress_paged_shape *s, int *out)
 {
     const ress::PagedPlan p = ress::paged_plan(s);
-    out[0] = p.rows, out[1] = p.blocks, out[2] = p.splits;
+    out[0] = p.rows, out[1] = p.blocks, out[2] = p.splits, out[3] = p.parts, out[4] = p.target;
 }
 void plan_head_bwd(int H_all, int N, int tokens_each, int *out)
 {

@@ -151,6 +151,23 @@ def test_offsets_that_descend_or_pass_the_rows(ress):
         assert (buf[:, :3] == 7.0).all() and (buf[:, 20:] == 7.0).all()
 
 
+@pytest.mark.parametrize("N", [12, 700])
+def test_offsets_in_no_order_where_keys_are_cut(ress, N):
+    """The same with keys that are cut over workgroups, whose parts stay in their workspace."""
+    B, g = 5, torch.Generator().manual_seed(N)
+    q, k, v, cu, tables = _state(4, 4, 2, 16, [9000, 7000, 3, 4000, 6000], [N // 5] * B, padding=N - N // 5 * 5)
+    k, v = k.nan_to_num(0.5), v.nan_to_num(0.5)
+    n = ress.ress_paged_attn_workspace_size(B, 4, 2, N, page=16, max_pages=tables.shape[1], n_pages=k.shape[0], window=8000)
+    assert n > 0
+    ws, buf = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda"), torch.full((4, N + 20, 64), 7.0, dtype=BF, device="cuda")
+    bad = [[0] + [10 ** 9] * B, [N, N // 2, 0, N, 0, N], [0, N, 0, N, 0, N], list(range(N, N - 6, -1))]
+    bad += [torch.randint(-20, N + 20, (B + 1,), generator=g).tolist() for _ in range(20)]
+    for cu in bad:
+        ress.ress_paged_attn(q, k, v, _t(cu), _t([9000, 7000, 3, 4000, 6000]), tables, window=8000, out=buf[:, 10:N + 10], workspace=ws[:n])
+        torch.cuda.synchronize()
+        assert (buf[:, :10] == 7.0).all() and (buf[:, N + 10:] == 7.0).all() and (ws[n:] == 77).all()
+
+
 def test_thousands_of_offsets_in_no_order(ress):
     """The same with a list of where blocks begin."""
     g = torch.Generator().manual_seed(3)
@@ -247,7 +264,8 @@ def test_many_sequences(ress):
 
 
 @pytest.mark.parametrize("B,H,H_kv,top,new", [(60, 8, 4, 6000, 1), (60, 8, 4, 6000, 30), (130, 2, 1, 5000, 1), (130, 2, 1, 5000, 90),
-                                              (256, 2, 2, 700, 1), (257, 2, 2, 700, 1), (40, 16, 16, 900, 1)])
+                                              (256, 2, 2, 700, 1), (257, 2, 2, 700, 1), (40, 16, 16, 900, 1), (12, 8, 8, 8000, 150),
+                                              (256, 2, 1, 2000, 100), (257, 2, 1, 2000, 100)])
 def test_uneven_lengths(ress, B, H, H_kv, top, new):
     """Keys cut by sequences' lengths, from one to `top` on a log scale: single tokens and chunks, some sequences without any."""
     lens = [round(top ** (i / (B - 1))) for i in range(B)]
