@@ -12,7 +12,7 @@
 //
 // Measured: one token of 16 heads for 4 over 43,961 keys 13 us and the join 3.3, where their 45 MB take 8.5: 256 workgroups, a wave of
 // which waits for 2 or 3 tiles one behind the other. One token of each of 4,096 sequences over 1,000 keys of one K/V head 203 us, 5.2
-// TB/s, a copy's rate.
+// TB/s, a copy's rate. One token of each of 24 sequences of 1 to 20,000 keys on a log scale, 16 heads for 4, 21 us.
 #include <float.h>
 
 #include "paged_device.h"

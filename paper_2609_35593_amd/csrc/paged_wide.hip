@@ -10,10 +10,11 @@
 // address a lane. Keys on a page
 // outside the cache, and keys that no row of the block sees, come from a row of zeros, their scores hidden.
 //
-// Measured: 8 sequences of four new frames each over a window of 3 and the first, 16 heads, 1,036 to 1,046 us, 860 TFLOP/s by the formula:
-// bound by issue slots, the matrix unit busy 41% of the cycles, the vector unit 58%, its clock lower the busier both are. A frame
-// over 31, cut into 16 parts and with the logarithm, 308 us and the join 18. 24 ragged sequences 84 us and the join 9: 386 blocks
-// of some 60 tiles in two parts each, of which a CU gets one to four, 0.8 to 1.0 us a tile and CU where full CUs take 0.67.
+// Measured: 8 sequences of four new frames each over a window of 3 and the first, 16 heads, 1,031 to 1,046 us, 860 TFLOP/s by the formula:
+// bound by issue slots, the matrix unit busy 40% of the cycles, the vector unit 58%, its clock lower the busier both are. A frame
+// over 31, cut into 14 parts and with the logarithm, 315 us and the join 16. 24 ragged sequences 80 us and the join 11: 386 blocks of
+// some 60 tiles in three parts each, more workgroups than places and not twice as many, so the last ones run in CUs half empty
+// (matrix unit busy 30%).
 #include "paged_device.h"
 
 namespace ress {
