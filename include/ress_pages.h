@@ -45,9 +45,9 @@ typedef struct {
 /* Between the projection and the attention, for every token and head of Q and of K
  *   y = turn(pos, (x - mean) rstd gamma + beta),  rstd = 1 / sqrt(var + eps),
  * with mean and variance over the head's D channels (RMS: mean 0, the variance the mean
- * square) and ress_rope's turn. Float32 (the variance from centred values; values up to 2^56), angles
- * as in ress_rope, rounded once to the type: what ress_layer_norm and ress_rope would round
- * in between is kept.
+ * square) and ress_rope's turn. Float32 (the mean is taken from the values before their squares and
+ * products; values up to 2^56), angles as in ress_rope, rounded once to the type: what ress_layer_norm
+ * and ress_rope would round in between is kept.
  *   pos                device int32 [N][n_axes]
  *   q_in, q_out        [H][N][D] by rope.q and rope.q_out; NULL where H is 0
  *   k_in, k_out        [H_kv][N][D] likewise; NULL where H_kv is 0

@@ -4,7 +4,7 @@
 // rope.hip a thread owns one chunk of a token's channels and walks over the heads, the angles
 // formed once; a head's chunks lie in `lanes` neighbouring lanes of a wave, which add up the row's sums among
 // themselves. Norm and turn are one step: an output is
-//   rstd (x_own A + x_other B - mean (A + B)) + C,
+//   rstd ((x_own - mean) A + (x_other - mean) B) + C,
 //   A = gamma_own cos, B = -+ gamma_other sin, C = beta_own cos -+ beta_other sin,
 // with coefficients that are kept over a token's heads; the weights they are formed from lie in LDS (read from
 // memory a value at a time they took longer than 4 heads of a token). The chunk that a chunk's pairs meet is
@@ -296,14 +296,15 @@ struct Batch {
         if (!store) return;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const float rstd = 1.f / sqrtf(fmaf(q[j], width, eps)), mr = -m[j] * rstd;
+            const float rstd = 1.f / sqrtf(fmaf(q[j], width, eps));
             forget(xo[j]);
             Chunk<T, V> y;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float z = get(INTERLEAVED ? xo[j].e[e ^ 1] : xp[j].e[e]);
-                const float t = fmaf(z, b[e], get(xo[j].e[e]) * a[e]);
-                put(y.e[e], fmaf(t, rstd, LAYER ? fmaf(mr, a[e] + b[e], c[e]) : c[e]));
+                // (Centred before the products: behind them, mean (A + B) would take away the digits of rows far from zero.)
+                const float z = get(INTERLEAVED ? xo[j].e[e ^ 1] : xp[j].e[e]) - (LAYER ? m[j] : 0.f);
+                const float x_own = get(xo[j].e[e]) - (LAYER ? m[j] : 0.f);
+                put(y.e[e], fmaf(fmaf(z, b[e], x_own * a[e]), rstd, c[e]));
             }
             *reinterpret_cast<Chunk<T, V> *>(rows.out + (h + j) * rows.out_step + x.c * V) = y;
             __builtin_amdgcn_sched_barrier(0);  // (one head's values at a time)
