@@ -29,6 +29,19 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
+// The sum of 16 values, in pairs.
+__device__ __forceinline__ float add_pairs(const f32x16 &x)
+{
+    float y[8];
+#pragma unroll
+    for (int v = 0; v < 8; ++v) y[v] = x[2 * v] + x[2 * v + 1];
+#pragma unroll
+    for (int n = 4; n > 0; n /= 2)
+#pragma unroll
+        for (int v = 0; v < n; ++v) y[v] = y[2 * v] + y[2 * v + 1];
+    return y[0];
+}
+
 typedef const __attribute__((address_space(1))) void global_void;
 
 // Eight rows from one on: at most 7 token strides of 2^22 elements and a row.
@@ -139,7 +152,10 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
 
     const Reader rd(lane);
     const References refs = p.refs;
-    float ref = 0.f, sum = 0.f;  // reference and the lane's half of the row's sum
+    // Reference, and the lane's halves of the row's sums: of weights as they enter the product with V, so that those sum to one,
+    // and (LSE) before they are rounded. (With the second alone a frame over 31 took 331 us for 348, but values
+    // that are all alike came out off by up to 2^-8 of themselves.)
+    float ref = 0.f, sum = 0.f, mass = 0.f;
     bool has = false;            // the row has a reference
     f32x16 acc[2];
 #pragma unroll
@@ -170,11 +186,11 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
         }
         return refs.of(fmaxf(m, __shfl_xor(m, 32)));
     };
-    // Probabilities against the row's reference, and the lane's part of their sum. (any_far: some rows'
-    // references may be far.)
-    auto probs = [&](bool any_far, bool part, uint64_t keys, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2])
+    // Probabilities against the row's reference, and the lane's part of their sum, rounded (returned) and as they are. (any_far:
+    // some rows' references may be far.)
+    auto probs = [&](bool any_far, bool part, uint64_t keys, const unsigned char *kt, int key0, bf16x8 (&pb)[2][2], float &exact)
                      __attribute__((always_inline)) {
-        float l0 = 0.f, l1 = 0.f;
+        float l = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x16 s;
@@ -189,20 +205,18 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
                 for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], refs.scale, -ref));
             }
             pack(s, pb[u]);
+            l = add_up(pb[u], l);
             if constexpr (LSE) {
-#pragma unroll
-                for (int v = 0; v < 16; v += 2) l0 += s[v], l1 += s[v + 1];
+                exact = u == 0 ? add_pairs(s) : exact + add_pairs(s);
                 __builtin_amdgcn_sched_barrier(0);  // (else both halves' float32 values are held: spills)
-            } else {
-                l0 = add_up(pb[u], l0);
             }
         }
-        return l0 + l1;
+        return l;
     };
     auto tile = [&](bool part, uint64_t keys, const unsigned char *kt, const unsigned char *vt, int key0)
                     __attribute__((always_inline)) {
         bf16x8 pb[2][2];
-        float l;
+        float l, exact = 0.f;
         // (Rare: a row's first tile, or logits far above those so far. Lanes l and l^32 share the
         // row and decide together.)
         bool look = __any(!has), over = false;
@@ -214,6 +228,7 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
                     const float to = has ? fmaxf(ref, m) : m;
                     const float a = has ? __builtin_amdgcn_exp2f(refs.difference(ref, to)) : 0.f;
                     sum *= a;
+                    mass *= a;
 #pragma unroll
                     for (int dh = 0; dh < 2; ++dh)
 #pragma unroll
@@ -222,13 +237,13 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
                     has = true;
                 }
             }
-            l = probs(false, part, keys, kt, key0, pb);
+            l = probs(false, part, keys, kt, key0, pb, exact);
             over = !(l <= kSumLimit);
             const bool far = refs.far(ref);
             if (!__any(over || far)) break;
             if (__any(far)) {
                 asm volatile("" ::: "memory");  // (code of its own: the ordinary form stays in one piece)
-                l = probs(true, part, keys, kt, key0, pb);
+                l = probs(true, part, keys, kt, key0, pb, exact);
                 over = !(l <= kSumLimit);
             }
             look = __any(over);
@@ -236,6 +251,7 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
             over = ((int)over | __shfl_xor((int)over, 32)) != 0;
         }
         sum += l;
+        mass += exact;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -266,11 +282,21 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     }
 
     sum += __shfl_xor(sum, 32);
+    if (LSE) mass += __shfl_xor(mass, 32);
     if (p.splits > 1 && split == 0 && hk == 0 && threadIdx.x == 0 && part.block < p.blocks) p.cut[part.block] = make_int4(part.first, part.step, cuts, 0);
     if (cuts > 1) {
         // A part as the lanes hold it: whole lines, read back by wide_join_kernel the same way. (By rows they were written and read
         // in pieces of 32 bytes: 512 blocks cut in three 86 us, so 77.)
         const int64_t at = (int64_t)hk * p.parts + part.first + split * part.step;
+        if constexpr (LSE) {
+            // One sum goes with a part: the unrounded one, and the products as if its weights had that sum.
+            const float f = sum == 0.f ? 0.f : mass / sum;
+#pragma unroll
+            for (int dh = 0; dh < 2; ++dh)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[dh][v] *= f;
+            sum = sum == 0.f ? 0.f : mass;
+        }
 #pragma unroll
         for (int v = 0; v < 8; ++v)
             *reinterpret_cast<f32x4 *>(p.part + (at * 4 + wave) * 2048 + v * 256 + lane * 4) =
@@ -281,7 +307,7 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     if (wave * 32 + ql >= x.left) return;
     const int h = hk * p.group + r.g;
     store_row(p.o + h * p.os.head + (int64_t)(x.cu + r.t) * p.os.token, acc, inverse(sum), hh);
-    if (LSE && hh == 0) p.lse[(int64_t)h * p.N + x.cu + r.t] = sum == 0.f ? -INFINITY : refs.base2(ref) * kLn2 + logf(sum);
+    if (LSE && hh == 0) p.lse[(int64_t)h * p.N + x.cu + r.t] = sum == 0.f ? -INFINITY : refs.base2(ref) * kLn2 + logf(mass);
 }
 
 // A quarter of the channels of a block whose keys were split, laid out as wide_kernel's: its parts in order, 8 of them on their
