@@ -53,6 +53,8 @@ _declare()
 def _rows(name, t, dtype, H, N, D, dev):
     """Strides (heads, tokens) and the address of a [heads][tokens][channels] tensor whose metadata must be these. (The
     stride of a dimension of one entry says nothing: torch may give any.)"""
+    if t is None:
+        raise ValueError(f"{name} must be given")
     head, token, channel = t.stride()
     if t.dtype is not dtype or t.shape != (H, N, D) or t.device != dev or channel != 1:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {(H, N, D)} on {dev} with contiguous channels")
@@ -145,6 +147,8 @@ def ress_qk_norm_rope(q, k, pos, *, dims, norm: str = "layer", q_gamma=None, q_b
 
 def _paged(name, t, dtype, shape, dev):
     """Strides (pages, heads, tokens) and the address of [pages][heads][tokens][channels] with this metadata."""
+    if t is None:
+        raise ValueError(f"{name} must be given")
     page, head, token, channel = t.stride()
     if t.dtype is not dtype or t.shape != shape or t.device != dev or (channel != 1 and shape[3] > 1):
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {dev} with contiguous channels")
@@ -158,8 +162,8 @@ def ress_qk_norm_rope_pages(q, k, v, pos, slots, k_pages, v_pages, *, dims, norm
     """ress_qk_norm_rope with k written into k_pages and v [H_kv][N][D] copied into v_pages (both [n_pages][H_kv][page][D],
     any strides with contiguous channels), token t at slots[t] (int32 [N]; a token without a slot in the cache is left
     out). q may be None. Returns q, k_pages and v_pages."""
-    if k is None or v is None:
-        raise ValueError("k and v must be given")
+    if k is None or v is None or k_pages is None:
+        raise ValueError("k, v and k_pages must be given")
     dtype, code, dev, N, D = _first(k, None)
     H, H_kv, pages = 0, k.shape[0], k_pages.shape
     if len(pages) != 4 or pages[1] != H_kv or pages[3] != D:
@@ -324,6 +328,8 @@ def ress_paged_attn(q, k_pages, v_pages, cu_q, lens, tables, *, window: int, fra
     [n_pages][H_kv][page][64]; any strides with contiguous channels; lens: int32 [B], the new tokens counted; tables: int32
     [B][max_pages]; window, frame, n_sink: as for ress_window_attn, causal. Returns o (bf16, as q) and, with want_lse or a
     given buffer, lse (float32 [H][N]); their rows outside every sequence are not written."""
+    if q is None or k_pages is None:
+        raise ValueError("q and k_pages must be given")
     dev, qn, kn = _device("q", q), q.shape, k_pages.shape
     if len(qn) != 3 or len(kn) != 4 or qn[2] != kn[3]:
         raise ValueError("q must be [H][N][64], k_pages and v_pages [n_pages][H_kv][page][64]")
