@@ -175,9 +175,12 @@ int ress_paged_attn_workspace_size(const ress_paged_shape *shape, size_t *bytes)
  * whose keys and values are all in its pages. A token at position p sees the keys s < lens[b] that a
  * causal query of ress_window_attn at p sees, but for those on a page outside [0, n_pages):
  *   o = softmax over them of (scale q . k) v
- * in the precision of ress_window_attn. A token that sees no key gets a zero output.
+ * in the precision of ress_window_attn at least: weights are rounded to bf16 for their product with v where N H / H_kv is
+ * more than 32 min(B, N), kept to 16 bits where it is not; those of a row sum to one as they enter it, with lse and
+ * without. A token that sees no key gets a zero output.
  *   q, o       bf16 [H][N][64]; rows of o outside every sequence are left as they are
- *   k, v       bf16 pages; what no token of a block of new tokens sees is not read
+ *   k, v       bf16 pages; what no token of a block of new tokens (up to 128 rows, neighbours in one
+ *              sequence) sees is not read; a NaN or infinity that some of them see may reach the others of the block
  *   cu_q       device int32 [B + 1], ascending, clamped to [0, N] (of offsets that descend, results
  *              mean nothing)
  *   lens       device int32 [B], the new tokens counted, clamped to [0, max_pages * page]. New tokens

@@ -14,11 +14,13 @@
 // Backward: the gradients of gamma and beta stay in registers over all tokens of a workgroup, which
 // leaves one row of partial sums; join_kernel adds the rows in order.
 //
-// Measured (kernels alone; a copy on this card moves 5.2 TB/s): 43,968 tokens of 16 + 16 bf16 heads, layer norm, two axes 79 us, 4.6 TB/s
-// (root mean square 76: the mean is a second chain of sums over lanes); 11,264 rows of 16 + 4 heads into pages, V with them, 16.4 us,
-// 4.2 TB/s (704 workgroups, each with its angles to form and its last stores to wait for). Backward 21,984 tokens 51 us,
-// 5.3 TB/s with some of it from the caches, and the join 4; 1,374 tokens, 12 + 4 float32 heads 10 us and the join 3: 688 workgroups of
-// one trip, which waits for positions, angles in float64, loads, and sums in turn. 24 tokens 5.9 us, the same chain.
+// Measured (a copy on this card moves 5.2 TB/s): 43,968 tokens of 16 + 16 bf16 heads, layer norm, two axes 80 us, 4.5 TB/s
+// (root mean square 77: the mean is a second chain of sums over lanes), float32 143 us, 5.0 TB/s; with axes of 20, 20 and 24
+// channels, by pairs, bf16 97 us, 3.7 TB/s, gradients of 21,984 tokens 97 where chunks take 62. 11,264 rows of 16 + 4 heads into
+// pages, V with them, 16.6 us, 4.2 TB/s (704 workgroups, each with its angles to form and its last stores to wait for). Kernels
+// alone: backward 21,984 tokens 51 us, 5.3 TB/s with some of it from the caches, and the join 4; 1,374 tokens, 12 + 4 float32 heads
+// 10 us and the join 3: 688 workgroups of one trip, which waits for positions, angles in float64, loads, and sums in turn; 24
+// tokens forward 5.9 us, the same chain.
 #include "pages_internal.h"
 
 namespace ress {

@@ -10,7 +10,7 @@
 // Keys on a page outside the cache, and keys that no row of the block sees, are not read: a row of zeros
 // takes their place, and their scores are hidden.
 //
-// Measured: one token of 16 heads for 4 over 43,961 keys 13 us and the join 3.3, where their 45 MB take 8.5: 256 workgroups, a wave of
+// Measured: one token of 16 heads for 4 over 43,961 keys 12.8 us and the join 3.8, where their 45 MB take 8.7: 256 workgroups, a wave of
 // which waits for 2 or 3 tiles one behind the other. One token of each of 4,096 sequences over 1,000 keys of one K/V head 203 us, 5.2
 // TB/s, a copy's rate. One token of each of 24 sequences of 1 to 20,000 keys on a log scale, 16 heads for 4, 21 us.
 #include <float.h>
@@ -299,7 +299,8 @@ hipError_t launch_paged(const PagedParams &p, int rows, hipStream_t s)
     }
     if (rows == 128) return launch_paged_wide(p, s);
     // Parts of all blocks: a block's share of kTileParts, rounded, and at least one. Heads first, so that workgroups without a part come
-    // last: between the others each left a CU with two and one with none (one token over 43,961 keys 17.5 us, so 14).
+    // last: between the others each left a CU with two and one with none (one token over 43,961 keys 17.5 us, so 14). (Blocks that
+    // are not cut lie head by head; those of rows that pad a batch are behind each head's.)
     const unsigned H_kv = (unsigned)p.H_kv;
     hipLaunchKernelGGL(tile_kernel, p.splits > 1 ? dim3(H_kv, (unsigned)p.parts) : dim3((unsigned)p.blocks, H_kv), dim3(64 * kWaves), 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;

@@ -10,11 +10,11 @@
 // address a lane. Keys on a page
 // outside the cache, and keys that no row of the block sees, come from a row of zeros, their scores hidden.
 //
-// Measured: 8 sequences of four new frames each over a window of 3 and the first, 16 heads, 1,031 to 1,046 us, 860 TFLOP/s by the formula:
-// bound by issue slots, the matrix unit busy 40% of the cycles, the vector unit 58%, its clock lower the busier both are. A frame
-// over 31, cut into 14 parts and with the logarithm, 315 us and the join 16. 24 ragged sequences 80 us and the join 11: 386 blocks of
-// some 60 tiles in three parts each, more workgroups than places and not twice as many, so the last ones run in CUs half empty
-// (matrix unit busy 30%).
+// Measured: 8 sequences of four new frames each over a window of 3 and the first, 16 heads, 1,031 to 1,069 us, 806 to 836 TFLOP/s by the
+// formula: bound by issue slots, the matrix unit busy 40% of the cycles, the vector unit 58%, its clock lower the busier both are. A
+// frame over 31, cut into 14 parts and with the logarithm, 332 us and the join 16. 24 ragged sequences 77 to 81 us and the join 11: 408
+// blocks in one to three parts by their sequences' lengths, 1,052 in all, most of 22 tiles, for 1,024 places, so the last ones
+// run in a nearly empty chip (matrix unit busy 30%).
 #include "paged_device.h"
 
 namespace ress {
@@ -56,8 +56,10 @@ __global__ void __launch_bounds__(256, 4) wide_kernel(const PagedParams p)
     __shared__ __attribute__((aligned(1024))) unsigned char k_0[kTileBytes], k_1[kTileBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char v_0[kTileBytes], v_1[kTileBytes];
 
-    // Runs of kRun blocks or parts of a K/V head, which see about the same keys, to the XCDs in turn, heads first, the last blocks first;
-    // workgroups that have nothing come last. (An eighth of them all to each XCD, empty ones among them: 24 prompts of 30 to
+    // Runs of kRun blocks or parts of a K/V head, which see about the same keys, to the XCDs in turn, heads first, the last ones first.
+    // Where keys are cut that is from the last part found, and workgroups that have nothing come last; else from the host's bound of
+    // blocks on, and those of rows that pad a batch come first and end at once (8 prompts of 2,000 tokens, 16 heads, in 16,000 /
+    // 32,000 / 64,000 rows: 399 / 397 / 407 us). (An eighth of them all to each XCD, empty ones among them: 24 prompts of 30 to
     // 6,000 tokens on a log scale, 8 heads for 2, 288 us, so 149; of equal ones 1,183 and 1,205. Runs of 4 / 8 / 16 / 32: 148 / 149
     // / 152 / 163.)
     const int id = blockIdx.x + gridDim.x * blockIdx.y, turn = id >> 3, run = turn / kRun * 8 + (id & 7);

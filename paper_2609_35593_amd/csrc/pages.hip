@@ -6,7 +6,7 @@
 // sequence by bisection in cu_q.
 //
 // Measured: 256 sequences of one new token 5.4 us (lengths, scan, pages, lists: four trips to memory, five barriers of 16 waves), 47 of 1,374
-// tokens each 6.8 and 1.9 for their 65,538 slots and positions. Pages given back by 64 sequences: 2.7 us for the counts, 3.8 for
+// tokens each 6.8 and 1.9 for their 65,538 slots and positions. Pages given back by 64 sequences: 3.0 us for the counts, 4.1 for
 // the stack (a launch between, because a stack's height depends on every sequence before).
 #include "pages_internal.h"
 #include "scan.h"
