@@ -58,7 +58,7 @@ def test_beside_work_that_is_pending(calls, name):
     call may take them, for its outputs or for its workspace."""
     call, side = calls[name], torch.cuda.Stream()
     want = {n: t.clone() for n, t in call().items()}
-    call(stream=side)  # (memory of that stream, which a first call has to ask the driver for)
+    call(stream=side)  # (that stream has memory from here on: no call waits for an allocation)
     done = torch.cuda.Event()
     for turn in range(3):
         scratch = [torch.zeros(1 << n, dtype=torch.uint8, device="cuda") for n in range(9, 29, 2) for _ in range(4)]
